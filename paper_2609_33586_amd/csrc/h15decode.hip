@@ -44,7 +44,7 @@
 // gains 0.3..0.5 us at four query rows a block and loses 4 us at 16.)
 #include <mutex>
 
-#include "attn_device.h"
+#include "unit_device.h"
 
 namespace {
 
@@ -52,113 +52,6 @@ constexpr int NW = 4;               // waves per workgroup
 // instruction classes of __builtin_amdgcn_sched_group_barrier
 constexpr int SG_MFMA = 0x008;
 constexpr int SG_DS_READ = 0x100;
-
-// The scores are next read by inline asm (v_max3_f32, the masking's compare
-// and select), and the compiler inserts no wait states between a matrix-core
-// write and an inline-asm read: this holds the wave for 24, more than the 20
-// that gfx950 requires after a 16-pass write.
-template <int NB>
-__device__ __forceinline__ void settle_unit(f32x16 (&v)[NB]) {
-  if constexpr (NB == 2) asm("s_nop 15\n\ts_nop 7" : "+v"(v[0]), "+v"(v[1]));
-  else asm("s_nop 15\n\ts_nop 7" : "+v"(v[0]));
-}
-
-// y over the scores of a unit (32 or 64 keys) whose key offset lies beyond lim
-template <int NB, int E = 0>
-__device__ __forceinline__ void mask_unit(f32x16 (&v)[NB], int lim, float y) {
-  if constexpr (E < 16 * NB) {
-    constexpr int kb = E / 16, j = E % 16;
-    v[kb][j] = select_beyond<kb * 32 + 8 * (j >> 2) + (j & 3)>(lim, v[kb][j], y);
-    mask_unit<NB, E + 1>(v, lim, y);
-  }
-}
-
-template <int NB>
-__device__ __forceinline__ float unit_max(const f32x16 (&v)[NB]) {
-  // 32 -> 11 -> 4 -> 2 -> 1, or 16 -> 6 -> 2 -> 1
-  if constexpr (NB == 2) {
-    float a[11], b[4];
-#pragma unroll
-    for (int i = 0; i < 10; ++i) {
-      const int e0 = 3 * i, e1 = 3 * i + 1, e2 = 3 * i + 2;
-      a[i] = max3(v[e0 >> 4][e0 & 15], v[e1 >> 4][e1 & 15], v[e2 >> 4][e2 & 15]);
-    }
-    a[10] = max3(v[1][14], v[1][15], v[1][15]);
-    b[0] = max3(a[0], a[1], a[2]);
-    b[1] = max3(a[3], a[4], a[5]);
-    b[2] = max3(a[6], a[7], a[8]);
-    b[3] = max3(a[9], a[10], a[10]);
-    const float c = max3(b[0], b[1], b[2]);
-    return max3(c, b[3], b[3]);
-  } else {
-    float a[5];
-#pragma unroll
-    for (int i = 0; i < 5; ++i) a[i] = max3(v[0][3 * i], v[0][3 * i + 1], v[0][3 * i + 2]);
-    const float b0 = max3(a[0], a[1], a[2]), b1 = max3(a[3], a[4], v[0][15]);
-    return max3(b0, b1, b1);
-  }
-}
-
-// The transposing LDS reads of V operands, with their wait in the same
-// statement: the builtin forms make the compiler wait for every copy into LDS
-// that is in flight, also those of the next round's K.
-// bf16: two blocks of 32 columns (a0, a1), the eight 8-row steps of 64 keys
-template <int RB>
-__device__ __forceinline__ void read_v16(i32x2v (&r)[16], uint32_t a0, uint32_t a1) {
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:%18\n\t"
-      "ds_read_b64_tr_b16 %2, %16 offset:%19\n\tds_read_b64_tr_b16 %3, %16 offset:%20\n\t"
-      "ds_read_b64_tr_b16 %4, %16 offset:%21\n\tds_read_b64_tr_b16 %5, %16 offset:%22\n\t"
-      "ds_read_b64_tr_b16 %6, %16 offset:%23\n\tds_read_b64_tr_b16 %7, %16 offset:%24\n\t"
-      "ds_read_b64_tr_b16 %8, %17\n\tds_read_b64_tr_b16 %9, %17 offset:%18\n\t"
-      "ds_read_b64_tr_b16 %10, %17 offset:%19\n\tds_read_b64_tr_b16 %11, %17 offset:%20\n\t"
-      "ds_read_b64_tr_b16 %12, %17 offset:%21\n\tds_read_b64_tr_b16 %13, %17 offset:%22\n\t"
-      "ds_read_b64_tr_b16 %14, %17 offset:%23\n\tds_read_b64_tr_b16 %15, %17 offset:%24\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7]),
-        "=&v"(r[8]), "=&v"(r[9]), "=&v"(r[10]), "=&v"(r[11]), "=&v"(r[12]), "=&v"(r[13]), "=&v"(r[14]), "=&v"(r[15])
-      : "v"(a0), "v"(a1), "n"(8 * RB), "n"(16 * RB), "n"(24 * RB), "n"(32 * RB), "n"(40 * RB), "n"(48 * RB),
-        "n"(56 * RB)
-      : "memory");
-}
-// the four 8-row steps of 32 keys
-template <int RB>
-__device__ __forceinline__ void read_v16(i32x2v (&r)[8], uint32_t a0, uint32_t a1) {
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%10\n\t"
-      "ds_read_b64_tr_b16 %2, %8 offset:%11\n\tds_read_b64_tr_b16 %3, %8 offset:%12\n\t"
-      "ds_read_b64_tr_b16 %4, %9\n\tds_read_b64_tr_b16 %5, %9 offset:%10\n\t"
-      "ds_read_b64_tr_b16 %6, %9 offset:%11\n\tds_read_b64_tr_b16 %7, %9 offset:%12\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
-      : "v"(a0), "v"(a1), "n"(8 * RB), "n"(16 * RB), "n"(24 * RB)
-      : "memory");
-}
-// fp8: two blocks of 32 columns, the four 16-row steps of 64 keys
-template <int RB>
-__device__ __forceinline__ void read_v8(i32x2v (&r)[8], uint32_t a0, uint32_t a1) {
-  asm volatile(
-      "ds_read_b64_tr_b8 %0, %8\n\tds_read_b64_tr_b8 %1, %8 offset:%10\n\t"
-      "ds_read_b64_tr_b8 %2, %8 offset:%11\n\tds_read_b64_tr_b8 %3, %8 offset:%12\n\t"
-      "ds_read_b64_tr_b8 %4, %9\n\tds_read_b64_tr_b8 %5, %9 offset:%10\n\t"
-      "ds_read_b64_tr_b8 %6, %9 offset:%11\n\tds_read_b64_tr_b8 %7, %9 offset:%12\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
-      : "v"(a0), "v"(a1), "n"(16 * RB), "n"(32 * RB), "n"(48 * RB)
-      : "memory");
-}
-
-// the two 16-row steps of 32 keys
-template <int RB>
-__device__ __forceinline__ void read_v8(i32x2v (&r)[4], uint32_t a0, uint32_t a1) {
-  asm volatile(
-      "ds_read_b64_tr_b8 %0, %4\n\tds_read_b64_tr_b8 %1, %4 offset:%6\n\t"
-      "ds_read_b64_tr_b8 %2, %5\n\tds_read_b64_tr_b8 %3, %5 offset:%6\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
-      : "v"(a0), "v"(a1), "n"(16 * RB)
-      : "memory");
-}
 
 // O and LSE of one row from its parts, by one wave: m = max m_p, f_p =
 // 2^(c1 (m_p - m)) (0 for a part that saw no key), l = sum f_p l_p,
