@@ -311,3 +311,9 @@ def attn_decode_probe(q, k, v, *, causal: bool, scale: float, exp_mode: int, spl
     if rc != ATTN_OK:
         raise AttnError(rc, "attn_decode_probe")
     return out, lse, s, w, pb
+
+
+# ---- shared and bounded caches (include/h15cache.h) -------------------------
+
+from .cache import (attn_decode_prefix, attn_decode_prefix_split_keys, attn_decode_prefix_workspace_bytes,  # noqa: E402
+                    attn_evict, attn_key_weights, attn_key_weights_workspace_bytes)

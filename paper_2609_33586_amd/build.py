@@ -21,6 +21,11 @@ ROOT = PKG.parent
 SRC = PKG / "csrc" / "h15attn.hip"     # forward kernels and their launchers
 DECODE_SRC = PKG / "csrc" / "h15decode.hip"  # decode kernels and their launchers
 API_SRC = PKG / "csrc" / "attn_api.cpp"  # C entry points: argument checks, per-call constants
+# the operators over shared and bounded caches: entry points and kernels
+CACHE_API_SRC = PKG / "csrc" / "cache_api.cpp"
+PREFIX_SRC = PKG / "csrc" / "h15prefix.hip"
+WEIGHTS_SRC = PKG / "csrc" / "h15weights.hip"
+EVICT_SRC = PKG / "csrc" / "h15evict.hip"
 INCLUDE = ROOT / "include"
 LIB_PATH = PKG / "libh15attn.so"
 ARCH = "gfx950"
@@ -48,6 +53,10 @@ UNITS = [
     ("fp8_lattice_d128", SRC, ["-DH15_FP8_LATTICE_D128=1", "-mllvm", "-amdgpu-sched-strategy=iterative-ilp"]),
     ("decode", DECODE_SRC, []),
     ("api", API_SRC, []),
+    ("cache_api", CACHE_API_SRC, []),
+    ("prefix", PREFIX_SRC, []),
+    ("weights", WEIGHTS_SRC, []),
+    ("evict", EVICT_SRC, []),
 ]
 
 

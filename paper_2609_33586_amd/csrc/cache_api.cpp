@@ -1,0 +1,284 @@
+// The C entry points declared in h15cache.h: argument checks, cuts and
+// workspaces, then the launchers of h15prefix.hip, h15weights.hip and
+// h15evict.hip.  Plain C++: no HIP types or calls here, so the same checks
+// build with a host compiler alone under the sanitizers.
+#include <math.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "cache_params.h"
+#include "h15cache.h"
+
+using namespace h15;
+
+namespace {
+
+bool finite_pos(float x) { return x > 0.0f && x < INFINITY; }
+
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+// Input-rounding order of an exp_mode that the caches' decode offers, 0 for
+// the hardware exponential, -1 for others.
+int exp_order(int exp_mode) {
+  switch (exp_mode) {
+    case ATTN_EXP_EXACT: return 0;
+    case ATTN_EXP_H15: return 1;
+    case ATTN_EXP_SQ4: return 2;
+    case ATTN_EXP_SQ8: return 3;
+    default: return -1;
+  }
+}
+
+int elem_bytes(int dtype) { return dtype == ATTN_BF16 ? 2 : 1; }
+
+bool misaligned(const void* x, uintptr_t to) { return ((uintptr_t)x & (to - 1)) != 0; }
+
+// Parts of `keys` keys cut at `split` (0 or >= keys: one part; no keys: none).
+int part_count(int keys, int split) {
+  if (keys <= 0) return 0;
+  return split <= 0 || split >= keys ? 1 : (int)ceil_div(keys, split);
+}
+
+// Type, head dimension, scale and descales; c1: the base-two logit scale.
+int check_kind(int d, float scale, int dtype, const attn_opts* opts, float* c1, float* vd) {
+  if (!finite_pos(scale)) return ATTN_EINVAL;
+  if (dtype != ATTN_BF16 && dtype != ATTN_FP8_E4M3) return ATTN_EUNSUPPORTED;
+  if (d != 64 && d != 128) return ATTN_EUNSUPPORTED;
+  if (opts && opts->rescale_threshold != 0.0f)
+    return opts->rescale_threshold > 0.0f && opts->rescale_threshold <= 64.0f ? ATTN_EUNSUPPORTED : ATTN_EINVAL;
+  float qd = 1.0f, kd = 1.0f;
+  *vd = 1.0f;
+  if (dtype == ATTN_FP8_E4M3) {
+    if (!opts) return ATTN_EINVAL;
+    qd = opts->q_descale;
+    kd = opts->k_descale;
+    *vd = opts->v_descale;
+    if (!finite_pos(qd) || !finite_pos(kd) || !finite_pos(*vd)) return ATTN_EINVAL;
+  }
+  *c1 = (float)((double)scale * (double)qd * (double)kd * 1.4426950408889634);
+  return ATTN_OK;
+}
+
+// Prefix rows of a KV head beyond one block of WROWS take workgroups of
+// PREFIX_ROWS rows (the keys are read once for four times as many).
+int prefix_rows(long long rows) { return rows > WROWS ? PREFIX_ROWS : WROWS; }
+
+size_t prefix_workspace(long long rows, int parts, int d) {
+  return parts <= 1 ? 0 : (size_t)rows * (size_t)parts * ((size_t)d + 2) * sizeof(float);
+}
+
+// The runs of query rows that the tiles of a key-weights call stay within: a
+// head's rows, or all rows of a KV head where a head has fewer than a tile.
+void weights_runs(int G, int Sq, int& heads, int& hrows) {
+  heads = Sq >= KW_ROWS ? G : 1;
+  hrows = Sq >= KW_ROWS ? Sq : G * Sq;
+}
+
+// Row parts of a key-weights call: at most 64 tiles in each.
+int weights_parts(int G, int Sq) {
+  int heads, hrows;
+  weights_runs(G, Sq, heads, hrows);
+  return (int)ceil_div((long long)heads * ceil_div(hrows, KW_ROWS), 64);
+}
+
+struct Range {
+  uintptr_t from, to;
+};
+Range range(const void* p, size_t bytes) { return {(uintptr_t)p, (uintptr_t)p + bytes}; }
+bool overlap(const Range& a, const Range& b) { return a.from < b.to && b.from < a.to; }
+}  // namespace
+
+extern "C" {
+
+int attn_decode_prefix_split_keys(int B, int Hq, int Hkv, int Sq, int P, int Sk, int d, int dtype,
+                                  int* prefix_split_keys, int* split_keys) {
+  (void)d;
+  (void)dtype;
+  if (!prefix_split_keys || !split_keys) return ATTN_EINVAL;
+  *prefix_split_keys = *split_keys = 0;
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || P < 0 || Sk < 0 || Hq % Hkv != 0) return ATTN_EINVAL;
+  const long long rows = (long long)(Hq / Hkv) * Sq;
+  auto cut = [](int keys, long long groups, long long want, long long least) {
+    const long long tiles = ceil_div(keys, BC);
+    long long parts = ceil_div(want, groups);
+    if (parts > tiles / least) parts = tiles / least;
+    return parts <= 1 ? 0 : (int)(ceil_div(tiles, parts) * BC);
+  };
+  const int block = prefix_rows(B * rows);
+  if (P > 0) *prefix_split_keys = cut(P, Hkv * ceil_div(B * rows, block), block == WROWS ? 512 : 256, 4);
+  if (Sk > 0) *split_keys = cut(Sk, (long long)B * Hkv * ceil_div(rows, WROWS), 512, 8);
+  return ATTN_OK;
+}
+
+size_t attn_decode_prefix_workspace_bytes(int B, int Hq, int Sq, int P, int Sk, int d, int prefix_split_keys,
+                                          int split_keys) {
+  if (B <= 0 || Hq <= 0 || Sq <= 0 || P < 0 || Sk < 0 || d <= 0 || prefix_split_keys < 0 || split_keys < 0) return 0;
+  return prefix_workspace((long long)B * Hq * Sq, part_count(P, prefix_split_keys) + part_count(Sk, split_keys), d);
+}
+
+int attn_decode_prefix(const void* q, const void* kp, const void* vp, const void* k, const void* v,
+                       const int32_t* lens, void* o, float* lse, int B, int Hq, int Hkv, int Sq, int P, int P_cap,
+                       int Sk, int Sk_cap, int d, int causal, float scale, int dtype, int exp_mode,
+                       int prefix_split_keys, int split_keys, void* workspace, size_t workspace_bytes,
+                       const attn_opts* opts) {
+  if (!q || !o || (P > 0 && (!kp || !vp)) || (Sk > 0 && (!k || !v))) return ATTN_EINVAL;
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || d <= 0 || P < 0 || Sk < 0 || P + (long long)Sk <= 0)
+    return ATTN_EINVAL;
+  if (Hq % Hkv != 0 || P > P_cap || Sk > Sk_cap) return ATTN_EINVAL;
+  if (prefix_split_keys < 0 || prefix_split_keys % BC != 0 || split_keys < 0 || split_keys % BC != 0)
+    return ATTN_EINVAL;
+  PrefixParams p = {};
+  const int rc = check_kind(d, scale, dtype, opts, &p.c1, &p.vd);
+  if (rc != ATTN_OK) return rc;
+  const int order = exp_order(exp_mode);
+  if (order < 0) return ATTN_EUNSUPPORTED;
+  if (misaligned(q, 16) || misaligned(o, 16) || misaligned(lse, 4) || misaligned(lens, 4)) return ATTN_EUNSUPPORTED;
+  if (P > 0 && (misaligned(kp, 16) || misaligned(vp, 16))) return ATTN_EUNSUPPORTED;
+  if (Sk > 0 && (misaligned(k, 16) || misaligned(v, 16))) return ATTN_EUNSUPPORTED;
+  const long long row = (long long)d * elem_bytes(dtype), rows = (long long)B * Hq * Sq;
+  if (rows > (1LL << 30)) return ATTN_EUNSUPPORTED;
+  if ((P > 0 && P_cap * row > INT32_MAX) || (Sk > 0 && Sk_cap * row > INT32_MAX)) return ATTN_EUNSUPPORTED;
+  p.q = (const uint8_t*)q;
+  p.kp = (const uint8_t*)kp;
+  p.vp = (const uint8_t*)vp;
+  p.k = (const uint8_t*)k;
+  p.v = (const uint8_t*)v;
+  p.lens = lens;
+  p.o = (uint16_t*)o;
+  p.lse = lse;
+  p.B = B;
+  p.Hq = Hq;
+  p.Hkv = Hkv;
+  p.Sq = Sq;
+  p.G = Hq / Hkv;
+  p.R = p.G * Sq;
+  p.P = P;
+  p.P_cap = P_cap;
+  p.Sk = Sk;
+  p.Sk_cap = Sk_cap;
+  p.causal = causal && Sq > 1;  // a single row sees its whole cache either way
+  p.p_parts = part_count(P, prefix_split_keys);
+  p.o_parts = part_count(Sk, split_keys);
+  p.parts = p.p_parts + p.o_parts;
+  // (one part of whole tiles: the cut at its end)
+  p.p_split = p.p_parts == 1 ? (int)(ceil_div(P, BC) * BC) : prefix_split_keys;
+  p.o_split = p.o_parts == 1 ? (int)(ceil_div(Sk, BC) * BC) : split_keys;
+  // a single part writes O itself, which only workgroups of WROWS rows do
+  p.p_rows = p.parts == 1 ? WROWS : prefix_rows((long long)B * p.R);
+  p.p_blocks = (int)ceil_div((long long)B * p.R, p.p_rows);
+  p.o_blocks = (int)ceil_div(p.R, WROWS);
+  const long long pg = (long long)Hkv * p.p_parts * p.p_blocks, og = (long long)B * Hkv * p.o_parts * p.o_blocks;
+  if (pg + og > INT32_MAX) return ATTN_EUNSUPPORTED;
+  p.p_groups = (int)pg;
+  p.o_groups = (int)og;
+  p.ck = ldexpf(p.c1, order);
+  const size_t need = prefix_workspace(rows, p.parts, d);
+  if (need) {
+    if (!workspace || misaligned(workspace, 16) || workspace_bytes < need) return ATTN_EINVAL;
+    p.part_o = (float*)workspace;
+    p.part_ml = p.part_o + (size_t)rows * p.parts * d;
+  }
+  const int mode = order == 0 ? (int)MODE_EXACT : 2 * order - 1;
+  return launch_prefix(p, dtype, d, mode, opts ? opts->stream : nullptr) == 0 ? ATTN_OK : ATTN_ELAUNCH;
+}
+
+size_t attn_key_weights_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int d) {
+  (void)d;
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || Hq % Hkv != 0) return 0;
+  if ((long long)(Hq / Hkv) * Sq > INT32_MAX) return 0;
+  const int parts = weights_parts(Hq / Hkv, Sq);
+  return parts <= 1 ? 0 : (size_t)parts * B * Hkv * Sk * sizeof(float);
+}
+
+int attn_key_weights(const void* q, const void* k, const float* lse, const int32_t* lens, float* acc, int B, int Hq,
+                     int Hkv, int Sq, int Sk, int Sk_cap, int d, int causal, float scale, float decay, int dtype,
+                     void* workspace, size_t workspace_bytes, const attn_opts* opts) {
+  if (!q || !k || !lse || !acc) return ATTN_EINVAL;
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || d <= 0) return ATTN_EINVAL;
+  if (Hq % Hkv != 0 || Sk > Sk_cap) return ATTN_EINVAL;
+  if (!(decay >= 0.0f && decay < INFINITY)) return ATTN_EINVAL;
+  WeightsParams p = {};
+  float vd;
+  const int rc = check_kind(d, scale, dtype, opts, &p.c1, &vd);
+  if (rc != ATTN_OK) return rc;
+  if (misaligned(q, 16) || misaligned(k, 16) || misaligned(lse, 4) || misaligned(lens, 4) || misaligned(acc, 4))
+    return ATTN_EUNSUPPORTED;
+  const long long row = (long long)d * elem_bytes(dtype);
+  if ((long long)B * Hq * Sq > (1LL << 30)) return ATTN_EUNSUPPORTED;
+  if (Sk_cap * row > INT32_MAX || (long long)(Hq / Hkv) * Sq * row > INT32_MAX) return ATTN_EUNSUPPORTED;
+  p.q = (const uint8_t*)q;
+  p.k = (const uint8_t*)k;
+  p.lse = lse;
+  p.lens = lens;
+  p.acc = acc;
+  p.B = B;
+  p.Hq = Hq;
+  p.Hkv = Hkv;
+  p.Sq = Sq;
+  p.G = Hq / Hkv;
+  p.Sk = Sk;
+  p.Sk_cap = Sk_cap;
+  p.causal = causal && Sq > 1;
+  weights_runs(p.G, Sq, p.heads, p.hrows);
+  p.parts = weights_parts(p.G, Sq);
+  p.blocks = (int)ceil_div(Sk, KW_KEYS);
+  p.decay = decay;
+  if ((long long)B * Hkv * p.parts * p.blocks > INT32_MAX) return ATTN_EUNSUPPORTED;
+  if (p.parts > 1) {
+    const size_t need = (size_t)p.parts * B * Hkv * Sk * sizeof(float);
+    if (!workspace || misaligned(workspace, 16) || workspace_bytes < need) return ATTN_EINVAL;
+    p.part = (float*)workspace;
+  }
+  return launch_weights(p, dtype, d, opts ? opts->stream : nullptr) == 0 ? ATTN_OK : ATTN_ELAUNCH;
+}
+
+int attn_evict(const void* k, const void* v, const float* acc, const int32_t* lens, void* k_out, void* v_out,
+               float* acc_out, int32_t* index, int32_t* lens_out, int B, int Hkv, int Sk, int Sk_cap, int out_cap,
+               int d, int keep, int recent, int dtype, const attn_opts* opts) {
+  if (!k || !v || !acc || !k_out || !v_out || !acc_out || !index || !lens_out) return ATTN_EINVAL;
+  if (B <= 0 || Hkv <= 0 || Sk <= 0 || Sk_cap <= 0 || out_cap <= 0 || d <= 0 || keep <= 0) return ATTN_EINVAL;
+  if (Sk > Sk_cap || keep > out_cap || recent < 0) return ATTN_EINVAL;
+  if (dtype != ATTN_BF16 && dtype != ATTN_FP8_E4M3) return ATTN_EUNSUPPORTED;
+  if (d != 64 && d != 128) return ATTN_EUNSUPPORTED;
+  if (misaligned(k, 16) || misaligned(v, 16) || misaligned(k_out, 16) || misaligned(v_out, 16))
+    return ATTN_EUNSUPPORTED;
+  if (misaligned(acc, 4) || misaligned(lens, 4) || misaligned(acc_out, 4) || misaligned(index, 4) ||
+      misaligned(lens_out, 4))
+    return ATTN_EUNSUPPORTED;
+  EvictParams p = {};
+  p.row_bytes = d * elem_bytes(dtype);
+  const size_t heads = (size_t)B * Hkv;
+  if (heads > INT32_MAX) return ATTN_EUNSUPPORTED;
+  // workgroups of the gather (at most 16 threads a row)
+  if (ceil_div((long long)heads * (p.row_bytes / 16), 256) * (long long)keep > INT32_MAX) return ATTN_EUNSUPPORTED;
+  const Range in[] = {range(k, heads * Sk_cap * p.row_bytes), range(v, heads * Sk_cap * p.row_bytes),
+                      range(acc, heads * Sk_cap * 4), range(lens, lens ? (size_t)B * 4 : 0)};
+  const Range out[] = {range(k_out, heads * out_cap * p.row_bytes), range(v_out, heads * out_cap * p.row_bytes),
+                       range(acc_out, heads * out_cap * 4), range(index, heads * keep * 4),
+                       range(lens_out, (size_t)B * 4)};
+  for (const Range& x : out) {
+    for (const Range& y : in)
+      if (overlap(x, y)) return ATTN_EINVAL;
+    for (const Range& y : out)
+      if (&x != &y && overlap(x, y)) return ATTN_EINVAL;
+  }
+  p.k = (const uint8_t*)k;
+  p.v = (const uint8_t*)v;
+  p.acc = acc;
+  p.lens = lens;
+  p.k_out = (uint8_t*)k_out;
+  p.v_out = (uint8_t*)v_out;
+  p.acc_out = acc_out;
+  p.index = index;
+  p.lens_out = lens_out;
+  p.B = B;
+  p.Hkv = Hkv;
+  p.Sk = Sk;
+  p.Sk_cap = Sk_cap;
+  p.keep = keep;
+  p.recent = recent;
+  p.out_cap = out_cap;
+  return launch_evict(p, opts ? opts->stream : nullptr) == 0 ? ATTN_OK : ATTN_ELAUNCH;
+}
+
+}  // extern "C"

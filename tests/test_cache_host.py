@@ -1,0 +1,89 @@
+"""The host side of the operators over shared and bounded caches
+(csrc/cache_api.cpp) built with a host compiler alone and linked with launchers
+that launch nothing (tests/cache_launch_stub.cpp): which form a call takes, and,
+under AddressSanitizer and UndefinedBehaviorSanitizer, that no refusal reaches a
+launcher."""
+import ctypes
+import os
+import subprocess
+import sys
+from pathlib import Path
+
+import pytest
+
+import paper_2609_33586_amd as pkg
+from oracle import build as obuild
+
+ROOT = Path(__file__).resolve().parent.parent
+CSRC = ROOT / "paper_2609_33586_amd" / "csrc"
+A = 0x100000  # never dereferenced
+
+
+@pytest.fixture(scope="module")
+def host(tmp_path_factory):
+    lib = tmp_path_factory.mktemp("cache_host") / "libh15cache_host.so"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fPIC", "-shared", "-ffp-contract=off", "-Wall", "-Wextra", "-Werror",
+                    f"-I{ROOT / 'include'}", f"-I{CSRC}", str(CSRC / "cache_api.cpp"),
+                    str(ROOT / "tests" / "cache_launch_stub.cpp"), "-o", str(lib)], check=True)
+    L = ctypes.CDLL(str(lib))
+    P, I, F, S = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
+    L.attn_decode_prefix.argtypes = [P] * 8 + [I] * 10 + [F] + [I] * 4 + [P, S, P]
+    L.attn_key_weights.argtypes = [P] * 5 + [I] * 8 + [F, F, I, P, S, P]
+    return L
+
+
+def prefix_form(L, B, Hq, Hkv, Sq, P, Sk, p_cut=0, cut=0, causal=1):
+    rc = L.attn_decode_prefix(A, A, A, A, A, None, A, None, B, Hq, Hkv, Sq, P, P, Sk, Sk, 128, causal, 0.1, 0, 0, p_cut,
+                              cut, A, 1 << 40, None)
+    assert rc == pkg.ATTN_ELAUNCH
+    names = ("p_parts", "o_parts", "p_rows", "p_groups", "o_groups", "p_split", "o_split", "causal")
+    return {n: L.h15_stub_prefix(i) for i, n in enumerate(names)}
+
+
+def test_prefix_forms(host):
+    # up to 32 rows of a KV head over the batch: workgroups of 32 rows, else of 128
+    assert prefix_form(host, 8, 8, 2, 1, 1000, 100)["p_rows"] == 32
+    f = prefix_form(host, 33, 8, 8, 1, 1000, 100, 512, 0)
+    assert f["p_rows"] == 128 and f["p_parts"] == 2 and f["o_parts"] == 1 and f["p_groups"] == 8 * 2
+    assert f["o_groups"] == 33 * 8 and f["o_split"] == 128 and f["p_split"] == 512
+    assert prefix_form(host, 33, 8, 8, 1, 1000, 0)["p_rows"] == 32  # a single part writes O itself
+    assert prefix_form(host, 65, 16, 8, 1, 1000, 300, 0, 128)["p_groups"] == 8 * 2  # 130 rows: two blocks
+    f = prefix_form(host, 2, 12, 2, 16, 0, 300, 0, 128)
+    assert f["p_groups"] == 0 and f["o_groups"] == 2 * 2 * 3 * 3  # 96 rows a sequence: three blocks
+    # one query row sees its whole cache with or without a causal mask
+    assert prefix_form(host, 2, 4, 2, 1, 10, 10)["causal"] == 0 and prefix_form(host, 2, 4, 2, 2, 10, 10)["causal"] == 1
+
+
+def test_weights_runs(host):
+    def form(Hq, Hkv, Sq, Sk):
+        rc = host.attn_key_weights(A, A, A, None, A, 1, Hq, Hkv, Sq, Sk, Sk, 128, 1, 0.1, 1.0, 0, A, 1 << 40, None)
+        assert rc == pkg.ATTN_ELAUNCH
+        return {n: host.h15_stub_weights(i) for i, n in enumerate(("heads", "hrows", "parts", "blocks", "causal"))}
+
+    assert form(8, 2, 1, 256) == {"heads": 1, "hrows": 4, "parts": 1, "blocks": 1, "causal": 0}
+    assert form(8, 2, 31, 257) == {"heads": 1, "hrows": 124, "parts": 1, "blocks": 2, "causal": 1}
+    assert form(8, 2, 32, 257)["heads"] == 4 and form(8, 2, 32, 257)["hrows"] == 32
+    # at most 64 tiles of 32 rows in a part
+    assert form(8, 2, 512, 512)["parts"] == 1 and form(8, 2, 513, 512)["parts"] == 2
+
+
+def test_checks_under_sanitizers(tmp_path):
+    lib = tmp_path / "libh15cache_san.so"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fno-omit-frame-pointer", "-fsanitize=address,undefined",
+                    "-fno-sanitize-recover=all", "-fPIC", "-shared", "-ffp-contract=off",
+                    "-Dh15_stub_launches=h15_forward_stub_launches", f"-I{ROOT / 'include'}", f"-I{CSRC}",
+                    str(CSRC / "attn_api.cpp"), str(ROOT / "tests" / "sanitize_launch_stub.cpp"), "-c"], cwd=tmp_path,
+                   check=True)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fno-omit-frame-pointer", "-fsanitize=address,undefined",
+                    "-fno-sanitize-recover=all", "-fPIC", "-shared", "-ffp-contract=off", f"-I{ROOT / 'include'}",
+                    f"-I{CSRC}", str(CSRC / "cache_api.cpp"), str(ROOT / "tests" / "cache_launch_stub.cpp"),
+                    str(tmp_path / "attn_api.o"), str(tmp_path / "sanitize_launch_stub.o"), "-o", str(lib)], check=True)
+    env = dict(os.environ, LD_PRELOAD=obuild.sanitizer_preload(), ASAN_OPTIONS="detect_leaks=0:abort_on_error=0",
+               UBSAN_OPTIONS="print_stacktrace=1", H15ATTN_LIB=str(lib))
+    code = ("import sys, pytest; rc = pytest.main(['tests/test_cache_api.py', '-q', '-p', 'no:cacheprovider']); "
+            "import paper_2609_33586_amd as p; assert p.lib()._name == %r and p.lib().h15_stub_launches() == 0; "
+            "sys.exit(rc)" % str(lib))
+    res = subprocess.run([sys.executable, "-c", code], cwd=ROOT, env=env, capture_output=True, text=True, timeout=600)
+    out = res.stdout + res.stderr
+    assert "AddressSanitizer" not in out and "runtime error" not in out, out[-4000:]
+    assert res.returncode == 0 and " passed" in out, out[-4000:]
