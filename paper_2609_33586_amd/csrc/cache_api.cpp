@@ -68,17 +68,29 @@ size_t prefix_workspace(long long rows, int parts, int d) {
 }
 
 // The runs of query rows that the tiles of a key-weights call stay within: a
-// head's rows, or all rows of a KV head where a head has fewer than a tile.
+// head's rows, or all rows of a KV head where a head has fewer than half a tile.
 void weights_runs(int G, int Sq, int& heads, int& hrows) {
-  heads = Sq >= KW_ROWS ? G : 1;
-  hrows = Sq >= KW_ROWS ? Sq : G * Sq;
+  heads = Sq >= KW_ROWS / 2 ? G : 1;
+  hrows = Sq >= KW_ROWS / 2 ? Sq : G * Sq;
 }
 
-// Row parts of a key-weights call: at most 64 tiles in each.
+// Tiles of each run in a row part of a key-weights call: 32 tiles in all.
+int weights_span(int heads) { return heads >= 32 ? 1 : 32 / heads; }
+
 int weights_parts(int G, int Sq) {
+  if ((long long)G * Sq <= KW_FEW_ROWS) return 1;
   int heads, hrows;
   weights_runs(G, Sq, heads, hrows);
-  return (int)ceil_div((long long)heads * ceil_div(hrows, KW_ROWS), 64);
+  return (int)ceil_div(ceil_div(hrows, KW_ROWS), weights_span(heads));
+}
+
+// Units of keys in a wave's run: about two workgroups per compute unit, three
+// units at most (B16 8K BF16, ragged: runs of 1, 2, 3 and 4 units 48, 41, 40 and
+// 49 us; B5 5K FP8 d = 64, whose 800 workgroups have runs of one: 5.0, of three
+// 6.6; 64 query rows B2 16K FP8, runs of 1, 2, 3 and 4: 30, 27, 32 and 34).
+int weights_run(long long heads, long long units) {
+  const long long run = heads * units / (512 * 4);
+  return run < 1 ? 1 : run > 3 ? 3 : (int)run;
 }
 
 struct Range {
@@ -221,7 +233,13 @@ int attn_key_weights(const void* q, const void* k, const float* lse, const int32
   p.causal = causal && Sq > 1;
   weights_runs(p.G, Sq, p.heads, p.hrows);
   p.parts = weights_parts(p.G, Sq);
+  p.span = weights_span(p.heads);
   p.blocks = (int)ceil_div(Sk, KW_KEYS);
+  if ((long long)p.G * Sq <= KW_FEW_ROWS) {
+    const long long units = ceil_div(Sk, KW_FEW_KEYS);
+    p.span = weights_run((long long)B * Hkv, units);
+    p.blocks = (int)ceil_div(units, 4 * p.span);
+  }
   p.decay = decay;
   if ((long long)B * Hkv * p.parts * p.blocks > INT32_MAX) return ATTN_EUNSUPPORTED;
   if (p.parts > 1) {

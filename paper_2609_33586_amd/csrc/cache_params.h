@@ -16,9 +16,15 @@ namespace h15 {
 constexpr int PREFIX_ROWS = 4 * WROWS;
 
 // Keys and query rows of a key-weights workgroup: four waves of 64 keys each,
-// a tile of 32 query rows at a time.
+// a tile of 64 query rows at a time.
 constexpr int KW_KEYS = 4 * 64;
-constexpr int KW_ROWS = WROWS;
+constexpr int KW_ROWS = 64;
+
+// Up to this many query rows of a KV head stay in LDS (64 KB of it at d = 128,
+// so that two workgroups share a compute unit), and each wave streams units of
+// KW_FEW_KEYS keys past them.
+constexpr int KW_FEW_ROWS = 256;
+constexpr int KW_FEW_KEYS = 64;
 
 // Decode over a shared prefix and each sequence's own cache.
 struct PrefixParams {
@@ -53,7 +59,9 @@ struct WeightsParams {
   float* part;  // [parts][B Hkv][Sk], several parts only
   int B, Hq, Hkv, Sq, G, Sk, Sk_cap, causal;
   int heads, hrows;  // runs of query rows that tiles stay within, and rows of each
-  int parts, blocks;  // row parts, blocks of KW_KEYS keys
+  // row parts, their tiles of each run, blocks of KW_KEYS keys; with up to
+  // KW_FEW_ROWS rows: 1, a wave's units of keys, blocks of 4 span units
+  int parts, span, blocks;
   float c1, decay;
 };
 

@@ -5,11 +5,16 @@
 // and writes their indexes; then their rows of K, V and acc are gathered into
 // the compact caches, 16 bytes a thread.
 //
-// The selection is a radix search for the weight of rank keep - recent: four
-// rounds over 8 bits, each a histogram in LDS of the keys that agree with the
-// digits found so far.  A first pass over the keys in order then counts, and a
-// second writes.  What bounds the call is the gather (read and written once)
-// and, with few caches, the rounds' latency.
+// The selection is a radix search for the weight of rank keep - recent in three
+// rounds over 11, 11 and 10 bits, each a histogram in LDS of the keys that agree
+// with the digits found so far; then a count of the keys that stay, stretch by
+// stretch, and a second pass that writes their indexes in order.  The weights
+// are read once, as ordered numbers into LDS (of a cache of more than 32K keys
+// every pass reads the rest again).  (In registers, 32 a thread, the passes had
+// to be unrolled, and a workgroup spent its time fetching code that it runs once:
+// 41 us for 32K keys; re-read from memory in every pass 53 us.)  What bounds the
+// call is the gather (read and written once) and, with few caches, the passes'
+// latency.
 #include "cache_params.h"
 
 #include <hip/hip_runtime.h>
@@ -21,7 +26,12 @@ using namespace h15;
 
 constexpr int SEL = 1024;  // threads of a selection
 constexpr int SW = SEL / 64;
-constexpr int BINS = 256;
+constexpr int BINS = 2048;
+constexpr int HELD = 32768;  // weights in LDS
+constexpr int STEP = 256;    // keys of a wave and step: four a lane
+constexpr int BATCH = 16;    // loads of a thread at a time
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Weights as unsigned numbers in their order: +0 and -0 alike, NaN above all.
 __device__ __forceinline__ uint32_t rank_of(float x) {
@@ -30,10 +40,48 @@ __device__ __forceinline__ uint32_t rank_of(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Adds one to the bin of every lane that has one (bin >= 0).  LDS adds to one
+// address follow each other: lanes that all have the same bin, as with equal
+// weights, are counted together.
+__device__ __forceinline__ void count(uint32_t* hist, int bin, int lane) {
+  const int one = __builtin_amdgcn_readfirstlane(bin);
+  if (!__ballot(bin != one)) {
+    if (lane == 0 && one >= 0) atomicAdd(&hist[one], 64u);
+  } else if (bin >= 0) {
+    atomicAdd(&hist[bin], 1u);
+  }
+}
+
+// Inclusive sum over the lanes of a wave: within rows of 16 by shifts, then from
+// row to row.
+__device__ __forceinline__ uint32_t scan(uint32_t x) {
+  int v = (int)x;
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);   // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);   // row_shr:2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);   // row_shr:4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);   // row_shr:8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast:15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast:31 into rows 2 and 3
+  return (uint32_t)v;
+}
+
+// Sum of the waves' numbers below this wave's
+__device__ __forceinline__ uint32_t sum_below(const uint32_t* waves, int wave) {
+  uint32_t sum = 0;
+#pragma unroll
+  for (int i = 0; i < SW; i += 4) {
+    const u32x4 x = *(const u32x4*)&waves[i];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum += i + e < wave ? x[e] : 0;
+  }
+  return sum;
+}
+
 __global__ __launch_bounds__(SEL) void attn_evict_select(EvictParams p) {
-  __shared__ uint32_t hist[BINS];
+  __shared__ __attribute__((aligned(16))) uint32_t ranks[HELD];
+  __shared__ uint32_t hist[2][BINS];  // odd and even lanes' counts
   __shared__ uint32_t found[2];  // digits so far, keys still wanted among those that agree
-  __shared__ uint32_t above[SW], equal[SW];
+  __shared__ __attribute__((aligned(16))) uint32_t above[SW], equal[SW], waves[SW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int bh = blockIdx.x, b = bh / p.Hkv;
   const int n = p.lens ? min(max(p.lens[b], 0), p.Sk) : p.Sk;
@@ -46,67 +94,110 @@ __global__ __launch_bounds__(SEL) void attn_evict_select(EvictParams p) {
   }
   const int late = n - min(p.recent, p.keep);  // the keys from here on stay
   const uint32_t want = (uint32_t)(p.keep - (n - late));
-  uint32_t digits = 0, left = want;
-  if (want > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < BINS) hist[tid] = 0;
-      __syncthreads();
-      for (int i = tid; i < late; i += SEL) {
-        const uint32_t u = rank_of(acc[i]);
-        if (shift == 24 || (u >> (shift + 8)) == digits) atomicAdd(&hist[(u >> shift) & 255], 1u);
-      }
-      __syncthreads();
-      if (wave == 0) {
-        // lane: four bins, from the top; the bin in which the count passes `left`
-        uint32_t c[4], own = 0;
+  for (int i = late + tid; i < n; i += SEL) index[want + (uint32_t)(i - late)] = i;
+  if (want == 0) return;
+
+  // (0, which no weight has, up to a whole step)
+  const int held = min((late + STEP - 1) / STEP * STEP, HELD);
+  for (int i0 = tid; i0 < held; i0 += BATCH * SEL) {
+    float x[BATCH];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) own += c[j] = hist[255 - (4 * lane + j)];
-        uint32_t upto = own;
-        for (int x = 1; x < 64; x <<= 1) {
-          const uint32_t y = __shfl_up(upto, x, 64);
-          if (lane >= x) upto += y;
-        }
-        uint32_t before = upto - own;
-        if (before < left && upto >= left) {
-          int j = 0;
-          while (before + c[j] < left) before += c[j++];
-          found[0] = (digits << 8) | (uint32_t)(255 - (4 * lane + j));
-          found[1] = left - before;
-        }
-      }
-      __syncthreads();
-      digits = found[0];
-      left = found[1];
+    for (int j = 0; j < BATCH; ++j) x[j] = acc[min(i0 + j * SEL, late - 1)];
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      const int i = i0 + j * SEL;
+      if (i < held) ranks[i] = i < late ? rank_of(x[j]) : 0;
     }
+  }
+  // the ranks of four keys, i a multiple of 4
+  auto four = [&](int i) {
+    if (i < HELD) return *(const u32x4*)&ranks[i];
+    u32x4 u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = i + e < late ? rank_of(acc[i + e]) : 0;
+    return u;
+  };
+  uint32_t digits = 0, left = want;
+#pragma unroll 1
+  for (int round = 0; round < 3; ++round) {
+    const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, width = round < 2 ? 11 : 10;
+    constexpr int PER = BINS / SEL;
+#pragma unroll
+    for (int i = 0; i < 2 * PER; ++i) hist[0][i * SEL + tid] = 0;
+    __syncthreads();
+    // (whole waves: the lanes beyond the last key have no bin)
+    for (int i = wave * STEP; i < late; i += SW * STEP) {
+      const u32x4 u = four(i + 4 * lane);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool in = u[e] != 0 && (round == 0 || (u[e] >> (shift + width)) == digits);
+        if (__ballot(in)) count(hist[lane & 1], in ? (int)((u[e] >> shift) & ((1u << width) - 1)) : -1, lane);
+      }
+    }
+    __syncthreads();
+    // a thread: two bins, from the top; the bin in which the count passes `left`
+    uint32_t c[PER], own = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int bin = BINS - 1 - (PER * tid + j);
+      c[j] = hist[0][bin] + hist[1][bin];
+      own += c[j];
+    }
+    const uint32_t upto = scan(own);
+    if (lane == 63) waves[wave] = upto;
+    __syncthreads();
+    const uint32_t before = upto - own + sum_below(waves, wave);
+    if (before < left && before + own >= left) {
+      const bool second = before + c[0] < left;
+      found[0] = (digits << width) | (uint32_t)(BINS - 1 - (PER * tid + (second ? 1 : 0)));
+      found[1] = left - before - (second ? c[0] : 0);
+    }
+    __syncthreads();
+    digits = found[0];
+    left = found[1];
   }
   // now: all keys above `digits` stay, and the first `left` of those equal to it.
   // Each wave has a stretch of the keys before `late`, in order.
-  const int stretch = (late + SEL - 1) / SEL * 64;
+  const int stretch = (late + SW * STEP - 1) / (SW * STEP) * STEP;
   const int i0 = min(wave * stretch, late), i1 = min(i0 + stretch, late);
   uint32_t na = 0, ne = 0;
-  for (int i = i0; i < i1; i += 64) {
-    const bool in = i + lane < i1;
-    const uint32_t u = in && want > 0 ? rank_of(acc[i + lane]) : 0;
-    na += __popcll(__ballot(in && want > 0 && u > digits));
-    ne += __popcll(__ballot(in && want > 0 && u == digits));
+  for (int i = i0; i < i1; i += STEP) {
+    const u32x4 u = four(i + 4 * lane);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      na += (uint32_t)__popcll(__ballot(u[e] > digits));
+      ne += (uint32_t)__popcll(__ballot(u[e] == digits));
+    }
   }
   if (lane == 0) above[wave] = na, equal[wave] = ne;
   __syncthreads();
-  uint32_t at = 0, eq = 0;  // kept, and equal, in the stretches before
-  for (int w = 0; w < wave; ++w) at += above[w], eq += equal[w];
-  at += min(eq, left);
+  // equal ones, and those that stay, in the stretches before
+  uint32_t eq = sum_below(equal, wave), at = sum_below(above, wave) + min(eq, left);
   const unsigned long long below = (1ull << lane) - 1;
-  for (int i = i0; i < i1; i += 64) {
-    const bool in = i + lane < i1;
-    const uint32_t u = in && want > 0 ? rank_of(acc[i + lane]) : 0;
-    const unsigned long long es = __ballot(in && want > 0 && u == digits);
-    const bool stays = in && want > 0 && (u > digits || (u == digits && eq + (uint32_t)__popcll(es & below) < left));
-    const unsigned long long ss = __ballot(stays);
-    if (stays) index[at + (uint32_t)__popcll(ss & below)] = i + lane;
-    at += (uint32_t)__popcll(ss);
-    eq += (uint32_t)__popcll(es);
+  for (int i = i0; i < i1; i += STEP) {
+    const u32x4 u = four(i + 4 * lane);
+    unsigned long long es[4];
+    uint32_t before = eq;  // equal ones before this lane's
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      es[e] = __ballot(u[e] == digits);
+      before += (uint32_t)__popcll(es[e] & below);
+      eq += (uint32_t)__popcll(es[e]);
+    }
+    bool stays[4];
+    uint32_t to = at;  // index of this lane's first key that stays
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      stays[e] = u[e] > digits || (u[e] == digits && before < left);
+      before += u[e] == digits ? 1 : 0;
+      const unsigned long long ss = __ballot(stays[e]);
+      to += (uint32_t)__popcll(ss & below);
+      at += (uint32_t)__popcll(ss);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (stays[e]) index[to++] = i + 4 * lane + e;
   }
-  for (int i = late + tid; i < n; i += SEL) index[want + (uint32_t)(i - late)] = i;
 }
 
 // Rows of K, V and acc at the indexes.  A thread: 16 bytes of a row of K and of V.

@@ -60,11 +60,17 @@ def test_weights_runs(host):
         assert rc == pkg.ATTN_ELAUNCH
         return {n: host.h15_stub_weights(i) for i, n in enumerate(("heads", "hrows", "parts", "blocks", "causal"))}
 
+    # up to 256 query rows of a KV head: one part, blocks of four waves with runs
+    # of one to three units of 64 keys, about 512 workgroups
     assert form(8, 2, 1, 256) == {"heads": 1, "hrows": 4, "parts": 1, "blocks": 1, "causal": 0}
     assert form(8, 2, 31, 257) == {"heads": 1, "hrows": 124, "parts": 1, "blocks": 2, "causal": 1}
-    assert form(8, 2, 32, 257)["heads"] == 4 and form(8, 2, 32, 257)["hrows"] == 32
-    # at most 64 tiles of 32 rows in a part
+    assert form(8, 2, 64, 257)["heads"] == 4 and form(8, 2, 64, 257)["blocks"] == 2
+    assert [form(8, 8, 1, 64 * 2048 * x // 8)["blocks"] for x in (1, 2, 3, 4)] == [64, 64, 64, 86]
+    # beyond: blocks of 256 keys, runs of one head from 32 rows on, parts of at most 32 tiles of 64 rows
+    assert form(16, 1, 31, 257) == {"heads": 1, "hrows": 496, "parts": 1, "blocks": 2, "causal": 1}
+    assert form(16, 1, 32, 257) == {"heads": 16, "hrows": 32, "parts": 1, "blocks": 2, "causal": 1}
     assert form(8, 2, 512, 512)["parts"] == 1 and form(8, 2, 513, 512)["parts"] == 2
+    assert form(64, 1, 65, 512)["parts"] == 2  # more heads than tiles: one tile of each
 
 
 def test_checks_under_sanitizers(tmp_path):

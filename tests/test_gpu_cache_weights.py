@@ -45,7 +45,10 @@ SHAPES = [
     (1, 3, 1, 77, 700, None),               # ragged last tiles
     (1, 2, 1, 500, 500, None),              # a whole prompt
     (2, 2, 2, 400, 300, [300, 20]),         # more rows than keys: the first see none
-    (1, 2, 1, 1500, 1300, [1290]),          # 94 tiles: two row parts
+    (1, 2, 1, 1500, 1300, [1290]),          # 48 tiles of 64 rows: two row parts
+    (2, 16, 2, 32, 200, [200, 30]),         # 256 rows: the most that stay in LDS
+    (1, 9, 1, 29, 300, None),               # 261 packed rows, positions repeat within a tile
+    (1, 40, 1, 70, 500, None),              # 40 heads of two tiles each: two row parts
 ]
 
 
