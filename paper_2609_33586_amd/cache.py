@@ -15,16 +15,17 @@ EXPORTS = ("attn_decode_prefix", "attn_decode_prefix_workspace_bytes", "attn_dec
            "attn_key_weights", "attn_key_weights_workspace_bytes", "attn_evict")
 
 _bound = None
-_device = None
+_device = None  # the number of the current device
+_torch = None
 
 
 def _lib() -> ctypes.CDLL:
     """The library with the argument types of these functions (bound on first
     use, so that a build of the h15attn.h entry points alone still loads)."""
-    global _bound, _device
+    global _bound, _device, _torch
+    if _bound is not None:
+        return _bound
     L = lib()
-    if _bound is L:
-        return L
     P, I, F, S, O = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t, ctypes.POINTER(attn_opts)
     IP = ctypes.POINTER(ctypes.c_int)
     for name, args, res in (
@@ -37,51 +38,63 @@ def _lib() -> ctypes.CDLL:
         fn = getattr(L, name)
         fn.argtypes, fn.restype = args, res
     import torch
+    _torch = torch
     _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     _bound = L
     return L
 
 
-def _tensor(name, t, shape, device, dtype=None):
-    """A contiguous tensor of this shape (None: any size) on the device."""
-    if t.device != device or not t.is_contiguous() or (dtype is not None and t.dtype != dtype) \
-            or len(t.shape) != len(shape) or any(w is not None and s != w for s, w in zip(t.shape, shape)):
-        want = "x".join("?" if w is None else str(w) for w in shape)
-        raise ValueError(f"{name} must be a contiguous tensor [{want}]{f' of {dtype}' if dtype else ''} on {device}")
+# Checks are on the path of every call, and the smallest calls are bound by it:
+# shapes are compared whole and devices by number, and the workspace of a caller
+# who gives one is sized by the library alone.
+def _tensor(name, t, shape, dev, dtype=None):
+    """A contiguous tensor of this shape on device number dev."""
+    if t.shape != shape or not t.is_contiguous() or t.get_device() != dev or (dtype is not None and t.dtype != dtype):
+        want = "x".join(map(str, shape))
+        raise ValueError(f"{name} must be a contiguous tensor [{want}]{f' of {dtype}' if dtype else ''} on "
+                         f"{f'GPU {dev}' if dev >= 0 else 'the host'}")
     return t
 
 
-def _on_current_device(t, name):
-    if not t.is_cuda or t.get_device() != _device():
+def _operand(name, t, shape, dev, first, dt):
+    """A tensor as _tensor, of the operand type dt that the first operand has."""
+    _tensor(name, t, shape, dev)
+    if t.dtype != first and _dtype_of(t) != dt:
+        raise TypeError(f"{name} and the first operand must share one operand type")
+    return t
+
+
+def _current_gpu(name, t) -> int:
+    """The number of t's device, which has to be the current one."""
+    dev = t.get_device()
+    if dev < 0 or dev != _device():
         raise ValueError(f"{name} must be on the current GPU")
-    return t.device
+    return dev
 
 
-def _lens_ptr(lens, B, device):
-    if lens is None:
-        return None
-    import torch
-    return _tensor("lens", lens, (B,), device, torch.int32).data_ptr()
+def _four(name, t):
+    if len(t.shape) != 4:
+        raise ValueError(f"{name} must be a contiguous 4-D device tensor")
+    return t.shape
 
 
-def _space(workspace, need, device, stream):
-    """The caller's workspace or a new one, its pointer and size."""
+def _lens_ptr(lens, B, dev):
+    return None if lens is None else _tensor("lens", lens, (B,), dev, _torch.int32).data_ptr()
+
+
+def _space(workspace, need, dev, stream):
+    """Pointer and size of the caller's workspace, or of a new one of need() bytes, which comes third."""
     if workspace is None:
-        if not need:
-            return None, None, 0
-        import torch
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        n = need()
+        if not n:
+            return None, 0, None
+        workspace = _torch.empty(n, dtype=_torch.uint8, device=f"cuda:{dev}")
         if stream is not None:
             workspace.record_stream(stream)  # it is let go before the work on that stream is done
-    elif not workspace.is_contiguous() or workspace.device != device:
-        raise ValueError(f"workspace must be a contiguous tensor on {device}")
-    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
-
-
-def _same_type(dt, **tensors):
-    for t in tensors.values():
-        if _dtype_of(t) != dt:
-            raise TypeError(f"{', '.join(tensors)} and the first operand must share one operand type")
+        return workspace.data_ptr(), n, workspace
+    if not workspace.is_contiguous() or workspace.get_device() != dev:
+        raise ValueError(f"workspace must be a contiguous tensor on GPU {dev}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def attn_decode_prefix_split_keys(B: int, Hq: int, Hkv: int, Sq: int, P: int, Sk: int, d: int,
@@ -109,35 +122,34 @@ def attn_decode_prefix(q, kp, vp, k, v, *, causal: bool, scale: float, exp_mode:
     first lens[b] rows (int32 [B]; default Sk, default all) are filled, or None
     for none.  Returns (O [B,Hq,Sq,d] bf16, LSE [B,Hq,Sq] fp32 or None)."""
     L = _lib()
-    if q.dim() != 4 or not q.is_contiguous():
-        raise ValueError("q must be a contiguous 4-D device tensor [B,Hq,Sq,d]")
-    dev = _on_current_device(q, "q")
-    B, Hq, Sq, d = q.shape
+    B, Hq, Sq, d = shape = _four("q", q)
+    dev, first = _current_gpu("q", q), q.dtype
+    _tensor("q", q, shape, dev)
     dt = _dtype_of(q)
-    Hkv = kp.shape[0] if kp is not None else k.shape[1] if k is not None else 0
-    P_cap = Sk_cap = 0
-    if kp is not None:
-        P_cap = kp.shape[1]
-        _tensor("kp", kp, (Hkv, P_cap, d), dev)
-        _tensor("vp", vp, (Hkv, P_cap, d), dev)
-        _same_type(dt, kp=kp, vp=vp)
+    Hkv = P_cap = Sk_cap = 0
+    kptr = vptr = kpptr = vpptr = None
     if k is not None:
-        Sk_cap = k.shape[2]
-        _tensor("k", k, (B, Hkv, Sk_cap, d), dev)
-        _tensor("v", v, (B, Hkv, Sk_cap, d), dev)
-        _same_type(dt, k=k, v=v)
+        _, Hkv, Sk_cap, _ = _four("k", k)
+        shape = (B, Hkv, Sk_cap, d)
+        kptr = _operand("k", k, shape, dev, first, dt).data_ptr()
+        vptr = _operand("v", v, shape, dev, first, dt).data_ptr()
+    if kp is not None:
+        if k is None:
+            Hkv = kp.shape[0]
+        P_cap = kp.shape[1] if len(kp.shape) > 1 else 0
+        shape = (Hkv, P_cap, d)
+        kpptr = _operand("kp", kp, shape, dev, first, dt).data_ptr()
+        vpptr = _operand("vp", vp, shape, dev, first, dt).data_ptr()
     P = P_cap if P is None else int(P)
     Sk = Sk_cap if Sk is None else int(Sk)
     out, lse = _outputs(q, out, lse, want_lse)
-    need = L.attn_decode_prefix_workspace_bytes(B, Hq, Sq, P, Sk, d, prefix_split_keys, split_keys)
-    ws, wptr, wbytes = _space(workspace, need, dev, stream)
+    wptr, wbytes, workspace = _space(workspace, lambda: L.attn_decode_prefix_workspace_bytes(
+        B, Hq, Sq, P, Sk, d, prefix_split_keys, split_keys), dev, stream)
     opts = _opts(descale, stream)
-    rc = L.attn_decode_prefix(q.data_ptr(), kp.data_ptr() if kp is not None else None,
-                              vp.data_ptr() if kp is not None else None, k.data_ptr() if k is not None else None,
-                              v.data_ptr() if k is not None else None, _lens_ptr(lens, B, dev), out.data_ptr(),
+    rc = L.attn_decode_prefix(q.data_ptr(), kpptr, vpptr, kptr, vptr, _lens_ptr(lens, B, dev), out.data_ptr(),
                               lse.data_ptr() if lse is not None else None, B, Hq, Hkv, Sq, P, P_cap, Sk, Sk_cap, d,
-                              int(bool(causal)), float(scale), dt, int(exp_mode), int(prefix_split_keys),
-                              int(split_keys), wptr, wbytes, ctypes.byref(opts))
+                              1 if causal else 0, scale, dt, exp_mode, prefix_split_keys, split_keys, wptr, wbytes,
+                              ctypes.byref(opts))
     if rc != ATTN_OK:
         raise AttnError(rc, "attn_decode_prefix")
     return out, lse
@@ -154,26 +166,23 @@ def attn_key_weights(q, k, lse, acc, *, causal: bool, scale: float, decay: float
     q: [B,Hq,Sq,d]; k: [B,Hkv,Sk_cap,d]; lse: [B,Hq,Sq] fp32 as the attention
     call over q returned it; acc: [B,Hkv,Sk_cap] fp32, updated in place and
     returned.  descale: (q, k) or (q, k, v) factors of FP8 operands."""
-    import torch
     L = _lib()
-    if q.dim() != 4 or not q.is_contiguous():
-        raise ValueError("q must be a contiguous 4-D device tensor [B,Hq,Sq,d]")
-    dev = _on_current_device(q, "q")
-    B, Hq, Sq, d = q.shape
+    B, Hq, Sq, d = shape = _four("q", q)
+    dev = _current_gpu("q", q)
+    _tensor("q", q, shape, dev)
     dt = _dtype_of(q)
-    _tensor("k", k, (B, None, None, d), dev)
-    _same_type(dt, k=k)
-    Hkv, cap = k.shape[1], k.shape[2]
-    _tensor("lse", lse, (B, Hq, Sq), dev, torch.float32)
-    _tensor("acc", acc, (B, Hkv, cap), dev, torch.float32)
+    _, Hkv, cap, _ = _four("k", k)
+    _operand("k", k, (B, Hkv, cap, d), dev, q.dtype, dt)
+    _tensor("lse", lse, (B, Hq, Sq), dev, _torch.float32)
+    _tensor("acc", acc, (B, Hkv, cap), dev, _torch.float32)
     Sk = cap if Sk is None else int(Sk)
-    need = L.attn_key_weights_workspace_bytes(B, Hq, Hkv, Sq, Sk, d)
-    ws, wptr, wbytes = _space(workspace, need, dev, stream)
+    wptr, wbytes, workspace = _space(workspace, lambda: L.attn_key_weights_workspace_bytes(B, Hq, Hkv, Sq, Sk, d), dev,
+                                     stream)
     if descale is not None:
         descale = (descale[0], descale[1], 1.0)
     opts = _opts(descale, stream)
     rc = L.attn_key_weights(q.data_ptr(), k.data_ptr(), lse.data_ptr(), _lens_ptr(lens, B, dev), acc.data_ptr(), B,
-                            Hq, Hkv, Sq, Sk, cap, d, int(bool(causal)), float(scale), float(decay), dt, wptr, wbytes,
+                            Hq, Hkv, Sq, Sk, cap, d, 1 if causal else 0, scale, decay, dt, wptr, wbytes,
                             ctypes.byref(opts))
     if rc != ATTN_OK:
         raise AttnError(rc, "attn_key_weights")
@@ -189,38 +198,26 @@ def attn_evict(k, v, acc, *, keep: int, recent: int, lens=None, Sk: int | None =
     [B,Hkv,out_cap,d], acc_out [B,Hkv,out_cap], index [B,Hkv,keep] int32,
     lens_out [B] int32): the given tensors, or new ones with out_cap = keep.
     Rows of the outputs from lens_out[b] on are left as they were."""
-    import torch
     L = _lib()
-    dev = _on_current_device(k, "k")
-    if k.dim() != 4:
-        raise ValueError("k must be a contiguous 4-D device tensor [B,Hkv,Sk_cap,d]")
-    B, Hkv, cap, d = k.shape
+    B, Hkv, cap, d = shape = _four("k", k)
+    dev, first, f32, i32 = _current_gpu("k", k), k.dtype, _torch.float32, _torch.int32
+    _tensor("k", k, shape, dev)
     dt = _dtype_of(k)
-    _tensor("k", k, (B, Hkv, cap, d), dev)
-    _tensor("v", v, (B, Hkv, cap, d), dev)
-    _same_type(dt, v=v)
-    _tensor("acc", acc, (B, Hkv, cap), dev, torch.float32)
+    _operand("v", v, shape, dev, first, dt)
+    _tensor("acc", acc, (B, Hkv, cap), dev, f32)
     Sk, keep = cap if Sk is None else int(Sk), int(keep)
     rows = max(keep, 1)
-    if k_out is None:
-        k_out = torch.empty((B, Hkv, v_out.shape[2] if v_out is not None else rows, d), dtype=k.dtype, device=dev)
-    if k_out.dim() != 4:
-        raise ValueError("k_out must be a contiguous 4-D device tensor [B,Hkv,out_cap,d]")
-    out_cap = k_out.shape[2]
-    if v_out is None:
-        v_out = torch.empty((B, Hkv, out_cap, d), dtype=v.dtype, device=dev)
-    if acc_out is None:
-        acc_out = torch.empty((B, Hkv, out_cap), dtype=torch.float32, device=dev)
-    if index is None:
-        index = torch.empty((B, Hkv, rows), dtype=torch.int32, device=dev)
-    if lens_out is None:
-        lens_out = torch.empty(B, dtype=torch.int32, device=dev)
-    _tensor("k_out", k_out, (B, Hkv, out_cap, d), dev)
-    _tensor("v_out", v_out, (B, Hkv, out_cap, d), dev)
-    _same_type(dt, k_out=k_out, v_out=v_out)
-    _tensor("acc_out", acc_out, (B, Hkv, out_cap), dev, torch.float32)
-    _tensor("index", index, (B, Hkv, rows), dev, torch.int32)
-    _tensor("lens_out", lens_out, (B,), dev, torch.int32)
+    given = k_out if k_out is not None else v_out
+    out_cap = rows if given is None else _four("k_out", given)[2]
+    shape = (B, Hkv, out_cap, d)
+    new = lambda size, dtype: _torch.empty(size, dtype=dtype, device=k.device)  # noqa: E731
+    k_out = new(shape, first) if k_out is None else _operand("k_out", k_out, shape, dev, first, dt)
+    v_out = new(shape, first) if v_out is None else _operand("v_out", v_out, shape, dev, first, dt)
+    shape = (B, Hkv, out_cap)
+    acc_out = new(shape, f32) if acc_out is None else _tensor("acc_out", acc_out, shape, dev, f32)
+    shape = (B, Hkv, rows)
+    index = new(shape, i32) if index is None else _tensor("index", index, shape, dev, i32)
+    lens_out = new((B,), i32) if lens_out is None else _tensor("lens_out", lens_out, (B,), dev, i32)
     opts = _opts(None, stream)
     rc = L.attn_evict(k.data_ptr(), v.data_ptr(), acc.data_ptr(), _lens_ptr(lens, B, dev), k_out.data_ptr(),
                       v_out.data_ptr(), acc_out.data_ptr(), index.data_ptr(), lens_out.data_ptr(), B, Hkv, Sk, cap,

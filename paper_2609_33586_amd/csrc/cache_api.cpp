@@ -59,9 +59,13 @@ int check_kind(int d, float scale, int dtype, const attn_opts* opts, float* c1, 
   return ATTN_OK;
 }
 
-// Prefix rows of a KV head beyond one block of WROWS take workgroups of
-// PREFIX_ROWS rows (the keys are read once for four times as many).
-int prefix_rows(long long rows) { return rows > WROWS ? PREFIX_ROWS : WROWS; }
+// Query rows of a prefix workgroup.  Up to four blocks of WROWS rows of a KV head
+// over the batch, each takes its own workgroup, whose four waves share out the
+// keys (the others' reads come from L2): fewer rows would leave waves of the
+// rows form idle, and a part takes half as long.  Beyond, PREFIX_ROWS rows share
+// each tile.  Times of a call with blocks of 32 / of 128 rows: 84 rows, 5003 keys
+// FP8 18 / 29 us; 128 rows, 8K keys BF16 33 / 35; 256 rows, 32K keys FP8 87 / 72.
+int prefix_rows(long long rows) { return rows > 4 * WROWS ? PREFIX_ROWS : WROWS; }
 
 size_t prefix_workspace(long long rows, int parts, int d) {
   return parts <= 1 ? 0 : (size_t)rows * (size_t)parts * ((size_t)d + 2) * sizeof(float);
@@ -116,9 +120,9 @@ int attn_decode_prefix_split_keys(int B, int Hq, int Hkv, int Sq, int P, int Sk,
     if (parts > tiles / least) parts = tiles / least;
     return parts <= 1 ? 0 : (int)(ceil_div(tiles, parts) * BC);
   };
-  const int block = prefix_rows(B * rows);
-  if (P > 0) *prefix_split_keys = cut(P, Hkv * ceil_div(B * rows, block), block == WROWS ? 512 : 256, 4);
-  if (Sk > 0) *split_keys = cut(Sk, (long long)B * Hkv * ceil_div(rows, WROWS), 512, 8);
+  // two workgroups a compute unit, half of them for each of the two kinds
+  if (P > 0) *prefix_split_keys = cut(P, Hkv * ceil_div(B * rows, prefix_rows(B * rows)), Sk > 0 ? 256 : 512, 4);
+  if (Sk > 0) *split_keys = cut(Sk, (long long)B * Hkv * ceil_div(rows, WROWS), P > 0 ? 256 : 512, 8);
   return ATTN_OK;
 }
 

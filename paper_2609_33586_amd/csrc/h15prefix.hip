@@ -584,39 +584,58 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 // O and LSE of a row from its parts: m = max m_p, f_p = 2^(c1 (m_p - m)),
 // l = sum f_p l_p, O = sum f_p O_p / l * v_descale, LSE = ln2 (m c1 + log2 l),
 // over the parts with l_p != 0 (the O of others was never written).  One wave
-// a row; a lane holds four columns and every (64 / (D / 4))th part.
+// a row; a lane holds four columns and every (64 / (D / 4))th part.  32 parts'
+// (m, l), one a lane, and then their rows are asked for at once: read one after
+// the other, 17 parts of 1024 rows took 8 us.
 template <int D>
 __global__ __launch_bounds__(256) void attn_prefix_merge(PrefixParams p) {
-  constexpr int LPP = D / 4, PG = 64 / LPP;
+  constexpr int LPP = D / 4, PG = 64 / LPP, MOST = 32, EACH = MOST / PG;
   const int lane = threadIdx.x & 63, pg = lane / LPP, col = 4 * (lane % LPP);
   const long long row = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (row >= (long long)p.B * p.Hq * p.Sq) return;
-  const float* ml = p.part_ml + (size_t)row * p.parts * 2;
-  const float* po = p.part_o + (size_t)row * p.parts * D;
-  float m = -INFINITY;
-  for (int s = lane; s < p.parts; s += 64) {
-    const f32x2 x = *(const f32x2*)(ml + 2 * s);
-    if (x[1] != 0.0f) m = __builtin_fmaxf(m, x[0]);
-  }
-#pragma unroll
-  for (int x = 32; x >= 1; x >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, x, 64));
-  float l = 0.0f;
+  const float* const ml = p.part_ml + (size_t)row * p.parts * 2;
+  const float* const po = p.part_o + (size_t)row * p.parts * D;
+  float m = -INFINITY, l = 0.0f;  // of the parts so far
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = pg; s < p.parts; s += PG) {
-    const f32x2 x = *(const f32x2*)(ml + 2 * s);
-    if (x[1] == 0.0f) continue;
-    const float f = __builtin_amdgcn_exp2f((x[0] - m) * p.c1);
-    const f32x4 o = *(const f32x4*)(po + (size_t)s * D + col);
-    l += f * x[1];
+  for (int s0 = 0; s0 < p.parts; s0 += MOST) {
+    const int here = min(p.parts - s0, MOST);
+    const f32x2 x = *(const f32x2*)(ml + 2 * (s0 + min(lane, here - 1)));
+    const bool some = lane < here && x[1] != 0.0f;
+    // (rows beyond the last part read as zero and touch no memory)
+    const __amdgpu_buffer_rsrc_t rsrc = rows_rsrc((const uint8_t*)(po + (size_t)s0 * D), here * D * 4);
+    f32x4 v[EACH];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] += f * o[e];
+    for (int u = 0; u < EACH; ++u) {
+      if (u > 0 && u * PG >= here) break;
+      v[u] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, ((u * PG + pg) * D + col) * 4, 0, 0));
+    }
+    float top = some ? x[0] : -INFINITY;
+#pragma unroll
+    for (int y = 32; y >= 1; y >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, y, 64));
+    const float m_new = __builtin_fmaxf(m, top);
+    if (m_new == -INFINITY && !__ballot(some)) continue;  // nothing yet
+    const float base = m_new == -INFINITY ? 0.0f : m_new;
+    const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - base) * p.c1);
+    const float f = some ? __builtin_amdgcn_exp2f((x[0] - base) * p.c1) : 0.0f;
+    float sum = some ? f * x[1] : 0.0f;
+#pragma unroll
+    for (int y = 32; y >= 1; y >>= 1) sum += __shfl_xor(sum, y, 64);
+    l = l * alpha + sum;
+    m = m_new;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] *= alpha;
+#pragma unroll
+    for (int u = 0; u < EACH; ++u) {
+      if (u > 0 && u * PG >= here) break;
+      const float fs = __shfl(f, u * PG + pg, 64);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += fs != 0.0f ? fs * v[u][e] : 0.0f;
+    }
   }
 #pragma unroll
-  for (int x = LPP; x < 64; x <<= 1) {
-    l += __shfl_xor(l, x, 64);
+  for (int x = LPP; x < 64; x <<= 1)
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], x, 64);
-  }
   if (pg == 0) {
     store_row4(p.o + (size_t)row * D + col, acc, inverse(l, p.vd));
     if (p.lse && col == 0) p.lse[row] = row_lse(m, l, p.c1);

@@ -145,6 +145,25 @@ struct RowOperand {
   }
 };
 
+// 16 bytes, chunk c of consecutive rows, into their BF16 rows in LDS, which are
+// then read as operands with K's swizzle.  An
+// FP8 chunk becomes two, in the operand order of RowOperand: chunk 2 t + g of a
+// row holds the operands 2 t and 2 t + 1 of half g, which lie at 2 (2 t) + g and
+// 2 (2 t + 1) + g.
+template <int DT, int D>
+__device__ __forceinline__ void store_row_chunk(uint8_t* rows, int c, i32x4 x) {
+  constexpr int NCH = Cfg<DT, D>::NCH;
+  const int r = c / NCH, i = c % NCH, swz = k_swz<DT_BF16, D>(r);
+  uint8_t* const row = rows + r * Cfg<DT_BF16, D>::RB;
+  if constexpr (DT == DT_BF16) {
+    *(i32x4*)(row + ((i ^ swz) << 4)) = x;
+  } else {
+    const int t = i >> 1, g = i & 1;
+    *(bf16x8*)(row + (((4 * t + g) ^ swz) << 4)) = widen(x[0], x[1]);
+    *(bf16x8*)(row + (((4 * t + 2 + g) ^ swz) << 4)) = widen(x[2], x[3]);
+  }
+}
+
 }  // namespace
 
 #endif  // H15ATTN_UNIT_DEVICE_H

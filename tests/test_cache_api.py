@@ -141,17 +141,25 @@ def test_binding_refuses_host_tensors():
         pkg.attn_evict(k, k, f, keep=2, recent=1)
 
 
-def test_binding_checks_shapes_and_types():
-    cpu = torch.device("cpu")
-    good = torch.zeros(2, 3, 4)
-    assert cache._tensor("x", good, (2, None, 4), cpu, torch.float32) is good
+def test_binding_checks_shapes_and_types(L):
+    good = torch.zeros(2, 3, 4)  # (device -1: the host)
+    assert cache._tensor("x", good, (2, 3, 4), -1, torch.float32) is good
     for bad in (torch.zeros(2, 3, 5), torch.zeros(2, 3), torch.zeros(2, 4, 3).transpose(1, 2),
                 torch.zeros(2, 3, 4, dtype=torch.int32)):
-        with pytest.raises(ValueError, match=r"x must be a contiguous tensor \[2x\?x4\]"):
-            cache._tensor("x", bad, (2, None, 4), cpu, torch.float32)
-    with pytest.raises(TypeError):
-        cache._same_type(pkg.ATTN_BF16, k=torch.zeros(2, dtype=torch.uint8))
-    with pytest.raises(ValueError):
-        cache._lens_ptr(torch.zeros(2, dtype=torch.int64), 2, cpu)
-    with pytest.raises(ValueError):
-        cache._space(torch.zeros(4, 4).t(), 8, cpu, None)
+        with pytest.raises(ValueError, match=r"x must be a contiguous tensor \[2x3x4\] of torch.float32"):
+            cache._tensor("x", bad, (2, 3, 4), -1, torch.float32)
+    with pytest.raises(ValueError, match="GPU 0"):
+        cache._tensor("x", good, (2, 3, 4), 0)
+    k = torch.zeros(2, dtype=torch.uint8)
+    assert cache._operand("k", k, (2,), -1, torch.float8_e4m3fn, pkg.ATTN_FP8_E4M3) is k  # e4m3 codes as bytes
+    with pytest.raises(TypeError, match="k and the first operand"):
+        cache._operand("k", k, (2,), -1, torch.bfloat16, pkg.ATTN_BF16)
+    with pytest.raises(ValueError, match="4-D"):
+        cache._four("k", k)
+    assert cache._lens_ptr(None, 2, -1) is None
+    for bad in (torch.zeros(2, dtype=torch.int64), torch.zeros(3, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="lens"):
+            cache._lens_ptr(bad, 2, -1)
+    with pytest.raises(ValueError, match="workspace"):
+        cache._space(torch.zeros(4, 4).t(), lambda: 8, -1, None)
+    assert cache._space(None, lambda: 0, -1, None) == (None, 0, None)

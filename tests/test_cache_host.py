@@ -41,13 +41,15 @@ def prefix_form(L, B, Hq, Hkv, Sq, P, Sk, p_cut=0, cut=0, causal=1):
 
 
 def test_prefix_forms(host):
-    # up to 32 rows of a KV head over the batch: workgroups of 32 rows, else of 128
-    assert prefix_form(host, 8, 8, 2, 1, 1000, 100)["p_rows"] == 32
-    f = prefix_form(host, 33, 8, 8, 1, 1000, 100, 512, 0)
-    assert f["p_rows"] == 128 and f["p_parts"] == 2 and f["o_parts"] == 1 and f["p_groups"] == 8 * 2
+    # up to 128 rows of a KV head over the batch: workgroups of 32 rows, else of 128
+    f = prefix_form(host, 8, 8, 2, 1, 1000, 100)
+    assert f["p_rows"] == 32 and f["p_groups"] == 2 and f["o_groups"] == 8 * 2
+    f = prefix_form(host, 32, 32, 8, 1, 1000, 100, 512, 0)
+    assert f["p_rows"] == 32 and f["p_groups"] == 8 * 2 * 4
+    f = prefix_form(host, 33, 32, 8, 1, 1000, 100, 512, 0)
+    assert f["p_rows"] == 128 and f["p_parts"] == 2 and f["o_parts"] == 1 and f["p_groups"] == 8 * 2 * 2
     assert f["o_groups"] == 33 * 8 and f["o_split"] == 128 and f["p_split"] == 512
-    assert prefix_form(host, 33, 8, 8, 1, 1000, 0)["p_rows"] == 32  # a single part writes O itself
-    assert prefix_form(host, 65, 16, 8, 1, 1000, 300, 0, 128)["p_groups"] == 8 * 2  # 130 rows: two blocks
+    assert prefix_form(host, 33, 32, 8, 1, 1000, 0)["p_rows"] == 32  # a single part writes O itself
     f = prefix_form(host, 2, 12, 2, 16, 0, 300, 0, 128)
     assert f["p_groups"] == 0 and f["o_groups"] == 2 * 2 * 3 * 3  # 96 rows a sequence: three blocks
     # one query row sees its whole cache with or without a causal mask

@@ -35,14 +35,14 @@ def run_and_check(dt, d, B, Hq, Hkv, Sq, P, Sk, lens, mode, p_cut, cut, causal, 
                  what)
 
 
-# (B, Hq, Hkv, Sq, P, Sk, lens, p_cut, cut): up to 32 rows of a KV head the keys
-# form, beyond the rows form
+# (B, Hq, Hkv, Sq, P, Sk, lens, p_cut, cut): up to 128 rows of a KV head over the
+# batch the keys form of a prefix workgroup, beyond the rows form
 SHAPES = [
     (1, 1, 1, 1, 1, 1, None, 0, 0),                       # one key on each side
     (3, 4, 2, 1, 200, 70, [70, 0, 33], 0, 0),             # an empty cache, two parts
     (2, 4, 1, 4, 513, 300, [300, 2], 128, 256),           # fewer own keys than rows
     (4, 8, 1, 1, 640, 1, [1, 1, 0, 1], 256, 128),         # 32 rows: a full block of the keys form
-    (5, 8, 1, 1, 129, 257, [257, 128, 1, 0, 200], 0, 128),  # 40 rows: the rows form, two of its waves empty
+    (5, 8, 1, 1, 129, 257, [257, 128, 1, 0, 200], 0, 128),  # 40 rows: two blocks of the keys form
     (9, 6, 2, 5, 700, 65, [65, 64, 63, 0, 4, 5, 6, 1, 30], 384, 0),  # 135 rows: two row blocks, the second ragged
     (2, 12, 4, 16, 300, 260, None, 128, 128),             # 48 rows a sequence: two own row blocks
     (3, 2, 1, 3, 0, 400, [400, 1, 129], 0, 128),          # no prefix
@@ -50,6 +50,10 @@ SHAPES = [
     (3, 2, 1, 2, 400, 0, None, 128, 0),                   # no own caches
     (40, 2, 1, 1, 150, 0, None, 0, 0),                    # no own caches, one part, 80 rows
     (17, 16, 2, 1, 2000, 40, None, 512, 0),               # 136 rows, several tiles a part
+    (32, 4, 1, 1, 600, 20, None, 256, 0),                 # 128 rows: four full blocks of the keys form
+    (43, 3, 1, 1, 1, 30, None, 0, 0),                     # 129 rows, one prefix key
+    (3, 96, 1, 1, 1300, 70, [70, 0, 1], 1152, 0),         # 288 rows: three row blocks, the last with one wave
+    (70, 4, 1, 1, 150, 0, None, 0, 0),                    # 280 rows, one part
 ]
 
 
