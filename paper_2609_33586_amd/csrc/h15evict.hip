@@ -40,7 +40,8 @@ __device__ __forceinline__ uint32_t rank_of(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Adds one to the bin of every lane that has one (bin >= 0).  LDS adds to one
+// Adds one to the bin of every lane that has one (bin >= 0), in two histograms,
+// of odd and of even lanes.  LDS adds to one
 // address follow each other: lanes that all have the same bin, as with equal
 // weights, are counted together.
 __device__ __forceinline__ void count(uint32_t* hist, int bin, int lane) {
@@ -97,7 +98,12 @@ __global__ __launch_bounds__(SEL) void attn_evict_select(EvictParams p) {
   for (int i = late + tid; i < n; i += SEL) index[want + (uint32_t)(i - late)] = i;
   if (want == 0) return;
 
-  // (0, which no weight has, up to a whole step)
+  constexpr int PER = BINS / SEL;
+#pragma unroll
+  for (int i = 0; i < 2 * PER; ++i) hist[0][i * SEL + tid] = 0;
+  __syncthreads();
+  // The first digits are counted as the weights come in.  (Rank 0, which no
+  // weight has, up to a whole step.)
   const int held = min((late + STEP - 1) / STEP * STEP, HELD);
   for (int i0 = tid; i0 < held; i0 += BATCH * SEL) {
     float x[BATCH];
@@ -106,9 +112,15 @@ __global__ __launch_bounds__(SEL) void attn_evict_select(EvictParams p) {
 #pragma unroll
     for (int j = 0; j < BATCH; ++j) {
       const int i = i0 + j * SEL;
-      if (i < held) ranks[i] = i < late ? rank_of(x[j]) : 0;
+      if (i - lane >= held) break;
+      const uint32_t u = i < late ? rank_of(x[j]) : 0;
+      ranks[i] = u;
+      count(hist[lane & 1], u != 0 ? (int)(u >> 21) : -1, lane);
     }
   }
+  for (int i0 = HELD + tid; i0 - lane < late; i0 += SEL)
+    count(hist[lane & 1], i0 < late ? (int)(rank_of(acc[i0]) >> 21) : -1, lane);
+  __syncthreads();
   // the ranks of four keys, i a multiple of 4
   auto four = [&](int i) {
     if (i < HELD) return *(const u32x4*)&ranks[i];
@@ -121,26 +133,27 @@ __global__ __launch_bounds__(SEL) void attn_evict_select(EvictParams p) {
 #pragma unroll 1
   for (int round = 0; round < 3; ++round) {
     const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, width = round < 2 ? 11 : 10;
-    constexpr int PER = BINS / SEL;
+    if (round > 0) {
+      // (whole waves: the lanes beyond the last key have no bin)
+      for (int i = wave * STEP; i < late; i += SW * STEP) {
+        const u32x4 u = four(i + 4 * lane);
+        bool in[4], any = false;
 #pragma unroll
-    for (int i = 0; i < 2 * PER; ++i) hist[0][i * SEL + tid] = 0;
-    __syncthreads();
-    // (whole waves: the lanes beyond the last key have no bin)
-    for (int i = wave * STEP; i < late; i += SW * STEP) {
-      const u32x4 u = four(i + 4 * lane);
+        for (int e = 0; e < 4; ++e) any |= in[e] = (u[e] >> (shift + width)) == digits;
+        if (!__ballot(any)) continue;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const bool in = u[e] != 0 && (round == 0 || (u[e] >> (shift + width)) == digits);
-        if (__ballot(in)) count(hist[lane & 1], in ? (int)((u[e] >> shift) & ((1u << width) - 1)) : -1, lane);
+        for (int e = 0; e < 4; ++e)
+          if (__ballot(in[e])) count(hist[lane & 1], in[e] ? (int)((u[e] >> shift) & ((1u << width) - 1)) : -1, lane);
       }
+      __syncthreads();
     }
-    __syncthreads();
     // a thread: two bins, from the top; the bin in which the count passes `left`
     uint32_t c[PER], own = 0;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const int bin = BINS - 1 - (PER * tid + j);
       c[j] = hist[0][bin] + hist[1][bin];
+      hist[0][bin] = hist[1][bin] = 0;  // for the next round
       own += c[j];
     }
     const uint32_t upto = scan(own);
