@@ -69,8 +69,9 @@ extern "C" {
  * multiple of attn_tile_bc(), or a missing or short workspace;
  * ATTN_EUNSUPPORTED for d not in {64, 128}, an unknown dtype or exp_mode, a
  * pointer that is not 16-byte aligned (lse, lens: 4), a rescale threshold
- * other than 0, B * Hq * Sq > 2^30, one head's cache or prefix beyond 2^31 - 1
- * bytes, or more than 2^31 - 1 workgroups. */
+ * other than 0, B * Hq * Sq > 2^30 (2^26 - 1 with more than one part), one
+ * head's cache or prefix beyond 2^31 - 1 bytes, or more than 2^24 - 1
+ * workgroups. */
 int attn_decode_prefix(const void* q, const void* kp, const void* vp, const void* k, const void* v,
                        const int32_t* lens, void* o, float* lse, int B, int Hq, int Hkv, int Sq, int P, int P_cap,
                        int Sk, int Sk_cap, int d, int causal, float scale, int dtype, int exp_mode,
@@ -142,7 +143,8 @@ size_t attn_key_weights_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Sk, 
  * positive, Sk > Sk_cap, keep < 1 or > out_cap, recent < 0, or an output that
  * overlaps an input or another output; ATTN_EUNSUPPORTED for d not in
  * {64, 128}, an unknown dtype, k, v, k_out or v_out not 16-byte aligned (the
- * others: 4), or more than 2^31 - 1 workgroups. */
+ * others: 4), B * Hkv beyond 2^22 - 1, or more than 2^32 - 256 chunks of 16
+ * bytes in the rows of K that may stay. */
 int attn_evict(const void* k, const void* v, const float* acc, const int32_t* lens, void* k_out, void* v_out,
                float* acc_out, int32_t* index, int32_t* lens_out, int B, int Hkv, int Sk, int Sk_cap, int out_cap,
                int d, int keep, int recent, int dtype, const attn_opts* opts);

@@ -17,6 +17,10 @@ bool finite_pos(float x) { return x > 0.0f && x < INFINITY; }
 
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
+// Work-items of a launch are counted in 32 bits: workgroups of 256 threads, and
+// rows of a merge, which have 64 each.
+constexpr long long MAX_GROUPS = (1LL << 24) - 1, MAX_MERGE_ROWS = (1LL << 26) - 1;
+
 // Input-rounding order of an exp_mode that the caches' decode offers, 0 for
 // the hardware exponential, -1 for others.
 int exp_order(int exp_mode) {
@@ -184,7 +188,7 @@ int attn_decode_prefix(const void* q, const void* kp, const void* vp, const void
   p.p_blocks = (int)ceil_div((long long)B * p.R, p.p_rows);
   p.o_blocks = (int)ceil_div(p.R, WROWS);
   const long long pg = (long long)Hkv * p.p_parts * p.p_blocks, og = (long long)B * Hkv * p.o_parts * p.o_blocks;
-  if (pg + og > INT32_MAX) return ATTN_EUNSUPPORTED;
+  if (pg + og > MAX_GROUPS || (p.parts > 1 && rows > MAX_MERGE_ROWS)) return ATTN_EUNSUPPORTED;
   p.p_groups = (int)pg;
   p.o_groups = (int)og;
   p.ck = ldexpf(p.c1, order);
@@ -245,7 +249,9 @@ int attn_key_weights(const void* q, const void* k, const float* lse, const int32
     p.blocks = (int)ceil_div(units, 4 * p.span);
   }
   p.decay = decay;
-  if ((long long)B * Hkv * p.parts * p.blocks > INT32_MAX) return ATTN_EUNSUPPORTED;
+  // (the sum of the parts takes blocks of 256 keys)
+  const long long heads = (long long)B * Hkv;
+  if (heads * p.parts * p.blocks > MAX_GROUPS || heads * ceil_div(Sk, 256) > MAX_GROUPS) return ATTN_EUNSUPPORTED;
   if (p.parts > 1) {
     const size_t need = (size_t)p.parts * B * Hkv * Sk * sizeof(float);
     if (!workspace || misaligned(workspace, 16) || workspace_bytes < need) return ATTN_EINVAL;
@@ -270,9 +276,9 @@ int attn_evict(const void* k, const void* v, const float* acc, const int32_t* le
   EvictParams p = {};
   p.row_bytes = d * elem_bytes(dtype);
   const size_t heads = (size_t)B * Hkv;
-  if (heads > INT32_MAX) return ATTN_EUNSUPPORTED;
-  // workgroups of the gather (at most 16 threads a row)
-  if (ceil_div((long long)heads * (p.row_bytes / 16), 256) * (long long)keep > INT32_MAX) return ATTN_EUNSUPPORTED;
+  // a selection has 1024 threads; the gather 4 to 16 a row
+  if (heads > MAX_GROUPS / 4 || (long long)heads * keep * (p.row_bytes / 16) > MAX_GROUPS * 256)
+    return ATTN_EUNSUPPORTED;
   const Range in[] = {range(k, heads * Sk_cap * p.row_bytes), range(v, heads * Sk_cap * p.row_bytes),
                       range(acc, heads * Sk_cap * 4), range(lens, lens ? (size_t)B * 4 : 0)};
   const Range out[] = {range(k_out, heads * out_cap * p.row_bytes), range(v_out, heads * out_cap * p.row_bytes),

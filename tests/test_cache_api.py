@@ -50,7 +50,7 @@ def test_prefix_refusals(L):
         assert prefix(L, **kw) == INV, kw
     for kw in ({"d": 96}, {"dtype": 2}, {"mode": pkg.ATTN_EXP_ROWMAX_POT}, {"mode": 7}, {"lens": FAKE + 2},
                {"lse": FAKE + 1}, {"o_": opts(tau=8.0)}, {"B": 1 << 15, "Hq": 1 << 14, "Sq": 4}, {"P_cap": 1 << 24},
-               {"cap": 1 << 24}):
+               {"cap": 1 << 24}, {"B": 1 << 12, "Hq": 1 << 13, "Hkv": 1 << 13}, {"B": 1 << 13, "Hq": 1 << 13, "Hkv": 1}):
         assert prefix(L, **kw) == UNS, kw
     for bad in ((0.0, 1.0, 1.0), (1.0, math.inf, 1.0), (1.0, 1.0, -1.0)):
         assert prefix(L, dtype=1, o_=opts(*bad)) == INV
@@ -86,7 +86,8 @@ def test_weights_refusals(L):
     for kw in ({"B": 0}, {"Hq": 0}, {"Hkv": 0}, {"Hkv": 3}, {"Sq": 0}, {"Sk": 0}, {"Sk": 321}, {"d": 0}, {"scale": -1.0},
                {"decay": -0.5}, {"decay": math.nan}, {"decay": math.inf}, {"dtype": 1}, {"Sq": 4096}):
         assert weights(L, **kw) == INV, kw  # (Sq 4096: a workspace is wanted)
-    for kw in ({"d": 96}, {"dtype": 2}, {"o_": opts(tau=1.0)}, {"cap": 1 << 24}, {"Sq": 1 << 23}):
+    for kw in ({"d": 96}, {"dtype": 2}, {"o_": opts(tau=1.0)}, {"cap": 1 << 24}, {"Sq": 1 << 23},
+               {"B": 1 << 12, "Hq": 1 << 12, "Hkv": 1 << 12}):
         assert weights(L, **kw) == UNS, kw
     need = pkg.attn_key_weights_workspace_bytes(2, 4, 2, 4096, 300, 128)
     assert need > 0 and need % (2 * 2 * 300 * 4) == 0
@@ -115,7 +116,8 @@ def test_evict_refusals(L):
         assert evict(L, at) == UNS, i
     for kw in ({"B": 0}, {"Hkv": 0}, {"Sk": 0}, {"Sk": 321}, {"out_cap": 99}, {"keep": 0}, {"recent": -1}, {"d": 0}):
         assert evict(L, **kw) == INV, kw
-    for kw in ({"d": 96}, {"dtype": 2}, {"lens": FAKE + 2}, {"B": 1 << 14, "Hkv": 1 << 14, "keep": 200, "out_cap": 200}):
+    for kw in ({"d": 96}, {"dtype": 2}, {"lens": FAKE + 2}, {"B": 1 << 14, "Hkv": 1 << 14, "keep": 200, "out_cap": 200},
+               {"B": 1 << 11, "Hkv": 1 << 11, "keep": 1, "recent": 0}):
         assert evict(L, **kw) == UNS, kw
     for i in range(3, 8):  # an output on an input or on another output, from its first or up to its last byte
         for j in range(8):

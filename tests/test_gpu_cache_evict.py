@@ -51,6 +51,15 @@ def test_sizes(n, keep, recent, dt, d):
     check(k, v, acc, None, keep, recent)
 
 
+@pytest.mark.parametrize("n,keep,recent", [(32768, 2048, 64), (32769, 32768, 0), (33024, 100, 0), (40000, 20000, 500),
+                                           (100003, 5, 1), (70001, 69000, 68999)])
+def test_caches_beyond_what_lds_holds(n, keep, recent):
+    k, v, acc = caches(FP8, 2, 1, n, 64, 60)
+    say(f"evict n={n} keep={keep} recent={recent}")
+    check(k, v, acc, None, keep, recent)
+    check(k, v, torch.floor(acc), [n, n - 200], keep, recent)  # many equal ones
+
+
 def test_ragged_batch_with_room_to_spare():
     k, v, acc = caches(BF16, 6, 3, 700, 128, 20)
     for keep, recent, cap in ((128, 16, 200), (300, 0, 300), (690, 690, 1000)):
