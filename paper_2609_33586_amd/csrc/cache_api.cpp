@@ -71,6 +71,18 @@ int check_kind(int d, float scale, int dtype, const attn_opts* opts, float* c1, 
 // FP8 18 / 29 us; 128 rows, 8K keys BF16 33 / 35; 256 rows, 32K keys FP8 87 / 72.
 int prefix_rows(long long rows) { return rows > 4 * WROWS ? PREFIX_ROWS : WROWS; }
 
+// A short prefix in one part before own caches in one: each own cache's
+// workgroup takes the prefix's keys too, at most two rounds of them, and there is
+// nothing to merge.  Not where many caches of a few rows would each take them.
+// Times of a call so / by two launches: 4 caches, 500 + 60 keys BF16 d = 64
+// 11.0 / 13.6 us; 64 caches of 8 heads, 256 + 3000 keys d = 128 138 / 143; a
+// prompt of 512 positions, 256 + 512 keys 20.9 / 34.6; 128 caches of 8 heads, 500 +
+// 512 keys FP8 37 / 31.
+bool chained(int P, int row_bytes, const PrefixParams& p) {
+  const int round = row_bytes >= 256 ? BC : 2 * BC;  // keys
+  return p.p_parts == 1 && p.o_parts == 1 && P <= 2 * round && (p.R >= WROWS || p.o_groups <= 512);
+}
+
 size_t prefix_workspace(long long rows, int parts, int d) {
   return parts <= 1 ? 0 : (size_t)rows * (size_t)parts * ((size_t)d + 2) * sizeof(float);
 }
@@ -193,6 +205,10 @@ int attn_decode_prefix(const void* q, const void* kp, const void* vp, const void
   p.o_groups = (int)og;
   p.ck = ldexpf(p.c1, order);
   const size_t need = prefix_workspace(rows, p.parts, d);
+  if (chained(P, (int)row, p)) {
+    p.chain = p.parts = 1;
+    p.p_groups = 0;
+  }
   if (need) {
     if (!workspace || misaligned(workspace, 16) || workspace_bytes < need) return ATTN_EINVAL;
     p.part_o = (float*)workspace;

@@ -42,7 +42,8 @@ struct PrefixParams {
   int P, P_cap, Sk, Sk_cap, causal;
   int p_parts, p_split;  // parts of the prefix (0: no prefix) and their keys
   int o_parts, o_split;  // parts of the own caches (0: none) and their keys
-  int parts;             // p_parts + o_parts
+  int parts;             // p_parts + o_parts (chained: 1)
+  int chain;             // a workgroup of an own cache takes the prefix first (one part of each)
   int p_rows;            // query rows of a prefix workgroup: PREFIX_ROWS or WROWS
   int p_blocks, o_blocks;  // row blocks of a KV head's rows of all sequences, of one sequence
   int p_groups, o_groups;  // workgroups

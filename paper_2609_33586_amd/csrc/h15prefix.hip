@@ -13,8 +13,27 @@
 // Two forms of a workgroup (4 waves):
 //   keys  32 query rows; each wave takes its own keys of a round (UNIT of
 //         them), copies them into its own LDS slots and exchanges only the
-//         maxima of its units with the others (one barrier a round);
-//   rows  128 query rows, 32 a wave; the waves share each tile of 128 keys.
+//         maxima of its units with the others (one barrier a round); a weight
+//         is rounded relative to the running maximum at its own tile, the
+//         prefix maximum of the round's units.  All own caches, and prefixes
+//         of up to four blocks of rows;
+//   rows  128 query rows, 32 a wave; the waves share each tile of 128 keys, so
+//         that more rows do not read the prefix again.
+// A workgroup of an own cache may take a short prefix first, in the keys form:
+// one launch and nothing to merge.  (The rules between these: cache_api.cpp.)
+//
+// What bounds it: HBM for BF16 (32 sequences of 32 heads over 8 KV heads, 8K
+// prefix, up to 1K own keys: 29 us + 4 of the merge for 115 MB; 64 such with 32K
+// and 2K keys each: 143 us for 671 MB, 4.7 TB/s).  A keys round of 128 BF16 keys
+// takes 3900 cycles, of which 750 wait for K; two workgroups share a compute
+// unit.  FP8 with many rows: a rows tile takes 5900 cycles, 1500 for Q K^T, 1900
+// for the weights and 1800 for P V (1024 of the matrix core each) in turn, next
+// to one workgroup of own caches (64 sequences, 32K prefix, 2K own keys: 66 us +
+// 6 for 230 MB).  Widening each FP8 tile once for the four waves, through
+// registers into BF16 tiles, was level for the exponential (LDS reads double)
+// and slower for the lattice weights, whose registers spilled (5K keys, 84 rows:
+// 25 -> 36 us).  Short caches wait: 4 chats of 500 + 60 keys BF16 d = 64 take 8.8 us
+// in one launch, 11 with the call.
 //
 // Arithmetic: that of attn_decode for BF16.  FP8 operands are widened to BF16,
 // which holds every e4m3 value, and meet in the BF16 matrix core: the FP8
@@ -168,7 +187,8 @@ struct Work {
   int row0;   // first of its rows: of the sequence's R, or of the prefix's B R
   int nrows;
   int open;   // the keys from here on (in the part) are not seen by every row
-  bool prefix;
+  bool prefix;  // the rows are the prefix's
+  bool whole;   // every row sees every key
 };
 
 // Output row (over [B][Hq][Sq]) of row r of a workgroup
@@ -198,178 +218,209 @@ __device__ __forceinline__ float row_lse(float m, float l, float c1) {
   return l == 0.0f ? -INFINITY : 0.69314718055994531f * (m * c1 + log2f(l));
 }
 
-template <int DT, int D, int MODE>
-__device__ __forceinline__ void keys_form(const PrefixParams& p, const Work& w, uint8_t* ksm, uint8_t* vsm,
+// CHAIN: the same rows meet `before` first, a part of its own with a running
+// maximum of its own, whose sums wait in registers and are merged in at the end.
+template <int DT, int D, int MODE, bool CHAIN>
+__device__ __forceinline__ void keys_form(const PrefixParams& p, const Work& before, const Work& own, uint8_t* ksm, uint8_t* vsm,
                                           float (*mx_lds)[32][NW], float (*m_lds)[NW], float (*l_lds)[NW]) {
   using C = PCfg<DT, D>;
   constexpr int NB = C::NB, UNIT = C::UNIT, TPR = C::TPR, SLOT = C::SLOT, RB = C::RB;
   constexpr int NDB = D / 32, LOADS = SLOT / 1024, RHALF = 16;
   const int tid = threadIdx.x, lane = tid & 63, i32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rowc = min(i32, w.nrows - 1);
-  // last key of the part that this lane's row sees
-  int limit = w.nk - 1;
-  if (!w.prefix && p.causal) limit = w.open + (w.row0 + rowc) % p.Sq - 1;
-
+  const int rowc = min(i32, own.nrows - 1);
   RowOperand<DT, D> q;
   {
-    const uint8_t* qp = p.q + out_row(p, w, rowc) * RB;
+    const uint8_t* qp = p.q + out_row(p, own, rowc) * RB;
 #pragma unroll
     for (int t = 0; t < q.CHUNKS; ++t) q.set(t, *(const i32x4*)(qp + 32 * t + 16 * g));
   }
-  // rows beyond the part read as zero without touching memory; scalar offsets
-  // stop at the resource's size, where every lane is out of range
-  const uint32_t part_bytes = (uint32_t)w.nk * RB;
-  const auto krsrc = rows_rsrc(w.k, part_bytes), vrsrc = rows_rsrc(w.v, part_bytes);
-  uint8_t* const kslot = ksm + wave * SLOT;
-  uint8_t* const vslot = vsm + wave * SLOT;
-  // the chunk swizzles repeat after every fourth copy at the latest
-  uint32_t koff[4], voff[2];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = copy_row<C::NCH>(i, lane);
-    koff[i] = (r - i * (64 / C::NCH)) * RB + (((lane % C::NCH) ^ k_swz<DT, D>(r)) << 4);
-  }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = copy_row<C::NCH>(i, lane);
-    voff[i] = (r - i * (64 / C::NCH)) * RB + (((lane % C::NCH) ^ v_swz<DT, D>(r)) << 4);
-  }
-  auto first_key = [&](int c) { return c * (TPR * BC) + wave * UNIT; };
-  auto stage = [&](const __amdgpu_buffer_rsrc_t rsrc, uint8_t* slot, const uint32_t* off, int mask,
-                   int c) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const uint32_t soff = min((uint32_t)first_key(c) * RB + i * 1024, part_bytes);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, LDS_PTR(void, slot + i * 1024), 16, off[i & mask], soff, 0, 0);
-    }
-  };
-  uint32_t vaddr[NDB];
-#pragma unroll
-  for (int db = 0; db < NDB; ++db)
-    vaddr[db] = v_address<DT, D>((uint32_t)(size_t)LDS_PTR(const uint8_t, vslot), db, lane);
-
-  f32x16 oacc[NDB];
-#pragma unroll
-  for (int db = 0; db < NDB; ++db) oacc[db] = f32x16{0.0f};
-  float m_seen = -INFINITY, m_wave = -INFINITY, l_part = 0.0f;
-  const int kswz = k_swz<DT, D>(i32);
-  const int wt = TPR == 1 ? 0 : wave >> 1;  // tile of the round
-
-  __builtin_amdgcn_sched_barrier(0);
-  stage(krsrc, kslot, koff, 3, 0);
-  __builtin_amdgcn_sched_barrier(0);
-  stage(vrsrc, vslot, voff, 1, 0);
-  __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-  for (int t = 0; t < q.CHUNKS * q.PER; ++t) asm volatile("" : "+v"(q.x[t]));
-  const int nrounds = (w.nk + TPR * BC - 1) / (TPR * BC);
+  // the chained part's sums: rows idx / (D / 4) of each half, four columns
+  constexpr int ITEMS = RHALF * (D / 4) / (NW * 64);
+  f32x4 held[2][ITEMS];
+  float held_m[2][ITEMS], held_l[2][ITEMS];
 #pragma unroll 1
-  for (int c = 0; c < nrounds; ++c) {
-    const int kw0 = first_key(c);
-    const bool need_mask = kw0 + UNIT > w.open || kw0 + UNIT > w.nk;
-    const int lim = min(limit, w.nk - 1) - kw0 - 4 * g;
-    // this round's K has landed once at most the V copies behind it are outstanding
-    wait_vmcnt<LOADS>();
-    f32x16 sv[NB];
+  for (int turn = CHAIN ? 0 : 1; turn < 2; ++turn) {
+    const Work& w = CHAIN && turn == 0 ? before : own;
+    // last key of the part that this lane's row sees
+    int limit = w.nk - 1;
+    if (!w.whole) limit = w.open + (w.row0 + rowc) % p.Sq - 1;
+    // rows beyond the part read as zero without touching memory; scalar offsets
+    // stop at the resource's size, where every lane is out of range
+    const uint32_t part_bytes = (uint32_t)w.nk * RB;
+    const auto krsrc = rows_rsrc(w.k, part_bytes), vrsrc = rows_rsrc(w.v, part_bytes);
+    uint8_t* const kslot = ksm + wave * SLOT;
+    uint8_t* const vslot = vsm + wave * SLOT;
+    // the chunk swizzles repeat after every fourth copy at the latest
+    uint32_t koff[4], voff[2];
 #pragma unroll
-    for (int t = 0; t < q.CHUNKS; ++t)
-#pragma unroll
-      for (int kb = 0; kb < NB; ++kb) {
-        const i32x4 kk = *(const i32x4*)(kslot + (32 * kb + i32) * RB + (((2 * t + g) ^ kswz) << 4));
-        sv[kb] = product(kk, q, t, t == 0 ? f32x16{0.0f} : sv[kb]);
-      }
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    stage(krsrc, kslot, koff, 3, c + 1);
-    settle_unit(sv);
-    if (need_mask) mask_unit(sv, lim, -INFINITY);
-    float ma, mb;
-    with_partner(unit_max(sv), ma, mb);
-    if (g == 0) mx_lds[c & 1][i32][wave] = __builtin_fmaxf(ma, mb);
-    // (the two copies of mx_lds alternate: a wave that runs ahead writes the other)
-    lds_barrier();
-    float anchor = m_seen;
-    {
-      const f32x4 x = *(const f32x4*)&mx_lds[c & 1][i32][0];
-      const float t0 = __builtin_fmaxf(x[0], x[1]), t1 = __builtin_fmaxf(x[2], x[3]);
-      m_seen = max3(m_seen, t0, t1);
-      anchor = TPR == 2 && wt == 0 ? __builtin_fmaxf(anchor, t0) : m_seen;
+    for (int i = 0; i < 4; ++i) {
+      const int r = copy_row<C::NCH>(i, lane);
+      koff[i] = (r - i * (64 / C::NCH)) * RB + (((lane % C::NCH) ^ k_swz<DT, D>(r)) << 4);
     }
-    // a row that has seen no key yet keeps m = -inf, l = 0, O = 0
-    const float alpha = anchor == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m_wave - anchor) * p.c1);
-    m_wave = anchor;
-    l_part *= alpha;
-    uint32_t wpk[NB][8];
-    weigh<MODE, NB>(sv, wpk, anchor == -INFINITY ? 0.0f : anchor, p.c1, p.ck, need_mask, lim, l_part);
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = copy_row<C::NCH>(i, lane);
+      voff[i] = (r - i * (64 / C::NCH)) * RB + (((lane % C::NCH) ^ v_swz<DT, D>(r)) << 4);
+    }
+    auto first_key = [&](int c) { return c * (TPR * BC) + wave * UNIT; };
+    auto stage = [&](const __amdgpu_buffer_rsrc_t rsrc, uint8_t* slot, const uint32_t* off, int mask,
+                     int c) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const uint32_t soff = min((uint32_t)first_key(c) * RB + i * 1024, part_bytes);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, LDS_PTR(void, slot + i * 1024), 16, off[i & mask], soff, 0, 0);
+      }
+    };
+    uint32_t vaddr[NDB];
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+      vaddr[db] = v_address<DT, D>((uint32_t)(size_t)LDS_PTR(const uint8_t, vslot), db, lane);
+
+    f32x16 oacc[NDB];
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) oacc[db] = f32x16{0.0f};
+    float m_seen = -INFINITY, m_wave = -INFINITY, l_part = 0.0f;
+    const int kswz = k_swz<DT, D>(i32);
+    const int wt = TPR == 1 ? 0 : wave >> 1;  // tile of the round
+
+    __builtin_amdgcn_sched_barrier(0);
+    stage(krsrc, kslot, koff, 3, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    stage(vrsrc, vslot, voff, 1, 0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int t = 0; t < q.CHUNKS * q.PER; ++t) asm volatile("" : "+v"(q.x[t]));
+    const int nrounds = (w.nk + TPR * BC - 1) / (TPR * BC);
+#pragma unroll 1
+    for (int c = 0; c < nrounds; ++c) {
+      const int kw0 = first_key(c);
+      const bool need_mask = kw0 + UNIT > w.open || kw0 + UNIT > w.nk;
+      const int lim = min(limit, w.nk - 1) - kw0 - 4 * g;
+      // this round's K has landed once at most the V copies behind it are outstanding
+      wait_vmcnt<LOADS>();
+      f32x16 sv[NB];
+#pragma unroll
+      for (int t = 0; t < q.CHUNKS; ++t)
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+          const i32x4 kk = *(const i32x4*)(kslot + (32 * kb + i32) * RB + (((2 * t + g) ^ kswz) << 4));
+          sv[kb] = product(kk, q, t, t == 0 ? f32x16{0.0f} : sv[kb]);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      stage(krsrc, kslot, koff, 3, c + 1);
+      settle_unit(sv);
+      if (need_mask) mask_unit(sv, lim, -INFINITY);
+      float ma, mb;
+      with_partner(unit_max(sv), ma, mb);
+      if (g == 0) mx_lds[c & 1][i32][wave] = __builtin_fmaxf(ma, mb);
+      // (the two copies of mx_lds alternate: a wave that runs ahead writes the other)
+      lds_barrier();
+      float anchor = m_seen;
+      {
+        const f32x4 x = *(const f32x4*)&mx_lds[c & 1][i32][0];
+        const float t0 = __builtin_fmaxf(x[0], x[1]), t1 = __builtin_fmaxf(x[2], x[3]);
+        m_seen = max3(m_seen, t0, t1);
+        anchor = TPR == 2 && wt == 0 ? __builtin_fmaxf(anchor, t0) : m_seen;
+      }
+      // a row that has seen no key yet keeps m = -inf, l = 0, O = 0
+      const float alpha = anchor == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m_wave - anchor) * p.c1);
+      m_wave = anchor;
+      l_part *= alpha;
+      uint32_t wpk[NB][8];
+      weigh<MODE, NB>(sv, wpk, anchor == -INFINITY ? 0.0f : anchor, p.c1, p.ck, need_mask, lim, l_part);
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) oacc[db][j] *= alpha;
+      }
+      bf16x8 pb[2 * NB];
+#pragma unroll
+      for (int ks = 0; ks < 2 * NB; ++ks) pb[ks] = p_operand<MODE>(sv[ks >> 1], wpk[ks >> 1], ks & 1);
+      wait_vmcnt<LOADS>();  // V has landed, the next round's K may be outstanding
+#pragma unroll
+      for (int db = 0; db < NDB; db += 2) add_pv<DT, D, NB>(oacc[db], oacc[db + 1], vaddr[db], vaddr[db + 1], pb);
+      stage(vrsrc, vslot, voff, 1, c + 1);
+    }
+    // every copy has landed (the last round's went to no key) and every wave is
+    // done with its slots before they are reused
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+
+    // ---- the waves' sums, each relative to its own anchor, added up: rows 0..15
+    // of every wave's O in vsm, rows 16..31 in ksm
+    {
+      float la, lb;
+      with_partner(l_part, la, lb);
+      if (g == 0) {
+        m_lds[i32][wave] = m_wave;
+        l_lds[i32][wave] = la + lb;
+      }
+    }
+    if (i32 < w.nrows) {
+      const int ri = i32 & (RHALF - 1);
+      float* red = (float*)(i32 < RHALF ? vsm : ksm) + (wave * RHALF + ri) * D;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) oacc[db][j] *= alpha;
+        for (int jq = 0; jq < 4; ++jq)
+          *(f32x4*)(red + 4 * ((8 * db + 2 * jq + g) ^ ri)) =
+              f32x4{oacc[db][4 * jq], oacc[db][4 * jq + 1], oacc[db][4 * jq + 2], oacc[db][4 * jq + 3]};
     }
-    bf16x8 pb[2 * NB];
+    lds_barrier();
 #pragma unroll
-    for (int ks = 0; ks < 2 * NB; ++ks) pb[ks] = p_operand<MODE>(sv[ks >> 1], wpk[ks >> 1], ks & 1);
-    wait_vmcnt<LOADS>();  // V has landed, the next round's K may be outstanding
+    for (int half = 0; half < 2; ++half) {
+      const int r0 = half * RHALF;
+      if (r0 >= w.nrows) break;
+      const float* red = (const float*)(half == 0 ? vsm : ksm);
 #pragma unroll
-    for (int db = 0; db < NDB; db += 2) add_pv<DT, D, NB>(oacc[db], oacc[db + 1], vaddr[db], vaddr[db + 1], pb);
-    stage(vrsrc, vslot, voff, 1, c + 1);
-  }
-  // every copy has landed (the last round's went to no key) and every wave is
-  // done with its slots before they are reused
-  __builtin_amdgcn_s_waitcnt(0);
-  __syncthreads();
-
-  // ---- the waves' sums, each relative to its own anchor, added up: rows 0..15
-  // of every wave's O in vsm, rows 16..31 in ksm
-  {
-    float la, lb;
-    with_partner(l_part, la, lb);
-    if (g == 0) {
-      m_lds[i32][wave] = m_wave;
-      l_lds[i32][wave] = la + lb;
-    }
-  }
-  if (i32 < w.nrows) {
-    const int ri = i32 & (RHALF - 1);
-    float* red = (float*)(i32 < RHALF ? vsm : ksm) + (wave * RHALF + ri) * D;
+      for (int i = 0; i < ITEMS; ++i) {
+        const int idx = i * NW * 64 + tid, rr = idx / (D / 4), ch = idx % (D / 4), r = r0 + rr;
+        if (r >= w.nrows) continue;
+        const f32x4 mw = *(const f32x4*)m_lds[r], lw = *(const f32x4*)l_lds[r];
+        float m = __builtin_fmaxf(__builtin_fmaxf(mw[0], mw[1]), __builtin_fmaxf(mw[2], mw[3]));
+        float l = 0.0f;
+        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
+        for (int x = 0; x < NW; ++x) {
+          const float f = mw[x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mw[x] - m) * p.c1);
+          l += f * lw[x];
+          const f32x4 o = *(const f32x4*)(red + (x * RHALF + rr) * D + 4 * (ch ^ rr));
 #pragma unroll
-      for (int jq = 0; jq < 4; ++jq)
-        *(f32x4*)(red + 4 * ((8 * db + 2 * jq + g) ^ ri)) =
-            f32x4{oacc[db][4 * jq], oacc[db][4 * jq + 1], oacc[db][4 * jq + 2], oacc[db][4 * jq + 3]};
-  }
-  lds_barrier();
-  for (int r0 = 0; r0 < w.nrows; r0 += RHALF) {
-    const float* red = (const float*)(r0 == 0 ? vsm : ksm);
+          for (int e = 0; e < 4; ++e) acc[e] += f * o[e];
+        }
+        if constexpr (CHAIN) {
+          if (turn == 0) {
+            held[half][i] = acc;
+            held_m[half][i] = m;
+            held_l[half][i] = l;
+            continue;
+          }
+          // (as the merge: a part with l = 0 takes no part)
+          const float l0 = held_l[half][i], m0 = l0 == 0.0f ? -INFINITY : held_m[half][i];
+          const float m1 = l == 0.0f ? -INFINITY : m;
+          const float top = __builtin_fmaxf(m0, m1);
+          const float f0 = l0 == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((m0 - top) * p.c1);
+          const float f1 = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((m1 - top) * p.c1);
+          l = f0 * l0 + f1 * l;
+          m = top;
 #pragma unroll
-    for (int i = 0; i < RHALF * (D / 4) / (NW * 64); ++i) {
-      const int idx = i * NW * 64 + tid, rr = idx / (D / 4), ch = idx % (D / 4), r = r0 + rr;
-      if (r >= w.nrows) continue;
-      const f32x4 mw = *(const f32x4*)m_lds[r], lw = *(const f32x4*)l_lds[r];
-      const float m = __builtin_fmaxf(__builtin_fmaxf(mw[0], mw[1]), __builtin_fmaxf(mw[2], mw[3]));
-      float l = 0.0f;
-      f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int x = 0; x < NW; ++x) {
-        const float f = mw[x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mw[x] - m) * p.c1);
-        l += f * lw[x];
-        const f32x4 o = *(const f32x4*)(red + (x * RHALF + rr) * D + 4 * (ch ^ rr));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] += f * o[e];
-      }
-      const size_t orow = out_row(p, w, r);
-      if (p.parts == 1) {
-        store_row4(p.o + orow * D + 4 * ch, acc, inverse(l, p.vd));
-        if (p.lse && ch == 0) p.lse[orow] = row_lse(m, l, p.c1);
-      } else {
-        const size_t at = orow * (size_t)p.parts + w.part;
-        *(f32x4*)(p.part_o + at * D + 4 * ch) = acc;
-        if (ch == 0) *(f32x2*)(p.part_ml + at * 2) = f32x2{m, l};
+          for (int e = 0; e < 4; ++e) acc[e] = f0 * held[half][i][e] + f1 * acc[e];
+        }
+        const size_t orow = out_row(p, w, r);
+        if (p.parts == 1) {
+          store_row4(p.o + orow * D + 4 * ch, acc, inverse(l, p.vd));
+          if (p.lse && ch == 0) p.lse[orow] = row_lse(m, l, p.c1);
+        } else {
+          const size_t at = orow * (size_t)p.parts + w.part;
+          *(f32x4*)(p.part_o + at * D + 4 * ch) = acc;
+          if (ch == 0) *(f32x2*)(p.part_ml + at * 2) = f32x2{m, l};
+        }
       }
     }
+    if (CHAIN && turn == 0) __syncthreads();  // the next part's copies go over the sums
   }
 }
 
@@ -521,8 +572,10 @@ __device__ __forceinline__ void place(int L, int units, int blocks, int& unit, i
   }
 }
 
-// ROWS: prefix workgroups take the rows form, else the keys form.
-template <int DT, int D, int MODE, bool ROWS>
+// FORM: how the prefix's rows are taken.
+enum { FORM_KEYS = 0, FORM_ROWS = 1, FORM_CHAIN = 2 };
+
+template <int DT, int D, int MODE, int FORM>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_prefix_kernel(
     PrefixParams p) {
   using C = PCfg<DT, D>;
@@ -533,12 +586,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __shared__ __attribute__((aligned(16))) float m_lds[32][NW], l_lds[32][NW];
   Work w;
   int unit, rb;
-  if ((int)blockIdx.x < p.p_groups) {
+  if (FORM != FORM_CHAIN && (int)blockIdx.x < p.p_groups) {
     place(blockIdx.x, p.Hkv * p.p_parts, p.p_blocks, unit, rb);
     w.h = unit / p.p_parts;
     w.part = unit - w.h * p.p_parts;
     w.b = 0;
-    w.prefix = true;
+    w.prefix = w.whole = true;
     const int j0 = w.part * p.p_split;
     w.nk = min(p.p_split, p.P - j0);
     w.open = w.nk;
@@ -547,7 +600,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const size_t at = ((size_t)w.h * (size_t)p.P_cap + (size_t)j0) * C::RB;
     w.k = p.kp + at;
     w.v = p.vp + at;
-    if constexpr (ROWS) {
+    if constexpr (FORM == FORM_ROWS) {
       rows_form<DT, D, MODE>(p, w, ksm, vsm);
       return;
     }
@@ -558,6 +611,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     w.h = bh - w.b * p.Hkv;
     w.part = p.p_parts + split;
     w.prefix = false;
+    w.whole = !p.causal;
     const int n = p.lens ? min(max(p.lens[w.b], 0), p.Sk) : p.Sk;
     const int j0 = split * p.o_split;
     // keys of this part that some row sees (the last row sees all n)
@@ -570,15 +624,24 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     w.k = p.k + at;
     w.v = p.v + at;
   }
-  if (w.nk == 0 && p.parts > 1) {
-    // nothing to read: the merge skips a part with l = 0
-    if ((int)threadIdx.x < w.nrows) {
-      const size_t at = out_row(p, w, threadIdx.x) * (size_t)p.parts + w.part;
-      *(f32x2*)(p.part_ml + at * 2) = f32x2{-INFINITY, 0.0f};
+  if constexpr (FORM == FORM_CHAIN) {
+    Work pre = w;
+    pre.whole = true;
+    pre.nk = pre.open = p.P;
+    pre.k = p.kp + (size_t)w.h * (size_t)p.P_cap * C::RB;
+    pre.v = p.vp + (size_t)w.h * (size_t)p.P_cap * C::RB;
+    keys_form<DT, D, MODE, true>(p, pre, w, ksm, vsm, mx_lds, m_lds, l_lds);
+  } else {
+    if (w.nk == 0 && p.parts > 1) {
+      // nothing to read: the merge skips a part with l = 0
+      if ((int)threadIdx.x < w.nrows) {
+        const size_t at = out_row(p, w, threadIdx.x) * (size_t)p.parts + w.part;
+        *(f32x2*)(p.part_ml + at * 2) = f32x2{-INFINITY, 0.0f};
+      }
+      return;
     }
-    return;
+    keys_form<DT, D, MODE, false>(p, w, w, ksm, vsm, mx_lds, m_lds, l_lds);
   }
-  keys_form<DT, D, MODE>(p, w, ksm, vsm, mx_lds, m_lds, l_lds);
 }
 
 // O and LSE of a row from its parts: m = max m_p, f_p = 2^(c1 (m_p - m)),
@@ -645,10 +708,10 @@ __global__ __launch_bounds__(256) void attn_prefix_merge(PrefixParams p) {
 template <int DT, int D, int MODE>
 hipError_t launch_one(const PrefixParams& p, hipStream_t st) {
   const dim3 grid((unsigned)(p.p_groups + p.o_groups));
-  if (p.p_rows == PREFIX_ROWS)
-    hipLaunchKernelGGL((attn_prefix_kernel<DT, D, MODE, true>), grid, dim3(NW * 64), 0, st, p);
-  else
-    hipLaunchKernelGGL((attn_prefix_kernel<DT, D, MODE, false>), grid, dim3(NW * 64), 0, st, p);
+  const dim3 block(NW * 64);
+  if (p.chain) hipLaunchKernelGGL((attn_prefix_kernel<DT, D, MODE, FORM_CHAIN>), grid, block, 0, st, p);
+  else if (p.p_rows == PREFIX_ROWS) hipLaunchKernelGGL((attn_prefix_kernel<DT, D, MODE, FORM_ROWS>), grid, block, 0, st, p);
+  else hipLaunchKernelGGL((attn_prefix_kernel<DT, D, MODE, FORM_KEYS>), grid, block, 0, st, p);
   return hipGetLastError();
 }
 

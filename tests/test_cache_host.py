@@ -36,7 +36,7 @@ def prefix_form(L, B, Hq, Hkv, Sq, P, Sk, p_cut=0, cut=0, causal=1):
     rc = L.attn_decode_prefix(A, A, A, A, A, None, A, None, B, Hq, Hkv, Sq, P, P, Sk, Sk, 128, causal, 0.1, 0, 0, p_cut,
                               cut, A, 1 << 40, None)
     assert rc == pkg.ATTN_ELAUNCH
-    names = ("p_parts", "o_parts", "p_rows", "p_groups", "o_groups", "p_split", "o_split", "causal")
+    names = ("p_parts", "o_parts", "p_rows", "p_groups", "o_groups", "p_split", "o_split", "causal", "chain")
     return {n: L.h15_stub_prefix(i) for i, n in enumerate(names)}
 
 
@@ -54,6 +54,20 @@ def test_prefix_forms(host):
     assert f["p_groups"] == 0 and f["o_groups"] == 2 * 2 * 3 * 3  # 96 rows a sequence: three blocks
     # one query row sees its whole cache with or without a causal mask
     assert prefix_form(host, 2, 4, 2, 1, 10, 10)["causal"] == 0 and prefix_form(host, 2, 4, 2, 2, 10, 10)["causal"] == 1
+
+
+def test_prefix_before_own_caches(host):
+    # a prefix of two rounds (of 128 BF16 keys, d = 128) in one part, own caches in one part
+    f = prefix_form(host, 8, 8, 2, 1, 256, 100)
+    assert f["chain"] == 1 and f["p_groups"] == 0 and f["o_groups"] == 8 * 2
+    assert prefix_form(host, 8, 8, 2, 1, 257, 100)["chain"] == 0
+    assert prefix_form(host, 8, 8, 2, 1, 256, 100, 128, 0)["chain"] == 0
+    assert prefix_form(host, 8, 8, 2, 1, 256, 300, 0, 128)["chain"] == 0
+    assert prefix_form(host, 8, 8, 2, 1, 256, 0)["chain"] == 0 and prefix_form(host, 8, 8, 2, 1, 0, 100)["chain"] == 0
+    # more than 512 own caches take it only with full blocks of 32 rows
+    assert prefix_form(host, 64, 32, 8, 1, 256, 100)["chain"] == 1
+    assert prefix_form(host, 65, 32, 8, 1, 256, 100)["chain"] == 0
+    assert prefix_form(host, 65, 32, 8, 8, 256, 100)["chain"] == 1
 
 
 def test_weights_runs(host):

@@ -39,7 +39,7 @@ def run_and_check(dt, d, B, Hq, Hkv, Sq, P, Sk, lens, mode, p_cut, cut, causal, 
 # batch the keys form of a prefix workgroup, beyond the rows form
 SHAPES = [
     (1, 1, 1, 1, 1, 1, None, 0, 0),                       # one key on each side
-    (3, 4, 2, 1, 200, 70, [70, 0, 33], 0, 0),             # an empty cache, two parts
+    (3, 4, 2, 1, 200, 70, [70, 0, 33], 0, 0),             # an empty cache
     (2, 4, 1, 4, 513, 300, [300, 2], 128, 256),           # fewer own keys than rows
     (4, 8, 1, 1, 640, 1, [1, 1, 0, 1], 256, 128),         # 32 rows: a full block of the keys form
     (5, 8, 1, 1, 129, 257, [257, 128, 1, 0, 200], 0, 128),  # 40 rows: two blocks of the keys form
@@ -54,6 +54,12 @@ SHAPES = [
     (43, 3, 1, 1, 1, 30, None, 0, 0),                     # 129 rows, one prefix key
     (3, 96, 1, 1, 1300, 70, [70, 0, 1], 1152, 0),         # 288 rows: three row blocks, the last with one wave
     (70, 4, 1, 1, 150, 0, None, 0, 0),                    # 280 rows, one part
+    (4, 8, 2, 1, 256, 300, [300, 0, 1, 255], 0, 0),       # a prefix of two rounds, before each own cache
+    (4, 8, 2, 2, 512, 129, [129, 0, 1, 128], 0, 0),       # two rounds, or four (BF16, d = 128): not before
+    (3, 4, 2, 1, 513, 70, [70, 0, 33], 0, 0),             # more than two rounds: two launches
+    (2, 12, 4, 16, 255, 260, [260, 17], 0, 0),            # 48 rows a sequence after the prefix
+    (260, 4, 2, 1, 130, 20, [i % 21 for i in range(260)], 0, 0),  # more than 512 own caches: two launches
+    (20, 2, 2, 40, 130, 90, [90 - 3 * i for i in range(20)], 0, 0),  # prompts after a prefix, some shorter than theirs
 ]
 
 
