@@ -113,6 +113,12 @@ int weights_run(long long heads, long long units) {
   return run < 1 ? 1 : run > 3 ? 3 : (int)run;
 }
 
+// Chunks of 16 bytes of a head's kept rows of K that the selecting workgroup
+// copies itself (times of a call so / with a second launch: 2 heads, 100 rows of 128
+// bytes 9.5 / 12.0 us; 256 rows of 256 bytes, 2 heads 9.7 / 12.0, 256 heads 18 / 20;
+// 512 rows, 2 heads 12.3 / 12.1, 320 heads 48 / 42).
+constexpr int EVICT_GATHER = 4096;
+
 struct Range {
   uintptr_t from, to;
 };
@@ -322,6 +328,7 @@ int attn_evict(const void* k, const void* v, const float* acc, const int32_t* le
   p.keep = keep;
   p.recent = recent;
   p.out_cap = out_cap;
+  p.gather = (long long)keep * (p.row_bytes / 16) <= EVICT_GATHER;
   return launch_evict(p, opts ? opts->stream : nullptr) == 0 ? ATTN_OK : ATTN_ELAUNCH;
 }
 

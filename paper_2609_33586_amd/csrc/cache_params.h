@@ -78,6 +78,7 @@ struct EvictParams {
   int32_t* index;
   int32_t* lens_out;
   int B, Hkv, Sk, Sk_cap, keep, recent, out_cap, row_bytes;
+  int gather;  // the selecting workgroup copies the rows, too: no second launch
 };
 
 // Launchers, as those of attn_params.h.  The caller has checked every argument.

@@ -27,9 +27,10 @@ using namespace h15;
 constexpr int SEL = 1024;  // threads of a selection
 constexpr int SW = SEL / 64;
 constexpr int BINS = 2048;
-constexpr int HELD = 32768;  // weights in LDS
+// Weights in LDS.  Few: two workgroups share a compute unit (a call on 320 heads,
+// 1000 keys of which 512 rows stay: 42 -> 38 us).
+constexpr int HELD_FEW = 8192, HELD_MANY = 32768;
 constexpr int STEP = 256;    // keys of a wave and step: four a lane
-constexpr int BATCH = 16;    // loads of a thread at a time
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -78,25 +79,25 @@ __device__ __forceinline__ uint32_t sum_below(const uint32_t* waves, int wave) {
   return sum;
 }
 
-__global__ __launch_bounds__(SEL) void attn_evict_select(EvictParams p) {
+// The indexes of the keys of one (batch, KV head) that stay.  HELD: weights in LDS.
+template <int HELD>
+__device__ __forceinline__ void select_keys(const EvictParams& p, int bh, int n, int32_t* index) {
   __shared__ __attribute__((aligned(16))) uint32_t ranks[HELD];
   __shared__ uint32_t hist[2][BINS];  // odd and even lanes' counts
   __shared__ uint32_t found[2];  // digits so far, keys still wanted among those that agree
   __shared__ __attribute__((aligned(16))) uint32_t above[SW], equal[SW], waves[SW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int bh = blockIdx.x, b = bh / p.Hkv;
-  const int n = p.lens ? min(max(p.lens[b], 0), p.Sk) : p.Sk;
-  int32_t* const index = p.index + (size_t)bh * p.keep;
   const float* const acc = p.acc + (size_t)bh * p.Sk_cap;
-  if (bh % p.Hkv == 0 && tid == 0) p.lens_out[b] = min(n, p.keep);
   if (n <= p.keep) {
     for (int i = tid; i < p.keep; i += SEL) index[i] = i < n ? i : -1;
     return;
   }
   const int late = n - min(p.recent, p.keep);  // the keys from here on stay
   const uint32_t want = (uint32_t)(p.keep - (n - late));
-  for (int i = late + tid; i < n; i += SEL) index[want + (uint32_t)(i - late)] = i;
-  if (want == 0) return;
+  auto put_late = [&] {
+    for (int i = late + tid; i < n; i += SEL) index[want + (uint32_t)(i - late)] = i;
+  };
+  if (want == 0) return put_late();
 
   constexpr int PER = BINS / SEL;
 #pragma unroll
@@ -105,6 +106,7 @@ __global__ __launch_bounds__(SEL) void attn_evict_select(EvictParams p) {
   // The first digits are counted as the weights come in.  (Rank 0, which no
   // weight has, up to a whole step.)
   const int held = min((late + STEP - 1) / STEP * STEP, HELD);
+  constexpr int BATCH = HELD / SEL;  // loads of a thread at a time
   for (int i0 = tid; i0 < held; i0 += BATCH * SEL) {
     float x[BATCH];
 #pragma unroll
@@ -121,9 +123,10 @@ __global__ __launch_bounds__(SEL) void attn_evict_select(EvictParams p) {
   for (int i0 = HELD + tid; i0 - lane < late; i0 += SEL)
     count(hist[lane & 1], i0 < late ? (int)(rank_of(acc[i0]) >> 21) : -1, lane);
   __syncthreads();
-  // the ranks of four keys, i a multiple of 4
+  // the ranks of this lane's four keys of the step from i (of the whole wave) on
   auto four = [&](int i) {
-    if (i < HELD) return *(const u32x4*)&ranks[i];
+    if (i < HELD) return *(const u32x4*)&ranks[i + 4 * lane];
+    i += 4 * lane;
     u32x4 u;
 #pragma unroll
     for (int e = 0; e < 4; ++e) u[e] = i + e < late ? rank_of(acc[i + e]) : 0;
@@ -136,14 +139,18 @@ __global__ __launch_bounds__(SEL) void attn_evict_select(EvictParams p) {
     if (round > 0) {
       // (whole waves: the lanes beyond the last key have no bin)
       for (int i = wave * STEP; i < late; i += SW * STEP) {
-        const u32x4 u = four(i + 4 * lane);
+        const u32x4 u = four(i);
         bool in[4], any = false;
 #pragma unroll
         for (int e = 0; e < 4; ++e) any |= in[e] = (u[e] >> (shift + width)) == digits;
-        if (!__ballot(any)) continue;
+        const unsigned long long who = __ballot(any);
+        if (!who) continue;
+        const bool few = __popcll(who) <= 16;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (__ballot(in[e])) count(hist[lane & 1], in[e] ? (int)((u[e] >> shift) & ((1u << width) - 1)) : -1, lane);
+          if (few) {
+            if (in[e]) atomicAdd(&hist[lane & 1][(u[e] >> shift) & ((1u << width) - 1)], 1u);
+          } else if (__ballot(in[e])) count(hist[lane & 1], in[e] ? (int)((u[e] >> shift) & ((1u << width) - 1)) : -1, lane);
       }
       __syncthreads();
     }
@@ -175,41 +182,75 @@ __global__ __launch_bounds__(SEL) void attn_evict_select(EvictParams p) {
   const int i0 = min(wave * stretch, late), i1 = min(i0 + stretch, late);
   uint32_t na = 0, ne = 0;
   for (int i = i0; i < i1; i += STEP) {
-    const u32x4 u = four(i + 4 * lane);
+    const u32x4 u = four(i);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      na += (uint32_t)__popcll(__ballot(u[e] > digits));
-      ne += (uint32_t)__popcll(__ballot(u[e] == digits));
+      na += u[e] > digits ? 1 : 0;
+      ne += u[e] == digits ? 1 : 0;
     }
   }
-  if (lane == 0) above[wave] = na, equal[wave] = ne;
+  na = scan(na);
+  ne = scan(ne);
+  if (lane == 63) above[wave] = na, equal[wave] = ne;
   __syncthreads();
-  // equal ones, and those that stay, in the stretches before
-  uint32_t eq = sum_below(equal, wave), at = sum_below(above, wave) + min(eq, left);
-  const unsigned long long below = (1ull << lane) - 1;
+  put_late();
+  // Above and equal ones before a key: of the equal ones the first `left` stay.
+  uint32_t ab = sum_below(above, wave), eq = sum_below(equal, wave);
   for (int i = i0; i < i1; i += STEP) {
-    const u32x4 u = four(i + 4 * lane);
-    unsigned long long es[4];
-    uint32_t before = eq;  // equal ones before this lane's
+    const u32x4 u = four(i);
+    uint32_t own = 0;  // equal ones, above ones: at most 256 each in a step
+#pragma unroll
+    for (int e = 0; e < 4; ++e) own += u[e] > digits ? 1 : u[e] == digits ? 1u << 16 : 0;
+    const uint32_t upto = scan(own), all = __builtin_amdgcn_readlane(upto, 63);
+    const uint32_t before = upto - own;
+    uint32_t e0 = eq + (before >> 16), to = ab + (before & 0xFFFF) + min(e0, left);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      es[e] = __ballot(u[e] == digits);
-      before += (uint32_t)__popcll(es[e] & below);
-      eq += (uint32_t)__popcll(es[e]);
+      const bool same = u[e] == digits;
+      if (u[e] > digits || (same && e0 < left)) index[to++] = i + 4 * lane + e;
+      e0 += same ? 1 : 0;
     }
-    bool stays[4];
-    uint32_t to = at;  // index of this lane's first key that stays
+    ab += all & 0xFFFF;
+    eq += all >> 16;
+  }
+}
+
+// GATHER: the workgroup copies the rows itself.
+template <bool GATHER, int HELD>
+__global__ __launch_bounds__(SEL) void attn_evict_select(EvictParams p) {
+  const int bh = blockIdx.x, b = bh / p.Hkv, tid = threadIdx.x;
+  const int n = p.lens ? min(max(p.lens[b], 0), p.Sk) : p.Sk;
+  int32_t* const index = p.index + (size_t)bh * p.keep;
+  if (bh % p.Hkv == 0 && tid == 0) p.lens_out[b] = min(n, p.keep);
+  select_keys<HELD>(p, bh, n, index);
+  if constexpr (GATHER) {
+    __syncthreads();
+    constexpr int U = 4;
+    const int chunks = p.row_bytes / 16, shift = __builtin_ctz(chunks);
+    const int items = min(n, p.keep) * chunks;
+    const size_t from = (size_t)bh * p.Sk_cap, to = (size_t)bh * p.out_cap;
+    const uint8_t* const k = p.k + from * p.row_bytes;
+    const uint8_t* const v = p.v + from * p.row_bytes;
+    for (int i0 = tid; i0 < items; i0 += U * SEL) {
+      int src[U];
+      u32x4 x[U], y[U];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      stays[e] = u[e] > digits || (u[e] == digits && before < left);
-      before += u[e] == digits ? 1 : 0;
-      const unsigned long long ss = __ballot(stays[e]);
-      to += (uint32_t)__popcll(ss & below);
-      at += (uint32_t)__popcll(ss);
+      for (int j = 0; j < U; ++j) src[j] = index[min(i0 + j * SEL, items - 1) >> shift];
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int c = (i0 + j * SEL) & (chunks - 1);
+        x[j] = *(const u32x4*)(k + (size_t)src[j] * p.row_bytes + 16 * c);
+        y[j] = *(const u32x4*)(v + (size_t)src[j] * p.row_bytes + 16 * c);
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int i = i0 + j * SEL;
+        if (i >= items) break;
+        *(u32x4*)(p.k_out + to * p.row_bytes + 16 * (size_t)i) = x[j];
+        *(u32x4*)(p.v_out + to * p.row_bytes + 16 * (size_t)i) = y[j];
+        if ((i & (chunks - 1)) == 0) p.acc_out[to + (i >> shift)] = p.acc[from + src[j]];
+      }
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (stays[e]) index[to++] = i + 4 * lane + e;
   }
 }
 
@@ -235,9 +276,17 @@ namespace h15 {
 
 int launch_evict(const EvictParams& p, void* stream) {
   hipStream_t st = (hipStream_t)stream;
-  hipLaunchKernelGGL(attn_evict_select, dim3((unsigned)(p.B * p.Hkv)), dim3(SEL), 0, st, p);
+  const dim3 heads((unsigned)(p.B * p.Hkv)), block(SEL);
+  // (two workgroups a compute unit where their weights fit)
+  if (p.Sk <= HELD_FEW) {
+    if (p.gather) hipLaunchKernelGGL((attn_evict_select<true, HELD_FEW>), heads, block, 0, st, p);
+    else hipLaunchKernelGGL((attn_evict_select<false, HELD_FEW>), heads, block, 0, st, p);
+  } else {
+    if (p.gather) hipLaunchKernelGGL((attn_evict_select<true, HELD_MANY>), heads, block, 0, st, p);
+    else hipLaunchKernelGGL((attn_evict_select<false, HELD_MANY>), heads, block, 0, st, p);
+  }
   hipError_t e = hipGetLastError();
-  if (e == hipSuccess) {
+  if (e == hipSuccess && !p.gather) {
     const long long threads = (long long)p.B * p.Hkv * p.keep * (p.row_bytes / 16);
     hipLaunchKernelGGL(attn_evict_gather, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, p);
     e = hipGetLastError();
