@@ -139,15 +139,21 @@ size_t attn_key_weights_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Sk, 
  * [B][Hkv][keep] int32; lens_out: [B] int32.  opts may be NULL; only its
  * stream is used.
  *
+ * workspace: attn_evict_workspace_bytes() bytes, 16-byte aligned, for long
+ * caches (may be NULL where that is 0).
+ *
  * Errors: ATTN_EINVAL for a null pointer (lens may be), a size that is not
  * positive, Sk > Sk_cap, keep < 1 or > out_cap, recent < 0, or an output that
- * overlaps an input or another output; ATTN_EUNSUPPORTED for d not in
+ * overlaps an input, the workspace or another output; ATTN_EUNSUPPORTED for d not in
  * {64, 128}, an unknown dtype, k, v, k_out or v_out not 16-byte aligned (the
  * others: 4), B * Hkv beyond 2^22 - 1, or more than 2^32 - 256 chunks of 16
  * bytes in the rows of K that may stay. */
 int attn_evict(const void* k, const void* v, const float* acc, const int32_t* lens, void* k_out, void* v_out,
                float* acc_out, int32_t* index, int32_t* lens_out, int B, int Hkv, int Sk, int Sk_cap, int out_cap,
-               int d, int keep, int recent, int dtype, const attn_opts* opts);
+               int d, int keep, int recent, int dtype, void* workspace, size_t workspace_bytes,
+               const attn_opts* opts);
+
+size_t attn_evict_workspace_bytes(int B, int Hkv, int Sk);
 
 #ifdef __cplusplus
 }

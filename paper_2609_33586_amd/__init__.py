@@ -316,4 +316,4 @@ def attn_decode_probe(q, k, v, *, causal: bool, scale: float, exp_mode: int, spl
 # ---- shared and bounded caches (include/h15cache.h) -------------------------
 
 from .cache import (attn_decode_prefix, attn_decode_prefix_split_keys, attn_decode_prefix_workspace_bytes,  # noqa: E402
-                    attn_evict, attn_key_weights, attn_key_weights_workspace_bytes)
+                    attn_evict, attn_evict_workspace_bytes, attn_key_weights, attn_key_weights_workspace_bytes)

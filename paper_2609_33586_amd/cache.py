@@ -12,7 +12,7 @@ from . import ATTN_OK, AttnError, _dtype_of, _opts, _outputs, attn_opts, lib
 
 # every symbol h15cache.h declares
 EXPORTS = ("attn_decode_prefix", "attn_decode_prefix_workspace_bytes", "attn_decode_prefix_split_keys",
-           "attn_key_weights", "attn_key_weights_workspace_bytes", "attn_evict")
+           "attn_key_weights", "attn_key_weights_workspace_bytes", "attn_evict", "attn_evict_workspace_bytes")
 
 _bound = None
 _device = None  # the number of the current device
@@ -34,7 +34,8 @@ def _lib() -> ctypes.CDLL:
             ("attn_decode_prefix_split_keys", [I] * 8 + [IP, IP], I),
             ("attn_key_weights", [P] * 5 + [I] * 8 + [F, F, I, P, S, O], I),
             ("attn_key_weights_workspace_bytes", [I] * 6, S),
-            ("attn_evict", [P] * 9 + [I] * 9 + [O], I)):
+            ("attn_evict", [P] * 9 + [I] * 9 + [P, S, O], I),
+            ("attn_evict_workspace_bytes", [I] * 3, S)):
         fn = getattr(L, name)
         fn.argtypes, fn.restype = args, res
     import torch
@@ -189,8 +190,12 @@ def attn_key_weights(q, k, lse, acc, *, causal: bool, scale: float, decay: float
     return acc
 
 
+def attn_evict_workspace_bytes(B: int, Hkv: int, Sk: int) -> int:
+    return int(_lib().attn_evict_workspace_bytes(int(B), int(Hkv), int(Sk)))
+
+
 def attn_evict(k, v, acc, *, keep: int, recent: int, lens=None, Sk: int | None = None, stream=None, k_out=None,
-               v_out=None, acc_out=None, index=None, lens_out=None):
+               v_out=None, acc_out=None, index=None, lens_out=None, workspace=None):
     """Keep min(lens[b], keep) keys of every cache, the last `recent` and those with the largest acc (see
     include/h15cache.h, attn_evict).
 
@@ -218,10 +223,11 @@ def attn_evict(k, v, acc, *, keep: int, recent: int, lens=None, Sk: int | None =
     shape = (B, Hkv, rows)
     index = new(shape, i32) if index is None else _tensor("index", index, shape, dev, i32)
     lens_out = new((B,), i32) if lens_out is None else _tensor("lens_out", lens_out, (B,), dev, i32)
+    wptr, wbytes, workspace = _space(workspace, lambda: L.attn_evict_workspace_bytes(B, Hkv, Sk), dev, stream)
     opts = _opts(None, stream)
     rc = L.attn_evict(k.data_ptr(), v.data_ptr(), acc.data_ptr(), _lens_ptr(lens, B, dev), k_out.data_ptr(),
                       v_out.data_ptr(), acc_out.data_ptr(), index.data_ptr(), lens_out.data_ptr(), B, Hkv, Sk, cap,
-                      out_cap, d, keep, int(recent), dt, ctypes.byref(opts))
+                      out_cap, d, keep, int(recent), dt, wptr, wbytes, ctypes.byref(opts))
     if rc != ATTN_OK:
         raise AttnError(rc, "attn_evict")
     return k_out, v_out, acc_out, index, lens_out

@@ -119,6 +119,16 @@ int weights_run(long long heads, long long units) {
 // 512 rows, 2 heads 12.3 / 12.1, 320 heads 48 / 42).
 constexpr int EVICT_GATHER = 4096;
 
+// Workgroups that select for one head: a single one, unless few heads have long
+// caches (of which it holds eight parts in LDS).  Times of a call with one / with a
+// workgroup a part, 256 FP8 rows of d = 64 staying: 8 heads, 16K keys 16 / 18 us, 25K
+// 20 / 19, 32K 23 / 19, 100K 99 / 21; 64 heads, 32K 24 / 25, 50K 51 / 40; 128 heads,
+// 50K 53 / 65; 256 heads 58 / 130.
+int evict_parts(long long heads, int Sk) {
+  if (Sk <= 5 * EVICT_PART || heads > (Sk > 8 * EVICT_PART ? 64 : 32)) return 1;
+  return (int)ceil_div(Sk, EVICT_PART);
+}
+
 struct Range {
   uintptr_t from, to;
 };
@@ -282,14 +292,22 @@ int attn_key_weights(const void* q, const void* k, const float* lse, const int32
   return launch_weights(p, dtype, d, opts ? opts->stream : nullptr) == 0 ? ATTN_OK : ATTN_ELAUNCH;
 }
 
+size_t attn_evict_workspace_bytes(int B, int Hkv, int Sk) {
+  if (B <= 0 || Hkv <= 0 || Sk <= 0) return 0;
+  const long long heads = (long long)B * Hkv;
+  const int parts = evict_parts(heads, Sk);
+  return parts == 1 ? 0 : (size_t)heads * parts * EVICT_PART_BYTES;
+}
+
 int attn_evict(const void* k, const void* v, const float* acc, const int32_t* lens, void* k_out, void* v_out,
                float* acc_out, int32_t* index, int32_t* lens_out, int B, int Hkv, int Sk, int Sk_cap, int out_cap,
-               int d, int keep, int recent, int dtype, const attn_opts* opts) {
+               int d, int keep, int recent, int dtype, void* workspace, size_t workspace_bytes,
+               const attn_opts* opts) {
   if (!k || !v || !acc || !k_out || !v_out || !acc_out || !index || !lens_out) return ATTN_EINVAL;
   if (B <= 0 || Hkv <= 0 || Sk <= 0 || Sk_cap <= 0 || out_cap <= 0 || d <= 0 || keep <= 0) return ATTN_EINVAL;
   if (Sk > Sk_cap || keep > out_cap || recent < 0) return ATTN_EINVAL;
   if (dtype != ATTN_BF16 && dtype != ATTN_FP8_E4M3) return ATTN_EUNSUPPORTED;
-  if (d != 64 && d != 128) return ATTN_EUNSUPPORTED;
+  if ((d != 64 && d != 128) || Sk > INT32_MAX - 2 * EVICT_PART) return ATTN_EUNSUPPORTED;
   if (misaligned(k, 16) || misaligned(v, 16) || misaligned(k_out, 16) || misaligned(v_out, 16))
     return ATTN_EUNSUPPORTED;
   if (misaligned(acc, 4) || misaligned(lens, 4) || misaligned(acc_out, 4) || misaligned(index, 4) ||
@@ -328,7 +346,19 @@ int attn_evict(const void* k, const void* v, const float* acc, const int32_t* le
   p.keep = keep;
   p.recent = recent;
   p.out_cap = out_cap;
-  p.gather = (long long)keep * (p.row_bytes / 16) <= EVICT_GATHER;
+  p.parts = evict_parts((long long)heads, Sk);
+  p.gather = p.parts == 1 && (long long)keep * (p.row_bytes / 16) <= EVICT_GATHER;
+  if ((long long)heads * p.parts > MAX_GROUPS / 4) return ATTN_EUNSUPPORTED;
+  if (p.parts > 1) {
+    const size_t need = heads * p.parts * EVICT_PART_BYTES;
+    if (!workspace || misaligned(workspace, 16) || workspace_bytes < need) return ATTN_EINVAL;
+    p.scratch = (uint8_t*)workspace;
+    const Range ws = range(workspace, need);
+    for (const Range& x : in)
+      if (overlap(ws, x)) return ATTN_EINVAL;
+    for (const Range& x : out)
+      if (overlap(ws, x)) return ATTN_EINVAL;
+  }
   return launch_evict(p, opts ? opts->stream : nullptr) == 0 ? ATTN_OK : ATTN_ELAUNCH;
 }
 

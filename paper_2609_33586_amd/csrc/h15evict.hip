@@ -1,9 +1,11 @@
 // Which keys of a cache stay (attn_evict): of the n keys of each (batch, KV
 // head) the last `recent` and, of the others, those with the largest
 // accumulated weight, `keep` in all (equal weights: the lowest index first),
-// in their order.  Two launches: one workgroup a (batch, KV head) finds them
-// and writes their indexes; then their rows of K, V and acc are gathered into
-// the compact caches, 16 bytes a thread.
+// in their order.  One workgroup a (batch, KV head) finds them and writes their
+// indexes; then their rows of K, V and acc are gathered into the compact caches,
+// 16 bytes a thread, by that workgroup if they are few, else by a launch of their
+// own.  Where few heads have long caches, parts of the keys have a workgroup each,
+// in three launches.  (The rules: cache_api.cpp.)
 //
 // The selection is a radix search for the weight of rank keep - recent in three
 // rounds over 11, 11 and 10 bits, each a histogram in LDS of the keys that agree
@@ -12,9 +14,15 @@
 // are read once, as ordered numbers into LDS (of a cache of more than 32K keys
 // every pass reads the rest again).  (In registers, 32 a thread, the passes had
 // to be unrolled, and a workgroup spent its time fetching code that it runs once:
-// 41 us for 32K keys; re-read from memory in every pass 53 us.)  What bounds the
-// call is the gather (read and written once) and, with few caches, the passes'
-// latency.
+// 41 us for 32K keys; re-read from memory in every pass 53 us.)
+//
+// What bounds it: the gather (read and written once: 32 caches of 8 heads, 4096 of
+// 5000 FP8 rows, 75 us at 5.4 TB/s after 9 of the selection); with few caches the
+// passes' latency.  A selection of 300 keys takes 7.5 us, the copy of 100 rows
+// included; of 32K keys by one workgroup 25 us: 6 for the first digits, whose
+// counts in LDS follow each other where weights are equal, 4 and 1.3 for the others,
+// 5 for the indexes, each instruction a key taking 0.25 us of a compute unit; in
+// parts 5 + 5 + 7 us, and 4 for the gather.
 #include "cache_params.h"
 
 #include <hip/hip_runtime.h>
@@ -79,13 +87,39 @@ __device__ __forceinline__ uint32_t sum_below(const uint32_t* waves, int wave) {
   return sum;
 }
 
+// The bin from the top in which a count passes `left`: c[j] is the count of this
+// thread's bin BINS - 1 - (PER tid + j).  Makes it the next digits, and `left`
+// what is still wanted of it.
+constexpr int PER = BINS / SEL;
+struct Search {
+  uint32_t waves[SW];
+  uint32_t found[2];  // digits so far, keys still wanted among those that agree
+};
+__device__ __forceinline__ void next_digits(Search& sh, const uint32_t (&c)[PER], int width, uint32_t& digits,
+                                            uint32_t& left, int tid, int lane, int wave) {
+  static_assert(PER == 2, "two bins a thread");
+  const uint32_t own = c[0] + c[1];
+  const uint32_t upto = scan(own);
+  if (lane == 63) sh.waves[wave] = upto;
+  __syncthreads();
+  const uint32_t before = upto - own + sum_below(sh.waves, wave);
+  if (before < left && before + own >= left) {
+    const bool second = before + c[0] < left;
+    sh.found[0] = (digits << width) | (uint32_t)(BINS - 1 - (PER * tid + (second ? 1 : 0)));
+    sh.found[1] = left - before - (second ? c[0] : 0);
+  }
+  __syncthreads();
+  digits = sh.found[0];
+  left = sh.found[1];
+}
+
 // The indexes of the keys of one (batch, KV head) that stay.  HELD: weights in LDS.
 template <int HELD>
 __device__ __forceinline__ void select_keys(const EvictParams& p, int bh, int n, int32_t* index) {
   __shared__ __attribute__((aligned(16))) uint32_t ranks[HELD];
   __shared__ uint32_t hist[2][BINS];  // odd and even lanes' counts
-  __shared__ uint32_t found[2];  // digits so far, keys still wanted among those that agree
-  __shared__ __attribute__((aligned(16))) uint32_t above[SW], equal[SW], waves[SW];
+  __shared__ __attribute__((aligned(16))) Search search;
+  __shared__ __attribute__((aligned(16))) uint32_t above[SW], equal[SW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const float* const acc = p.acc + (size_t)bh * p.Sk_cap;
   if (n <= p.keep) {
@@ -99,7 +133,6 @@ __device__ __forceinline__ void select_keys(const EvictParams& p, int bh, int n,
   };
   if (want == 0) return put_late();
 
-  constexpr int PER = BINS / SEL;
 #pragma unroll
   for (int i = 0; i < 2 * PER; ++i) hist[0][i * SEL + tid] = 0;
   __syncthreads();
@@ -154,27 +187,14 @@ __device__ __forceinline__ void select_keys(const EvictParams& p, int bh, int n,
       }
       __syncthreads();
     }
-    // a thread: two bins, from the top; the bin in which the count passes `left`
-    uint32_t c[PER], own = 0;
+    uint32_t c[PER];
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const int bin = BINS - 1 - (PER * tid + j);
       c[j] = hist[0][bin] + hist[1][bin];
       hist[0][bin] = hist[1][bin] = 0;  // for the next round
-      own += c[j];
     }
-    const uint32_t upto = scan(own);
-    if (lane == 63) waves[wave] = upto;
-    __syncthreads();
-    const uint32_t before = upto - own + sum_below(waves, wave);
-    if (before < left && before + own >= left) {
-      const bool second = before + c[0] < left;
-      found[0] = (digits << width) | (uint32_t)(BINS - 1 - (PER * tid + (second ? 1 : 0)));
-      found[1] = left - before - (second ? c[0] : 0);
-    }
-    __syncthreads();
-    digits = found[0];
-    left = found[1];
+    next_digits(search, c, width, digits, left, tid, lane, wave);
   }
   // now: all keys above `digits` stay, and the first `left` of those equal to it.
   // Each wave has a stretch of the keys before `late`, in order.
@@ -212,6 +232,181 @@ __device__ __forceinline__ void select_keys(const EvictParams& p, int bh, int n,
     }
     ab += all & 0xFFFF;
     eq += all >> 16;
+  }
+}
+
+// The same by EVICT_PART keys a workgroup, in three launches: the first digits of
+// every part's weights are counted; every workgroup adds up its head's counts and
+// writes down its part's candidates, the keys with the digits found; every
+// workgroup finds the remaining digits from its head's candidates, and places its
+// own part's keys, those of the parts before it being counted from their
+// candidates.  What the launches hand on, for each part:
+struct Part {
+  uint32_t counts[BINS / 2];     // of two bins, the even one's low
+  uint32_t above, candidates;    // keys with higher first digits, and with these
+  uint32_t rest[EVICT_PART];     // the candidates' remaining digits, in order of the keys
+  uint32_t digits, left;         // the first digits, what is wanted of the head's candidates
+};
+static_assert(sizeof(Part) == EVICT_PART_BYTES, "the workspace is sized by it");
+
+struct Place {  // of a workgroup
+  int bh, part, n, late;
+  uint32_t want;
+  Part* parts;  // of its head
+};
+
+// False where nothing is to be sought: all keys stay, or only the late ones.
+__device__ __forceinline__ bool place(const EvictParams& p, Place& w) {
+  w.bh = blockIdx.x / p.parts;
+  w.part = blockIdx.x - w.bh * p.parts;
+  w.n = p.lens ? min(max(p.lens[w.bh / p.Hkv], 0), p.Sk) : p.Sk;
+  w.late = w.n - min(p.recent, p.keep);
+  w.want = (uint32_t)(p.keep - (w.n - w.late));
+  w.parts = (Part*)p.scratch + (size_t)w.bh * p.parts;
+  return w.n > p.keep && w.want > 0;
+}
+
+// The ranks of four keys from i on, 0 from `late` on
+__device__ __forceinline__ u32x4 ranks_of(const float* acc, int i, int late) {
+  float x[4];
+  u32x4 u;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = acc[min(i + e, late - 1)];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) u[e] = i + e < late ? rank_of(x[e]) : 0;
+  return u;
+}
+
+__global__ __launch_bounds__(SEL) void attn_evict_count(EvictParams p) {
+  __shared__ uint32_t hist[2][BINS];
+  const int tid = threadIdx.x, lane = tid & 63;
+  Place w;
+  if (!place(p, w) || w.part * EVICT_PART >= w.late) return;
+  const u32x4 u = ranks_of(p.acc + (size_t)w.bh * p.Sk_cap, w.part * EVICT_PART + 4 * tid, w.late);
+#pragma unroll
+  for (int i = 0; i < 2 * PER; ++i) hist[0][i * SEL + tid] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < 4; ++e) count(hist[lane & 1], u[e] != 0 ? (int)(u[e] >> 21) : -1, lane);
+  __syncthreads();
+  w.parts[w.part].counts[tid] =
+      (hist[0][2 * tid] + hist[1][2 * tid]) | (hist[0][2 * tid + 1] + hist[1][2 * tid + 1]) << 16;
+}
+
+__global__ __launch_bounds__(SEL) void attn_evict_narrow(EvictParams p) {
+  __shared__ __attribute__((aligned(16))) Search search;
+  __shared__ __attribute__((aligned(16))) uint32_t waves[SW];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Place w;
+  if (!place(p, w) || w.part * EVICT_PART >= w.late) return;
+  const u32x4 u = ranks_of(p.acc + (size_t)w.bh * p.Sk_cap, w.part * EVICT_PART + 4 * tid, w.late);
+  // the head's counts
+  const int used = (w.late + EVICT_PART - 1) / EVICT_PART;
+  uint32_t c[PER] = {0, 0};
+#pragma unroll 8
+  for (int i = 0; i < used; ++i) {
+    const uint32_t x = w.parts[i].counts[SEL - 1 - tid];
+    c[0] += x >> 16;
+    c[1] += x & 0xFFFF;
+  }
+  uint32_t digits = 0, left = w.want;
+  next_digits(search, c, 11, digits, left, tid, lane, wave);
+  uint32_t own = 0;  // candidates, above ones: EVICT_PART each at most
+#pragma unroll
+  for (int e = 0; e < 4; ++e) own += (u[e] >> 21) > digits ? 1 : (u[e] >> 21) == digits ? 1u << 16 : 0;
+  const uint32_t upto = scan(own);
+  if (lane == 63) waves[wave] = upto;
+  __syncthreads();
+  const uint32_t before = upto - own + sum_below(waves, wave);
+  Part& part = w.parts[w.part];
+  uint32_t at = before >> 16;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if ((u[e] >> 21) == digits) part.rest[at++] = u[e] & ((1u << 21) - 1);
+  if (tid == SEL - 1) {
+    part.above = (before + own) & 0xFFFF;
+    part.candidates = (before + own) >> 16;
+    part.digits = digits;
+    part.left = left;
+  }
+}
+
+__global__ __launch_bounds__(SEL) void attn_evict_place(EvictParams p) {
+  __shared__ uint32_t hist[2][BINS];
+  __shared__ __attribute__((aligned(16))) Search search;
+  __shared__ __attribute__((aligned(16))) uint32_t above[SW], equal[SW], waves[SW];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Place w;
+  const bool seek = place(p, w);
+  int32_t* const index = p.index + (size_t)w.bh * p.keep;
+  if (w.bh % p.Hkv == 0 && w.part == 0 && tid == 0) p.lens_out[w.bh / p.Hkv] = min(w.n, p.keep);
+  const int first = w.part * SEL + tid, step = p.parts * SEL;
+  if (w.n <= p.keep) {
+    for (int i = first; i < p.keep; i += step) index[i] = i < w.n ? i : -1;
+    return;
+  }
+  for (int i = w.late + first; i < w.n; i += step) index[w.want + (uint32_t)(i - w.late)] = i;
+  if (!seek || w.part * EVICT_PART >= w.late) return;
+  const int k0 = w.part * EVICT_PART + 4 * tid;
+  const u32x4 u = ranks_of(p.acc + (size_t)w.bh * p.Sk_cap, k0, w.late);
+#pragma unroll
+  for (int i = 0; i < 2 * PER; ++i) hist[0][i * SEL + tid] = 0;
+  __syncthreads();
+  const uint32_t top = w.parts[w.part].digits;
+  uint32_t digits = 0, left = w.parts[w.part].left;
+  // (a wave: the candidates of every SW-th part)
+  const int used = (w.late + EVICT_PART - 1) / EVICT_PART;
+#pragma unroll 1
+  for (int round = 1; round < 3; ++round) {
+    const int shift = round == 1 ? 10 : 0, width = round == 1 ? 11 : 10;
+    for (int i = wave; i < used; i += SW) {
+      const Part& part = w.parts[i];
+      const int m = (int)part.candidates;
+      for (int j = lane; j - lane < m; j += 64) {
+        const uint32_t r = j < m ? part.rest[j] : ~0u;  // (no digits are that high)
+        const bool in = j < m && (round == 1 || r >> width == digits);
+        if (__ballot(in)) count(hist[lane & 1], in ? (int)((r >> shift) & ((1u << width) - 1)) : -1, lane);
+      }
+    }
+    __syncthreads();
+    uint32_t c[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int bin = BINS - 1 - (PER * tid + j);
+      c[j] = hist[0][bin] + hist[1][bin];
+      hist[0][bin] = hist[1][bin] = 0;
+    }
+    next_digits(search, c, width, digits, left, tid, lane, wave);
+  }
+  // above and equal ones in the parts before this one
+  uint32_t na = 0, ne = 0;
+  for (int i = wave; i < w.part; i += SW) {
+    const Part& part = w.parts[i];
+    const int m = (int)part.candidates;
+    if (lane == 0) na += part.above;
+    for (int j = lane; j < m; j += 64) {
+      const uint32_t r = part.rest[j];
+      na += r > digits ? 1 : 0;
+      ne += r == digits ? 1 : 0;
+    }
+  }
+  na = scan(na);
+  ne = scan(ne);
+  digits |= top << 21;
+  uint32_t own = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) own += u[e] > digits ? 1 : u[e] == digits ? 1u << 16 : 0;
+  const uint32_t upto = scan(own);
+  if (lane == 63) above[wave] = na, equal[wave] = ne, waves[wave] = upto;
+  __syncthreads();
+  const uint32_t before = upto - own + sum_below(waves, wave);
+  uint32_t e0 = sum_below(equal, SW) + (before >> 16);
+  uint32_t to = sum_below(above, SW) + (before & 0xFFFF) + min(e0, left);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const bool same = u[e] == digits;
+    if (u[e] > digits || (same && e0 < left)) index[to++] = k0 + e;
+    e0 += same ? 1 : 0;
   }
 }
 
@@ -278,7 +473,12 @@ int launch_evict(const EvictParams& p, void* stream) {
   hipStream_t st = (hipStream_t)stream;
   const dim3 heads((unsigned)(p.B * p.Hkv)), block(SEL);
   // (two workgroups a compute unit where their weights fit)
-  if (p.Sk <= HELD_FEW) {
+  if (p.parts > 1) {
+    const dim3 all((unsigned)(p.B * p.Hkv * p.parts));
+    hipLaunchKernelGGL(attn_evict_count, all, block, 0, st, p);
+    hipLaunchKernelGGL(attn_evict_narrow, all, block, 0, st, p);
+    hipLaunchKernelGGL(attn_evict_place, all, block, 0, st, p);
+  } else if (p.Sk <= HELD_FEW) {
     if (p.gather) hipLaunchKernelGGL((attn_evict_select<true, HELD_FEW>), heads, block, 0, st, p);
     else hipLaunchKernelGGL((attn_evict_select<false, HELD_FEW>), heads, block, 0, st, p);
   } else {

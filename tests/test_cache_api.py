@@ -101,9 +101,11 @@ def spread(n):
     return [0x100000 + (i << 46) for i in range(n)]
 
 
-def evict(L, at=None, lens=None, B=2, Hkv=2, Sk=300, cap=320, out_cap=128, d=128, keep=100, recent=10, dtype=0):
+def evict(L, at=None, lens=None, B=2, Hkv=2, Sk=300, cap=320, out_cap=128, d=128, keep=100, recent=10, dtype=0,
+          ws=None, wsb=0):
     k, v, acc, ko, vo, ao, ix, lo = at or spread(8)
-    return L.attn_evict(k, v, acc, lens, ko, vo, ao, ix, lo, B, Hkv, Sk, cap, out_cap, d, keep, recent, dtype, None)
+    return L.attn_evict(k, v, acc, lens, ko, vo, ao, ix, lo, B, Hkv, Sk, cap, out_cap, d, keep, recent, dtype, ws, wsb,
+                        None)
 
 
 def test_evict_refusals(L):
@@ -130,6 +132,21 @@ def test_evict_refusals(L):
     assert evict(L, at) == INV
     at = spread(8)
     assert evict(L, at, lens=at[7]) == INV  # new lens over the old ones
+    big = (1 << 31) - 1
+    assert evict(L, Sk=big, cap=big, ws=FAKE, wsb=1 << 60) == UNS
+    assert evict(L, Sk=big, cap=big, keep=big, out_cap=big) == UNS
+
+
+def test_evict_workspace(L):
+    need = pkg.attn_evict_workspace_bytes(2, 2, 40000)
+    assert need > 0 and need % 16 == 0 and pkg.attn_evict_workspace_bytes(2, 2, 300) == 0
+    assert pkg.attn_evict_workspace_bytes(0, 2, 40000) == pkg.attn_evict_workspace_bytes(2, 2, 0) == 0
+    at = spread(9)
+    for ws, wsb in ((None, need), (at[8], need - 1), (at[8] + 8, need)):
+        assert evict(L, at[:8], Sk=40000, cap=40000, ws=ws, wsb=wsb) == INV
+    for i in range(8):
+        assert evict(L, at[:8], Sk=40000, cap=40000, ws=at[i], wsb=need) == INV, i
+    assert evict(L, at[:8], lens=at[8] + need - 4, Sk=40000, cap=40000, ws=at[8], wsb=need) == INV
 
 
 def test_binding_refuses_host_tensors():

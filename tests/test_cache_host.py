@@ -29,6 +29,8 @@ def host(tmp_path_factory):
     P, I, F, S = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
     L.attn_decode_prefix.argtypes = [P] * 8 + [I] * 10 + [F] + [I] * 4 + [P, S, P]
     L.attn_key_weights.argtypes = [P] * 5 + [I] * 8 + [F, F, I, P, S, P]
+    L.attn_evict.argtypes = [P] * 9 + [I] * 9 + [P, S, P]
+    L.attn_evict_workspace_bytes.restype = S
     return L
 
 
@@ -87,6 +89,21 @@ def test_weights_runs(host):
     assert form(16, 1, 32, 257) == {"heads": 16, "hrows": 32, "parts": 1, "blocks": 2, "causal": 1}
     assert form(8, 2, 512, 512)["parts"] == 1 and form(8, 2, 513, 512)["parts"] == 2
     assert form(64, 1, 65, 512)["parts"] == 2  # more heads than tiles: one tile of each
+
+
+def test_evict_forms(host):
+    def form(B, Hkv, Sk, keep, d=128):
+        at = [0x100000 + (i << 46) for i in range(9)]
+        rc = host.attn_evict(at[0], at[1], at[2], None, *at[3:8], B, Hkv, Sk, Sk, keep, d, keep, 0, 0, at[8],
+                             host.attn_evict_workspace_bytes(B, Hkv, Sk), None)
+        assert rc == pkg.ATTN_ELAUNCH
+        return host.h15_stub_evict(0), host.h15_stub_evict(1)
+
+    # (parts of 4096 keys, whether the selecting workgroup copies the rows: up to 4096 chunks of 16 bytes)
+    assert form(1, 2, 300, 100) == (1, 1) and form(1, 2, 300, 256) == (1, 1) and form(1, 2, 300, 257) == (1, 0)
+    assert form(1, 2, 5 * 4096, 100) == (1, 1) and form(1, 2, 5 * 4096 + 1, 100) == (6, 0)
+    assert form(4, 8, 32768, 1000) == (8, 0) and form(11, 3, 32768, 1000) == (1, 0)
+    assert form(8, 8, 32769, 100) == (9, 0) and form(13, 5, 32769, 100) == (1, 1)
 
 
 def test_checks_under_sanitizers(tmp_path):

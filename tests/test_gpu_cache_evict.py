@@ -60,6 +60,68 @@ def test_caches_beyond_what_lds_holds(n, keep, recent):
     check(k, v, torch.floor(acc), [n, n - 200], keep, recent)  # many equal ones
 
 
+def test_many_caches_beyond_what_lds_holds():
+    k, v, acc = caches(FP8, 35, 2, 33024, 64, 70)  # one workgroup for each
+    lens = [33024 - 700 * (b % 7) for b in range(35)]
+    check(k, v, acc, lens, 500, 17)
+    check(k, v, torch.floor(acc), lens, 33000, 0)
+
+
+def test_more_heads_than_compute_units():
+    k, v, acc = caches(BF16, 75, 4, 500, 64, 80)
+    for keep in (90, 400):  # rows copied by the selecting workgroup, and by others
+        check(k, v, torch.floor(acc), [500 - 6 * b for b in range(75)], keep, 30)
+
+
+# (lens, keep, recent) for caches of 30000 keys that eight workgroups share
+PARTS = [([30000, 29999, 4096], 1000, 100), ([4097, 4095, 12289], 4096, 0), ([0, 1, 30000], 1, 0), ([20000, 8192, 8193], 8192, 9000),
+         ([30000, 20481, 50], 20480, 20479), ([30000, 24577, 12288], 12288, 1)]
+
+
+@pytest.mark.parametrize("dt,d", [(BF16, 64), (FP8, 128)])
+@pytest.mark.parametrize("lens,keep,recent", PARTS)
+def test_parts_of_ragged_caches(lens, keep, recent, dt, d):
+    k, v, acc = caches(dt, 3, 2, 30100, d, 90)
+    for a in (acc, torch.floor(acc), torch.full_like(acc, 0.5), acc.sort(dim=-1)[0], acc.sort(dim=-1, descending=True)[0]):
+        say(f"evict parts lens={lens} keep={keep} recent={recent} {dt}")
+        check(k, v, a, lens, keep, recent, Sk=30000, out_cap=keep + 3)
+
+
+def test_parts_with_signs_infinities_and_nan():
+    k, v, acc = caches(FP8, 1, 1, 25000, 64, 95)
+    a = 1.0 - acc
+    a[..., ::3], a[..., 1::50] = math.inf, -math.inf
+    a[..., 7::110] = math.nan
+    a.view(torch.int32)[..., 9::1100] = -1  # NaN with its sign set
+    a[..., 4::9], a[..., 5::9] = 0.0, -0.0
+    for keep in (1, 250, 251, 8000, 12000, 24999):
+        check(k, v, a, None, keep, 0)
+    close = (1.0 + torch.arange(25000, device="cuda").float().flip(0) % 97 * 2.0 ** -23).view(1, 1, -1)
+    check(k, v, close, None, 5000, 3)
+
+
+def test_parts_stay_within_their_workspace_and_replay():
+    k, v, acc = caches(BF16, 2, 1, 22000, 64, 97)
+    need = pkg.attn_evict_workspace_bytes(2, 1, 22000)
+    space = torch.full((need + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    lens = torch.tensor([22000, 21000], dtype=torch.int32, device="cuda")
+    out = pkg.attn_evict(k, v, acc, lens=lens, keep=700, recent=50, workspace=space[2048:2048 + need])
+    torch.cuda.synchronize()
+    assert bool((space[:2048] == 0x5A).all()) and bool((space[2048 + need:] == 0x5A).all())
+    kw = dict(zip(("k_out", "v_out", "acc_out", "index", "lens_out"), out))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        pkg.attn_evict(k, v, acc, lens=lens, keep=700, recent=50, **kw)
+    for n in (22000, 500, 0, 16385):
+        lens.fill_(n)
+        acc.copy_(torch.rand_like(acc))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for i, want in enumerate(evict_ref(acc, [n] * 2, 700, 50)):
+            assert out[3][i, 0].tolist() == want.tolist() + [-1] * (700 - len(want))
+
+
 def test_ragged_batch_with_room_to_spare():
     k, v, acc = caches(BF16, 6, 3, 700, 128, 20)
     for keep, recent, cap in ((128, 16, 200), (300, 0, 300), (690, 690, 1000)):
