@@ -123,6 +123,8 @@ def attn_decode_prefix(q, kp, vp, k, v, *, causal: bool, scale: float, exp_mode:
     first lens[b] rows (int32 [B]; default Sk, default all) are filled, or None
     for none.  Returns (O [B,Hq,Sq,d] bf16, LSE [B,Hq,Sq] fp32 or None)."""
     L = _lib()
+    if (k is None) != (v is None) or (kp is None) != (vp is None):
+        raise ValueError("k and v, kp and vp: both or neither")
     B, Hq, Sq, d = shape = _four("q", q)
     dev, first = _current_gpu("q", q), q.dtype
     _tensor("q", q, shape, dev)

@@ -95,8 +95,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
                                                     krsrc, (wave * KEYS + 32 * kb + i32) * RB + 32 * t + 16 * g, 0, 0)));
 
   // ---- query rows of this (batch, KV head): heads * hrows consecutive ones.
-  // Tile in flight: chunk `step * 256 + tid` of its rows, and a row's log-sum
-  // (threads 0..63).  The loads have no branch, so that the waits can count
+  // Tile in flight: chunk `step * 256 + tid` of its rows, and each lane's row's
+  // log-sum.  The loads have no branch, so that the waits can count
   // them: rows beyond the last read as zero and touch no memory.  (Rows beyond
   // the end of a run are the next run's; the masks leave them out.)
   const size_t row0 = ((size_t)b * p.Hq + (size_t)h * p.G) * (size_t)p.Sq;
@@ -114,10 +114,18 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     for (int i = 0; i < STEPS; ++i)
       chunk[i] = __builtin_bit_cast(
           i32x4, __builtin_amdgcn_raw_buffer_load_b128(qrsrc, (i * NW * 64 + tid) * 16, row * RB, 0));
-    lse = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(lrsrc, tid * 4, row * 4, 0));
+    lse = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(lrsrc, lane * 4, row * 4, 0));
     if (++head == p.heads) head = 0, pos += KW_ROWS;
   };
   auto store = [&](int slot, int slot4) __attribute__((always_inline)) {
+    // rows that give nothing: their queries may hold anything
+    static_assert(KW_ROWS == 64, "a lane a row");
+    const unsigned long long none = __ballot(lse == -INFINITY);
+    if (none) {
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i)
+        if (none >> ((i * NW * 64 + tid) / C::NCH) & 1) chunk[i] = i32x4{0, 0, 0, 0};
+    }
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) store_row_chunk<DT, D>(tile[slot], i * NW * 64 + tid, chunk[i]);
     if (tid < KW_ROWS) top[slot4][tid] = lse != -INFINITY ? lse * 1.4426950408889634f : INFINITY;
@@ -277,6 +285,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   constexpr int RB = C::RB, KEYS = KW_FEW_KEYS, NB = KEYS / 32, CH = C::NCH / 2, NQ = D / 16;
   __shared__ __attribute__((aligned(16))) uint8_t rows[KW_FEW_ROWS * B16::RB];
   __shared__ __attribute__((aligned(16))) float top[KW_FEW_ROWS];  // lse log2(e) of the row, +inf for none
+  __shared__ __attribute__((aligned(16))) int dead[NW];  // whether a wave's rows hold one with lse = -inf
   const int tid = threadIdx.x, lane = tid & 63, i32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // the blocks are rotated from one (batch, KV head) to the next: with a number
@@ -335,9 +344,21 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
   if (tid < ntiles * HALF) {
     const float e = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(lrsrc, tid * 4, 0, 0));
-    top[tid] = tid < nrows && e != -INFINITY ? e * 1.4426950408889634f : INFINITY;
+    const bool none = e == -INFINITY;
+    top[tid] = tid < nrows && !none ? e * 1.4426950408889634f : INFINITY;
+    const bool some = __ballot(none) != 0;
+    if (lane == 0) dead[wave] = some ? 1 : 0;
+  } else if (lane == 0) {
+    dead[wave] = 0;
   }
   __syncthreads();
+  const i32x4 any = *(const i32x4*)dead;
+  if (any[0] | any[1] | any[2] | any[3]) {
+    // rows that give nothing: their queries may hold anything
+    for (int c = tid; c < ntiles * HALF * B16::NCH; c += NW * 64)
+      if (top[c / B16::NCH] == INFINITY) *(i32x4*)(rows + c * 16) = i32x4{0, 0, 0, 0};
+    __syncthreads();
+  }
   const int open = p.causal ? n - p.Sq + 1 : n;  // keys from here on are not seen by every row
   const int kswz = k_swz<DT_BF16, D>(i32);
   const uint8_t* qlane[NQ];

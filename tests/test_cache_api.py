@@ -154,6 +154,9 @@ def test_binding_refuses_host_tensors():
     k, f = torch.zeros(1, 2, 5, 64, dtype=torch.bfloat16), torch.zeros(1, 2, 5)
     with pytest.raises(ValueError, match="current GPU"):
         pkg.attn_decode_prefix(q, kp, kp, k, k, causal=True, scale=0.1, exp_mode=0, prefix_split_keys=0, split_keys=0)
+    for kv in ((kp, None, k, k), (None, kp, k, k), (kp, kp, k, None), (kp, kp, None, k)):
+        with pytest.raises(ValueError, match="both or neither"):
+            pkg.attn_decode_prefix(q, *kv, causal=True, scale=0.1, exp_mode=0, prefix_split_keys=0, split_keys=0)
     with pytest.raises(ValueError, match="current GPU"):
         pkg.attn_key_weights(q, k, f[..., :1], f, causal=True, scale=0.1)
     with pytest.raises(ValueError, match="current GPU"):

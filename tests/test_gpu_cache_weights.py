@@ -54,6 +54,29 @@ SHAPES = [
 
 @pytest.mark.parametrize("dt", [BF16, FP8])
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("shape", [SHAPES[1], SHAPES[3], SHAPES[6], SHAPES[9], SHAPES[10], SHAPES[12]])
+def test_rows_without_a_sum_give_nothing_whatever_they_hold(shape, d, dt):
+    B, Hq, Hkv, Sq, Sk, lens = shape
+    for causal in (True, False):
+        q, k, lse, acc, descale = setup(dt, d, B, Hq, Hkv, Sq, Sk, lens or [Sk] * B, causal, 150)
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(151)
+        out = torch.rand(lse.shape, generator=gen, device="cuda") < 0.2  # padding among the query rows
+        out[:, 0] = True
+        lse[out] = -math.inf
+        say(f"weights, rows left out {dt} d={d} {shape} causal={causal}")
+        want, tol = weights_ref(q, k, lse, acc, lens or [Sk] * B, causal, scale_of(d), descale, 0.5)
+        bad = q.float()
+        bad[out] = math.nan
+        q = bad.to(q.dtype)
+        t = torch.tensor(lens, dtype=torch.int32, device="cuda") if lens else None
+        pkg.attn_key_weights(q, k, lse, acc, lens=t, causal=causal, scale=scale_of(d), decay=0.5, descale=descale)
+        torch.cuda.synchronize()
+        assert bool(((acc.double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("dt", [BF16, FP8])
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("shape", SHAPES, ids=[str(i) for i in range(len(SHAPES))])
 def test_shapes(shape, d, dt):
     B, Hq, Hkv, Sq, Sk, lens = shape
