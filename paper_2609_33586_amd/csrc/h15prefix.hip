@@ -33,7 +33,8 @@
 // registers into BF16 tiles, was level for the exponential (LDS reads double)
 // and slower for the lattice weights, whose registers spilled (5K keys, 84 rows:
 // 25 -> 36 us).  Two FP8 tiles in LDS at a time, with a tile's time for their copies
-// and one barrier, were level too (66 -> 67 us): the waits are filled by the other
+// and one barrier, V's reads in half as many waits, and a higher wave priority of one
+// kind of workgroup were level (66 -> 66..72 us): the waits are filled by the other
 // workgroup.  Short caches wait: 4 chats of 500 + 60 keys BF16 d = 64 take 8.8 us
 // in one launch, 11 with the call.
 //
