@@ -83,6 +83,16 @@ bool chained(int P, int row_bytes, const PrefixParams& p) {
   return p.p_parts == 1 && p.o_parts == 1 && P <= 2 * round && (p.R >= WROWS || p.o_groups <= 512);
 }
 
+// Whether ragged own caches are taken longest first: where they are more than
+// one for each slot (two workgroups a compute unit, one of them the prefix's), so
+// that no long one starts last (32 heads over 8; in their own order / so: 128 caches of
+// up to 2K keys after 8K BF16 156 / 150 us, 64 92 / 87; up to 8K after 32K FP8 180 / 170,
+// 2K level).  With a slot each there is nothing to order.
+bool by_length(const PrefixParams& p) {
+  const int slots = 512 - (p.p_groups < 256 ? p.p_groups : 256);
+  return p.lens && p.B > 1 && p.B <= 256 && p.o_groups > slots;
+}
+
 size_t prefix_workspace(long long rows, int parts, int d) {
   return parts <= 1 ? 0 : (size_t)rows * (size_t)parts * ((size_t)d + 2) * sizeof(float);
 }
@@ -225,6 +235,7 @@ int attn_decode_prefix(const void* q, const void* kp, const void* vp, const void
     p.chain = p.parts = 1;
     p.p_groups = 0;
   }
+  p.longest = by_length(p);
   if (need) {
     if (!workspace || misaligned(workspace, 16) || workspace_bytes < need) return ATTN_EINVAL;
     p.part_o = (float*)workspace;

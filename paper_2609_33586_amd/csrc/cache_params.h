@@ -43,6 +43,7 @@ struct PrefixParams {
   int p_parts, p_split;  // parts of the prefix (0: no prefix) and their keys
   int o_parts, o_split;  // parts of the own caches (0: none) and their keys
   int parts;             // p_parts + o_parts (chained: 1)
+  int longest;           // own caches are taken in the order of their lengths (B <= 256)
   int chain;             // a workgroup of an own cache takes the prefix first (one part of each)
   int p_rows;            // query rows of a prefix workgroup: PREFIX_ROWS or WROWS
   int p_blocks, o_blocks;  // row blocks of a KV head's rows of all sequences, of one sequence

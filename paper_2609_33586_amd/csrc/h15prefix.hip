@@ -575,6 +575,26 @@ __device__ __forceinline__ void place(int L, int units, int blocks, int& unit, i
   }
 }
 
+// The sequence of rank `at` by the length of its cache, the longest first.
+__device__ __forceinline__ int longest(const PrefixParams& p, int at, int* lens) {
+  const int tid = threadIdx.x;
+  const int n = tid < p.B ? min(max(p.lens[tid], 0), p.Sk) : -1;
+  lens[tid] = n;
+  __syncthreads();
+  int rank = 0;
+  for (int j = 0; j < p.B; j += 4) {
+    const i32x4 x = *(const i32x4*)&lens[j];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) rank += x[e] > n || (x[e] == n && j + e < tid) ? 1 : 0;
+  }
+  __syncthreads();
+  if (tid < p.B && rank == at) lens[0] = tid;
+  __syncthreads();
+  const int b = __builtin_amdgcn_readfirstlane(lens[0]);
+  __syncthreads();
+  return b;
+}
+
 // FORM: how the prefix's rows are taken.
 enum { FORM_KEYS = 0, FORM_ROWS = 1, FORM_CHAIN = 2 };
 
@@ -609,9 +629,14 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
   } else {
     place(blockIdx.x - p.p_groups, p.B * p.Hkv * p.o_parts, p.o_blocks, unit, rb);
-    const int bh = unit / p.o_parts, split = unit - bh * p.o_parts;
+    int bh = unit / p.o_parts;
+    const int split = unit - bh * p.o_parts;
     w.b = bh / p.Hkv;
     w.h = bh - w.b * p.Hkv;
+    if (p.longest) {
+      w.b = longest(p, w.b, (int*)mx_lds);
+      bh = w.b * p.Hkv + w.h;
+    }
     w.part = p.p_parts + split;
     w.prefix = false;
     w.whole = !p.causal;

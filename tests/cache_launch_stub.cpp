@@ -22,7 +22,7 @@ extern "C" {
 int h15_stub_launches(void) { return g_launches; }
 int h15_stub_prefix(int what) {
   const int v[] = {g_prefix.p_parts, g_prefix.o_parts, g_prefix.p_rows, g_prefix.p_groups, g_prefix.o_groups,
-                   g_prefix.p_split, g_prefix.o_split, g_prefix.causal, g_prefix.chain};
+                   g_prefix.p_split, g_prefix.o_split, g_prefix.causal, g_prefix.chain, g_prefix.longest};
   return v[what];
 }
 int h15_stub_evict(int what) { return what == 0 ? g_evict.parts : g_evict.gather; }

@@ -34,11 +34,11 @@ def host(tmp_path_factory):
     return L
 
 
-def prefix_form(L, B, Hq, Hkv, Sq, P, Sk, p_cut=0, cut=0, causal=1):
-    rc = L.attn_decode_prefix(A, A, A, A, A, None, A, None, B, Hq, Hkv, Sq, P, P, Sk, Sk, 128, causal, 0.1, 0, 0, p_cut,
+def prefix_form(L, B, Hq, Hkv, Sq, P, Sk, p_cut=0, cut=0, causal=1, lens=None):
+    rc = L.attn_decode_prefix(A, A, A, A, A, lens, A, None, B, Hq, Hkv, Sq, P, P, Sk, Sk, 128, causal, 0.1, 0, 0, p_cut,
                               cut, A, 1 << 40, None)
     assert rc == pkg.ATTN_ELAUNCH
-    names = ("p_parts", "o_parts", "p_rows", "p_groups", "o_groups", "p_split", "o_split", "causal", "chain")
+    names = ("p_parts", "o_parts", "p_rows", "p_groups", "o_groups", "p_split", "o_split", "causal", "chain", "longest")
     return {n: L.h15_stub_prefix(i) for i, n in enumerate(names)}
 
 
@@ -70,6 +70,18 @@ def test_prefix_before_own_caches(host):
     assert prefix_form(host, 64, 32, 8, 1, 256, 100)["chain"] == 1
     assert prefix_form(host, 65, 32, 8, 1, 256, 100)["chain"] == 0
     assert prefix_form(host, 65, 32, 8, 8, 256, 100)["chain"] == 1
+
+
+def test_long_caches_first(host):
+    # 256 slots next to 256 prefix workgroups or more, 512 less those there are
+    many = (1, 32768, 100, 1024, 0)  # Sq, P, Sk and cuts: 32 parts of 8 heads
+    assert prefix_form(host, 32, 32, 8, *many, lens=A)["longest"] == 0
+    assert prefix_form(host, 33, 32, 8, *many, lens=A)["longest"] == 1
+    assert prefix_form(host, 33, 32, 8, *many)["longest"] == 0  # all alike
+    assert prefix_form(host, 256, 2, 2, 1, 0, 100, lens=A)["longest"] == 0
+    assert prefix_form(host, 256, 3, 3, 1, 0, 100, lens=A)["longest"] == 1
+    assert prefix_form(host, 257, 3, 3, 1, 0, 100, lens=A)["longest"] == 0  # more than a workgroup's threads
+    assert prefix_form(host, 1, 64, 64, 1, 0, 4096, 0, 128, lens=A)["longest"] == 0
 
 
 def test_weights_runs(host):

@@ -72,6 +72,22 @@ def test_shapes(shape, d, dt):
         run_and_check(dt, d, B, Hq, Hkv, Sq, P, Sk, lens, mode, p_cut, cut, True, 100)
 
 
+# more ragged own caches than slots, which are taken in the order of their lengths
+MANY = [
+    (150, 4, 4, 1, 600, 150, [(37 * i) % 151 for i in range(150)], 128, 0),
+    (256, 6, 3, 2, 0, 70, [70 if i % 3 else i % 70 for i in range(256)], 0, 0),  # many of one length
+    (255, 3, 3, 1, 0, 140, [0] * 254 + [140], 0, 128),
+    (99, 12, 3, 16, 200, 30, [30 - i % 31 for i in range(99)], 0, 0),  # two row blocks a cache, the prefix before them
+]
+
+
+@pytest.mark.parametrize("dt", [BF16, FP8])
+@pytest.mark.parametrize("shape", MANY, ids=[str(i) for i in range(len(MANY))])
+def test_long_caches_first(shape, dt):
+    B, Hq, Hkv, Sq, P, Sk, lens, p_cut, cut = shape
+    run_and_check(dt, 64, B, Hq, Hkv, Sq, P, Sk, lens, EXACT, p_cut, cut, True, 700)
+
+
 @pytest.mark.parametrize("dt", [BF16, FP8])
 @pytest.mark.parametrize("mode", [EXACT, H15, SQ4, SQ8])
 def test_modes_without_causal_mask(mode, dt):
