@@ -98,8 +98,8 @@ int attn_decode_prefix_split_keys(int B, int Hq, int Hkv, int Sq, int P, int Sk,
  * j <= n - Sq + i when causal, every key otherwise.  lse is what an attention
  * call returned for these rows (any entry point and exp_mode; with a prefix
  * the weights are shares of the whole, own keys only being counted); a row
- * with lse = -inf gives nothing.  decay = 1 accumulates; with decay = 0 the
- * old values are not read.  decay must be finite and >= 0.
+ * with lse = -inf gives nothing, whatever its q holds.  decay = 1 accumulates;
+ * with decay = 0 the old values are not read.  decay must be finite and >= 0.
  *
  * Sums are in FP32 (of FP32 logits), in a fixed order: results are
  * deterministic.
@@ -109,7 +109,8 @@ int attn_decode_prefix_split_keys(int B, int Hq, int Hkv, int Sq, int P, int Sk,
  * included.
  *
  * workspace: attn_key_weights_workspace_bytes() bytes, 16-byte aligned, for
- * calls with many query rows (may be NULL where that is 0).
+ * calls with many query rows (may be NULL where that is 0); it needs no
+ * initialising; two calls in flight at once must not share it.
  *
  * Errors: as attn_decode_prefix (lse, acc: 4-byte aligned); ATTN_EINVAL for
  * a decay that is negative or not finite; ATTN_EUNSUPPORTED for one KV head's
@@ -140,14 +141,16 @@ size_t attn_key_weights_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Sk, 
  * stream is used.
  *
  * workspace: attn_evict_workspace_bytes() bytes, 16-byte aligned, for long
- * caches (may be NULL where that is 0).
+ * caches (may be NULL where that is 0); it needs no initialising; two calls in
+ * flight at once must not share it.
  *
  * Errors: ATTN_EINVAL for a null pointer (lens may be), a size that is not
- * positive, Sk > Sk_cap, keep < 1 or > out_cap, recent < 0, or an output that
- * overlaps an input, the workspace or another output; ATTN_EUNSUPPORTED for d not in
- * {64, 128}, an unknown dtype, k, v, k_out or v_out not 16-byte aligned (the
- * others: 4), B * Hkv beyond 2^22 - 1, or more than 2^32 - 256 chunks of 16
- * bytes in the rows of K that may stay. */
+ * positive, Sk > Sk_cap, keep < 1 or > out_cap, recent < 0, a missing or short
+ * workspace, or an output or workspace that overlaps an input or another
+ * output; ATTN_EUNSUPPORTED for d not in {64, 128}, an unknown dtype, k, v,
+ * k_out or v_out not 16-byte aligned (the others: 4), Sk beyond 2^31 - 8193,
+ * B * Hkv (times the parts of 4096 keys of long caches) beyond 2^22 - 1, or
+ * more than 2^32 - 256 chunks of 16 bytes in the rows of K that may stay. */
 int attn_evict(const void* k, const void* v, const float* acc, const int32_t* lens, void* k_out, void* v_out,
                float* acc_out, int32_t* index, int32_t* lens_out, int B, int Hkv, int Sk, int Sk_cap, int out_cap,
                int d, int keep, int recent, int dtype, void* workspace, size_t workspace_bytes,

@@ -67,11 +67,11 @@ struct WeightsParams {
   float c1, decay;
 };
 
-// The keys that stay in each cache.
 // Keys of a selection's part, and what its launches hand on about one.
 constexpr int EVICT_PART = 4096;
 constexpr int EVICT_PART_BYTES = 4 * (1024 + 2 + EVICT_PART + 2);
 
+// The keys that stay in each cache.
 struct EvictParams {
   const uint8_t* k;
   const uint8_t* v;
@@ -83,9 +83,9 @@ struct EvictParams {
   int32_t* index;
   int32_t* lens_out;
   int B, Hkv, Sk, Sk_cap, keep, recent, out_cap, row_bytes;
-  uint8_t* scratch;
-  int parts;   // of EVICT_PART keys, if more than one workgroup selects for a head
-  int gather;  // the selecting workgroup copies the rows, too: no second launch
+  uint8_t* scratch;  // [B Hkv][parts] of EVICT_PART_BYTES (several parts only)
+  int parts;         // of EVICT_PART keys, a workgroup each
+  int gather;        // the selecting workgroup copies the rows, too: no second launch
 };
 
 // Launchers, as those of attn_params.h.  The caller has checked every argument.

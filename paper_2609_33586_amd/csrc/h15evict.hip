@@ -183,7 +183,9 @@ __device__ __forceinline__ void select_keys(const EvictParams& p, int bh, int n,
         for (int e = 0; e < 4; ++e)
           if (few) {
             if (in[e]) atomicAdd(&hist[lane & 1][(u[e] >> shift) & ((1u << width) - 1)], 1u);
-          } else if (__ballot(in[e])) count(hist[lane & 1], in[e] ? (int)((u[e] >> shift) & ((1u << width) - 1)) : -1, lane);
+          } else if (__ballot(in[e])) {
+            count(hist[lane & 1], in[e] ? (int)((u[e] >> shift) & ((1u << width) - 1)) : -1, lane);
+          }
       }
       __syncthreads();
     }

@@ -224,8 +224,9 @@ __device__ __forceinline__ float row_lse(float m, float l, float c1) {
 // CHAIN: the same rows meet `before` first, a part of its own with a running
 // maximum of its own, whose sums wait in registers and are merged in at the end.
 template <int DT, int D, int MODE, bool CHAIN>
-__device__ __forceinline__ void keys_form(const PrefixParams& p, const Work& before, const Work& own, uint8_t* ksm, uint8_t* vsm,
-                                          float (*mx_lds)[32][NW], float (*m_lds)[NW], float (*l_lds)[NW]) {
+__device__ __forceinline__ void keys_form(const PrefixParams& p, const Work& before, const Work& own, uint8_t* ksm,
+                                          uint8_t* vsm, float (*mx_lds)[32][NW], float (*m_lds)[NW],
+                                          float (*l_lds)[NW]) {
   using C = PCfg<DT, D>;
   constexpr int NB = C::NB, UNIT = C::UNIT, TPR = C::TPR, SLOT = C::SLOT, RB = C::RB;
   constexpr int NDB = D / 32, LOADS = SLOT / 1024, RHALF = 16;
@@ -737,9 +738,12 @@ template <int DT, int D, int MODE>
 hipError_t launch_one(const PrefixParams& p, hipStream_t st) {
   const dim3 grid((unsigned)(p.p_groups + p.o_groups));
   const dim3 block(NW * 64);
-  if (p.chain) hipLaunchKernelGGL((attn_prefix_kernel<DT, D, MODE, FORM_CHAIN>), grid, block, 0, st, p);
-  else if (p.p_rows == PREFIX_ROWS) hipLaunchKernelGGL((attn_prefix_kernel<DT, D, MODE, FORM_ROWS>), grid, block, 0, st, p);
-  else hipLaunchKernelGGL((attn_prefix_kernel<DT, D, MODE, FORM_KEYS>), grid, block, 0, st, p);
+  if (p.chain)
+    hipLaunchKernelGGL((attn_prefix_kernel<DT, D, MODE, FORM_CHAIN>), grid, block, 0, st, p);
+  else if (p.p_rows == PREFIX_ROWS)
+    hipLaunchKernelGGL((attn_prefix_kernel<DT, D, MODE, FORM_ROWS>), grid, block, 0, st, p);
+  else
+    hipLaunchKernelGGL((attn_prefix_kernel<DT, D, MODE, FORM_KEYS>), grid, block, 0, st, p);
   return hipGetLastError();
 }
 
