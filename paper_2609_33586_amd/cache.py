@@ -74,9 +74,10 @@ def _current_gpu(name, t) -> int:
 
 
 def _four(name, t):
-    if len(t.shape) != 4:
+    shape = t.shape
+    if len(shape) != 4 or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous 4-D device tensor")
-    return t.shape
+    return shape
 
 
 def _lens_ptr(lens, B, dev):
@@ -127,7 +128,6 @@ def attn_decode_prefix(q, kp, vp, k, v, *, causal: bool, scale: float, exp_mode:
         raise ValueError("k and v, kp and vp: both or neither")
     B, Hq, Sq, d = shape = _four("q", q)
     dev, first = _current_gpu("q", q), q.dtype
-    _tensor("q", q, shape, dev)
     dt = _dtype_of(q)
     Hkv = P_cap = Sk_cap = 0
     kptr = vptr = kpptr = vpptr = None
@@ -145,7 +145,11 @@ def attn_decode_prefix(q, kp, vp, k, v, *, causal: bool, scale: float, exp_mode:
         vpptr = _operand("vp", vp, shape, dev, first, dt).data_ptr()
     P = P_cap if P is None else int(P)
     Sk = Sk_cap if Sk is None else int(Sk)
-    out, lse = _outputs(q, out, lse, want_lse)
+    if out is None or lse is None:
+        out, lse = _outputs(q, out, lse, want_lse)
+    else:
+        _tensor("out", out, q.shape, dev, _torch.bfloat16)
+        _tensor("lse", lse, q.shape[:3], dev, _torch.float32)
     wptr, wbytes, workspace = _space(workspace, lambda: L.attn_decode_prefix_workspace_bytes(
         B, Hq, Sq, P, Sk, d, prefix_split_keys, split_keys), dev, stream)
     opts = _opts(descale, stream)
@@ -172,7 +176,6 @@ def attn_key_weights(q, k, lse, acc, *, causal: bool, scale: float, decay: float
     L = _lib()
     B, Hq, Sq, d = shape = _four("q", q)
     dev = _current_gpu("q", q)
-    _tensor("q", q, shape, dev)
     dt = _dtype_of(q)
     _, Hkv, cap, _ = _four("k", k)
     _operand("k", k, (B, Hkv, cap, d), dev, q.dtype, dt)
@@ -208,7 +211,6 @@ def attn_evict(k, v, acc, *, keep: int, recent: int, lens=None, Sk: int | None =
     L = _lib()
     B, Hkv, cap, d = shape = _four("k", k)
     dev, first, f32, i32 = _current_gpu("k", k), k.dtype, _torch.float32, _torch.int32
-    _tensor("k", k, shape, dev)
     dt = _dtype_of(k)
     _operand("v", v, shape, dev, first, dt)
     _tensor("acc", acc, (B, Hkv, cap), dev, f32)
