@@ -68,6 +68,11 @@ def test_prefix_sizes(L):
                  (64, 64, 1, 16, 0, 65536)):
         a, b = pkg.attn_decode_prefix_split_keys(*args, 128, 0)
         assert a >= 0 and b >= 0 and a % 128 == 0 and b % 128 == 0
+    cuts = pkg.attn_decode_prefix_split_keys
+    assert cuts(16, 32, 8, 1, 0, 8192, 128, 0) == (0, 2048) and cuts(16, 32, 8, 1, 300, 8192, 128, 0) == (0, 4096)
+    # next to a prefix in parts: own caches in as many parts as workgroups are left of 512, of two tiles or more
+    assert cuts(7, 24, 8, 4, 5003, 777, 128, 1) == (512, 384) and cuts(24, 32, 8, 1, 8192, 1024, 128, 1) == (768, 0)
+    assert cuts(64, 32, 8, 1, 32768, 2048, 128, 0) == (2048, 0) and cuts(1, 8, 1, 4096, 8192, 512, 128, 0)[1] == 0
     assert pkg.attn_decode_prefix_split_keys(0, 32, 8, 1, 100, 100, 128, 0) == (0, 0)
     assert pkg.attn_decode_prefix_split_keys(1, 32, 7, 1, 100000, 100000, 128, 0) == (0, 0)
     assert L.attn_decode_prefix_split_keys(1, 32, 8, 1, 100, 100, 128, 0, None, None) == INV
