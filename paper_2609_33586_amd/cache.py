@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 
-from . import ATTN_OK, AttnError, _dtype_of, _opts, _outputs, attn_opts, lib
+from . import ATTN_OK, AttnError, _current_stream, _dtype_of, _outputs, attn_opts, lib
 
 # every symbol h15cache.h declares
 EXPORTS = ("attn_decode_prefix", "attn_decode_prefix_workspace_bytes", "attn_decode_prefix_split_keys",
@@ -80,6 +80,24 @@ def _four(name, t):
     return shape
 
 
+def _cache(name, t, B, d, dev, first, dt):
+    """KV heads and rows of a cache [B,Hkv,rows,d] on device number dev, of the first operand's type."""
+    shape = t.shape
+    if len(shape) != 4 or shape[0] != B or shape[3] != d or not t.is_contiguous() or t.get_device() != dev:
+        _tensor(name, t, (B, *shape[1:3], d), dev)
+    if t.dtype != first and _dtype_of(t) != dt:
+        raise TypeError(f"{name} and the first operand must share one operand type")
+    return shape[1], shape[2]
+
+
+def _call_opts(descale, stream):
+    handle = stream.cuda_stream if stream is not None else _current_stream()
+    if descale is None:
+        return attn_opts(1.0, 1.0, 1.0, handle, 0.0, 0)
+    qd, kd, vd = descale
+    return attn_opts(float(qd), float(kd), float(vd), handle, 0.0, 0)
+
+
 def _lens_ptr(lens, B, dev):
     return None if lens is None else _tensor("lens", lens, (B,), dev, _torch.int32).data_ptr()
 
@@ -132,10 +150,9 @@ def attn_decode_prefix(q, kp, vp, k, v, *, causal: bool, scale: float, exp_mode:
     Hkv = P_cap = Sk_cap = 0
     kptr = vptr = kpptr = vpptr = None
     if k is not None:
-        _, Hkv, Sk_cap, _ = _four("k", k)
-        shape = (B, Hkv, Sk_cap, d)
-        kptr = _operand("k", k, shape, dev, first, dt).data_ptr()
-        vptr = _operand("v", v, shape, dev, first, dt).data_ptr()
+        Hkv, Sk_cap = _cache("k", k, B, d, dev, first, dt)
+        kptr = k.data_ptr()
+        vptr = _operand("v", v, k.shape, dev, first, dt).data_ptr()
     if kp is not None:
         if k is None:
             Hkv = kp.shape[0]
@@ -152,7 +169,7 @@ def attn_decode_prefix(q, kp, vp, k, v, *, causal: bool, scale: float, exp_mode:
         _tensor("lse", lse, q.shape[:3], dev, _torch.float32)
     wptr, wbytes, workspace = _space(workspace, lambda: L.attn_decode_prefix_workspace_bytes(
         B, Hq, Sq, P, Sk, d, prefix_split_keys, split_keys), dev, stream)
-    opts = _opts(descale, stream)
+    opts = _call_opts(descale, stream)
     rc = L.attn_decode_prefix(q.data_ptr(), kpptr, vpptr, kptr, vptr, _lens_ptr(lens, B, dev), out.data_ptr(),
                               lse.data_ptr() if lse is not None else None, B, Hq, Hkv, Sq, P, P_cap, Sk, Sk_cap, d,
                               1 if causal else 0, scale, dt, exp_mode, prefix_split_keys, split_keys, wptr, wbytes,
@@ -177,8 +194,7 @@ def attn_key_weights(q, k, lse, acc, *, causal: bool, scale: float, decay: float
     B, Hq, Sq, d = shape = _four("q", q)
     dev = _current_gpu("q", q)
     dt = _dtype_of(q)
-    _, Hkv, cap, _ = _four("k", k)
-    _operand("k", k, (B, Hkv, cap, d), dev, q.dtype, dt)
+    Hkv, cap = _cache("k", k, B, d, dev, q.dtype, dt)
     _tensor("lse", lse, (B, Hq, Sq), dev, _torch.float32)
     _tensor("acc", acc, (B, Hkv, cap), dev, _torch.float32)
     Sk = cap if Sk is None else int(Sk)
@@ -186,7 +202,7 @@ def attn_key_weights(q, k, lse, acc, *, causal: bool, scale: float, decay: float
                                      stream)
     if descale is not None:
         descale = (descale[0], descale[1], 1.0)
-    opts = _opts(descale, stream)
+    opts = _call_opts(descale, stream)
     rc = L.attn_key_weights(q.data_ptr(), k.data_ptr(), lse.data_ptr(), _lens_ptr(lens, B, dev), acc.data_ptr(), B,
                             Hq, Hkv, Sq, Sk, cap, d, 1 if causal else 0, scale, decay, dt, wptr, wbytes,
                             ctypes.byref(opts))
@@ -228,7 +244,7 @@ def attn_evict(k, v, acc, *, keep: int, recent: int, lens=None, Sk: int | None =
     index = new(shape, i32) if index is None else _tensor("index", index, shape, dev, i32)
     lens_out = new((B,), i32) if lens_out is None else _tensor("lens_out", lens_out, (B,), dev, i32)
     wptr, wbytes, workspace = _space(workspace, lambda: L.attn_evict_workspace_bytes(B, Hkv, Sk), dev, stream)
-    opts = _opts(None, stream)
+    opts = _call_opts(None, stream)
     rc = L.attn_evict(k.data_ptr(), v.data_ptr(), acc.data_ptr(), _lens_ptr(lens, B, dev), k_out.data_ptr(),
                       v_out.data_ptr(), acc_out.data_ptr(), index.data_ptr(), lens_out.data_ptr(), B, Hkv, Sk, cap,
                       out_cap, d, keep, int(recent), dt, wptr, wbytes, ctypes.byref(opts))

@@ -183,6 +183,15 @@ def test_binding_checks_shapes_and_types(L):
         cache._operand("k", k, (2,), -1, torch.bfloat16, pkg.ATTN_BF16)
     with pytest.raises(ValueError, match="4-D"):
         cache._four("k", k)
+    c = torch.zeros(2, 3, 5, 64, dtype=torch.uint8)
+    assert cache._cache("k", c, 2, 64, -1, torch.float8_e4m3fn, pkg.ATTN_FP8_E4M3) == (3, 5)
+    for bad in (c[:1], c[..., :32].contiguous(), c[0], c.unsqueeze(0), c.transpose(1, 2), c[0, 0, 0], c[0, 0]):
+        with pytest.raises(ValueError, match="k must be a contiguous tensor"):
+            cache._cache("k", bad, 2, 64, -1, torch.uint8, pkg.ATTN_FP8_E4M3)
+    with pytest.raises(ValueError, match="GPU 0"):
+        cache._cache("k", c, 2, 64, 0, torch.uint8, pkg.ATTN_FP8_E4M3)
+    with pytest.raises(TypeError, match="k and the first operand"):
+        cache._cache("k", c, 2, 64, -1, torch.bfloat16, pkg.ATTN_BF16)
     assert cache._lens_ptr(None, 2, -1) is None
     for bad in (torch.zeros(2, dtype=torch.int64), torch.zeros(3, dtype=torch.int32)):
         with pytest.raises(ValueError, match="lens"):
