@@ -7,6 +7,11 @@ declared in ``include/h15attn.h``.  The functions carry the C names.
 
 There is no fallback: if the library is missing or a call fails, an exception
 is raised.
+
+With ``stream`` a call runs there, not on the current stream.  Nothing is waited
+for: what the caller gives must be ready on that stream, and stay until the
+work is done there (``Tensor.record_stream``).  Tensors that the call takes
+itself, outputs and workspaces that are not given, come from that stream's pool.
 """
 from __future__ import annotations
 
@@ -134,7 +139,33 @@ def _check(q, k, v):
     return B, Hq, sk[1], S, d, _one_dtype(q, k, v)
 
 
-def _outputs(q, out, lse, want_lse):
+def _new(shape, dtype, device, stream):
+    """A new tensor that a call on this stream (None: the current one) writes and returns.
+
+    It is taken from the pool of the stream that writes it: the current
+    stream's pool may hand out a block that was just let go and that a kernel
+    still running there uses.  The caller's stream has it next, so its release
+    waits for that one, too."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    caller = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(caller)
+    return t
+
+
+def _new_workspace(nbytes, device, stream):
+    """A workspace for one call on this stream, of that stream's pool as in _new (and back to it after the call)."""
+    import torch
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _outputs(q, out, lse, want_lse, stream=None):
     """O [B,Hq,S,d] bf16 and LSE [B,Hq,S] fp32 (None unless wanted or given):
     the caller's tensors after checks, else new ones.  The library writes
     through the data pointers, so a given tensor must be contiguous, of the
@@ -142,12 +173,12 @@ def _outputs(q, out, lse, want_lse):
     import torch
     shape, device = q.shape, q.device
     if out is None:
-        out = torch.empty(shape, dtype=torch.bfloat16, device=device)
+        out = _new(shape, torch.bfloat16, device, stream)
     elif out.shape != shape or out.dtype != torch.bfloat16 or not out.is_contiguous() or out.device != device:
         raise ValueError(f"out must be a contiguous bfloat16 tensor {tuple(shape)} on {device}")
     if lse is None:
         if want_lse:
-            lse = torch.empty(shape[:3], dtype=torch.float32, device=device)
+            lse = _new(shape[:3], torch.float32, device, stream)
     elif lse.shape != shape[:3] or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != device:
         raise ValueError(f"lse must be a contiguous float32 tensor {tuple(shape[:3])} on {device}")
     return out, lse
@@ -179,7 +210,7 @@ def attn_fwd_ex(q, k, v, *, causal: bool, scale: float, exp_mode: int, descale=N
     """O (and LSE) of attention; see include/h15attn.h for the definition.
     tau / tau_per_wave: the conditional-rescale threshold and its granularity."""
     B, Hq, Hkv, S, d, dt = _check(q, k, v)
-    out, lse = _outputs(q, out, lse, want_lse)
+    out, lse = _outputs(q, out, lse, want_lse, stream)
     opts = _opts(descale, stream, tau, tau_per_wave)
     rc = lib().attn_fwd_ex(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                            lse.data_ptr() if lse is not None else None, B, Hq, Hkv, S, d,
@@ -208,10 +239,8 @@ def attn_fwd_probe(q, k, v, *, causal: bool, scale: float, exp_mode: int, b: int
     """Returns (O, LSE, s, w, p_bits) with s/w/p_bits of shape [nrows, S]."""
     import torch
     B, Hq, Hkv, S, d, dt = _check(q, k, v)
-    out, lse = _outputs(q, None, None, True)
-    s = torch.empty((nrows, S), dtype=torch.float32, device=q.device)
-    w = torch.empty((nrows, S), dtype=torch.float32, device=q.device)
-    pb = torch.empty((nrows, S), dtype=torch.int32, device=q.device)
+    out, lse = _outputs(q, None, None, True, stream)
+    s, w, pb = (_new((nrows, S), t, q.device, stream) for t in (torch.float32, torch.float32, torch.int32))
     opts = _opts(descale, stream, tau, tau_per_wave)
     rc = lib().attn_fwd_probe(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
                               B, Hq, Hkv, S, d, int(bool(causal)), float(scale), dt, int(exp_mode),
@@ -243,11 +272,10 @@ def _check_decode(q, k, v, Sk):
     return B, Hq, sk[1], Sq, (cap if Sk is None else int(Sk)), cap, d, _one_dtype(q, k, v)
 
 
-def _workspace(q, B, Hq, Sq, Sk, d, split_keys, workspace):
-    import torch
+def _workspace(q, B, Hq, Sq, Sk, d, split_keys, workspace, stream=None):
     need = attn_decode_workspace_bytes(B, Hq, Sq, Sk, d, split_keys)
     if workspace is None:
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device) if need else None
+        workspace = _new_workspace(max(need, 16), q.device, stream) if need else None
     elif not workspace.is_contiguous() or workspace.device != q.device:
         raise ValueError(f"workspace must be a contiguous tensor on {q.device}")
     ptr = workspace.data_ptr() if workspace is not None else None
@@ -264,8 +292,8 @@ def attn_decode(q, k, v, *, causal: bool, scale: float, exp_mode: int, split_key
     workspace: a device buffer of attn_decode_workspace_bytes() bytes
     (allocated here when None and the cut has several parts)."""
     B, Hq, Hkv, Sq, Sk, cap, d, dt = _check_decode(q, k, v, Sk)
-    out, lse = _outputs(q, out, lse, want_lse)
-    ws, wptr, wbytes = _workspace(q, B, Hq, Sq, Sk, d, split_keys, workspace)
+    out, lse = _outputs(q, out, lse, want_lse, stream)
+    ws, wptr, wbytes = _workspace(q, B, Hq, Sq, Sk, d, split_keys, workspace, stream)
     opts = _opts(descale, stream)
     rc = lib().attn_decode(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                            lse.data_ptr() if lse is not None else None, B, Hq, Hkv, Sq, Sk, cap, d,
@@ -282,7 +310,7 @@ def attn_decode_noalloc(q, k, v, *, causal: bool, scale: float, exp_mode: int, s
     attn_decode_noalloc).  Pass out (and lse) to keep the call free of
     allocations; calls that overlap on one GPU race on the built-in buffer."""
     B, Hq, Hkv, Sq, Sk, cap, d, dt = _check_decode(q, k, v, Sk)
-    out, lse = _outputs(q, out, lse, want_lse)
+    out, lse = _outputs(q, out, lse, want_lse, stream)
     opts = _opts(descale, stream)
     rc = lib().attn_decode_noalloc(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                                    lse.data_ptr() if lse is not None else None, B, Hq, Hkv, Sq, Sk, cap, d,
@@ -298,11 +326,9 @@ def attn_decode_probe(q, k, v, *, causal: bool, scale: float, exp_mode: int, spl
     """Returns (O, LSE, s, w, p_bits) with s/w/p_bits of shape [Sk] for query row (b, h, i)."""
     import torch
     B, Hq, Hkv, Sq, Sk, cap, d, dt = _check_decode(q, k, v, Sk)
-    out, lse = _outputs(q, None, None, True)
-    ws, wptr, wbytes = _workspace(q, B, Hq, Sq, Sk, d, split_keys, None)
-    s = torch.empty(Sk, dtype=torch.float32, device=q.device)
-    w = torch.empty(Sk, dtype=torch.float32, device=q.device)
-    pb = torch.empty(Sk, dtype=torch.int32, device=q.device)
+    out, lse = _outputs(q, None, None, True, stream)
+    ws, wptr, wbytes = _workspace(q, B, Hq, Sq, Sk, d, split_keys, None, stream)
+    s, w, pb = (_new((Sk,), t, q.device, stream) for t in (torch.float32, torch.float32, torch.int32))
     opts = _opts(descale, stream)
     rc = lib().attn_decode_probe(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), B, Hq,
                                  Hkv, Sq, Sk, cap, d, int(bool(causal)), float(scale), dt, int(exp_mode),

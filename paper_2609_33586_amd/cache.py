@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 
-from . import ATTN_OK, AttnError, _current_stream, _dtype_of, _outputs, attn_opts, lib
+from . import ATTN_OK, AttnError, _current_stream, _dtype_of, _new, _new_workspace, _outputs, attn_opts, lib
 
 # every symbol h15cache.h declares
 EXPORTS = ("attn_decode_prefix", "attn_decode_prefix_workspace_bytes", "attn_decode_prefix_split_keys",
@@ -108,9 +108,7 @@ def _space(workspace, need, dev, stream):
         n = need()
         if not n:
             return None, 0, None
-        workspace = _torch.empty(n, dtype=_torch.uint8, device=f"cuda:{dev}")
-        if stream is not None:
-            workspace.record_stream(stream)  # it is let go before the work on that stream is done
+        workspace = _new_workspace(n, f"cuda:{dev}", stream)
         return workspace.data_ptr(), n, workspace
     if not workspace.is_contiguous() or workspace.get_device() != dev:
         raise ValueError(f"workspace must be a contiguous tensor on GPU {dev}")
@@ -163,7 +161,7 @@ def attn_decode_prefix(q, kp, vp, k, v, *, causal: bool, scale: float, exp_mode:
     P = P_cap if P is None else int(P)
     Sk = Sk_cap if Sk is None else int(Sk)
     if out is None or lse is None:
-        out, lse = _outputs(q, out, lse, want_lse)
+        out, lse = _outputs(q, out, lse, want_lse, stream)
     else:
         _tensor("out", out, q.shape, dev, _torch.bfloat16)
         _tensor("lse", lse, q.shape[:3], dev, _torch.float32)
@@ -235,7 +233,7 @@ def attn_evict(k, v, acc, *, keep: int, recent: int, lens=None, Sk: int | None =
     given = k_out if k_out is not None else v_out
     out_cap = rows if given is None else _four("k_out", given)[2]
     shape = (B, Hkv, out_cap, d)
-    new = lambda size, dtype: _torch.empty(size, dtype=dtype, device=k.device)  # noqa: E731
+    new = lambda size, dtype: _new(size, dtype, k.device, stream)  # noqa: E731
     k_out = new(shape, first) if k_out is None else _operand("k_out", k_out, shape, dev, first, dt)
     v_out = new(shape, first) if v_out is None else _operand("v_out", v_out, shape, dev, first, dt)
     shape = (B, Hkv, out_cap)
