@@ -149,8 +149,8 @@ size_t attn_key_weights_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Sk, 
  * workspace, or an output or workspace that overlaps an input or another
  * output; ATTN_EUNSUPPORTED for d not in {64, 128}, an unknown dtype, k, v,
  * k_out or v_out not 16-byte aligned (the others: 4), Sk beyond 2^31 - 8193,
- * B * Hkv (times the parts of 4096 keys of long caches) beyond 2^22 - 1, or
- * more than 2^32 - 256 chunks of 16 bytes in the rows of K that may stay. */
+ * B * Hkv beyond 2^22 - 1, or more than 2^32 - 256 chunks of 16 bytes in the
+ * rows of K that may stay. */
 int attn_evict(const void* k, const void* v, const float* acc, const int32_t* lens, void* k_out, void* v_out,
                float* acc_out, int32_t* index, int32_t* lens_out, int B, int Hkv, int Sk, int Sk_cap, int out_cap,
                int d, int keep, int recent, int dtype, void* workspace, size_t workspace_bytes,

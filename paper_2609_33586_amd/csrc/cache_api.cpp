@@ -129,14 +129,25 @@ int weights_run(long long heads, long long units) {
 // 512 rows, 2 heads 12.3 / 12.1, 320 heads 48 / 42).
 constexpr int EVICT_GATHER = 4096;
 
-// Workgroups that select for one head: a single one, unless few heads have long
-// caches (of which it holds eight parts in LDS).  Times of a call with one / with a
-// workgroup a part, 256 FP8 rows of d = 64 staying: 8 heads, 16K keys 16 / 18 us, 25K
-// 20 / 19, 32K 23 / 19, 100K 99 / 21; 64 heads, 32K 24 / 25, 50K 51 / 40; 128 heads,
-// 50K 53 / 65; 256 heads 58 / 130.
-int evict_parts(long long heads, int Sk) {
-  if (Sk <= 5 * EVICT_PART || heads > (Sk > 8 * EVICT_PART ? 64 : 32)) return 1;
-  return (int)ceil_div(Sk, EVICT_PART);
+// Keys of a workgroup's part in the selection for a head: all of them, unless few heads
+// have long caches (of which one workgroup holds eight parts of EVICT_PART in LDS).  Times of a
+// call with one workgroup a head for spread / for equal weights, and in parts for
+// either, 256 FP8 rows of d = 64 staying: 8 heads, 25K keys 20 / 27 and 25 us, 33K 24 / 33
+// and 24, 128K 132 / 163 and 27, 1M 1197 / 1385 and 59; 32 heads, 33K 24 / 33 and 31, 64K
+// 62 / 79 and 33; 64 heads, 33K 24 / 33 and 40, 50K 48 / 61 and 41, 1M 1655 / 1904 and 348.
+// A head has 32 parts at most, all heads 640 (beyond, each takes more keys, as far as
+// its counts can): every workgroup adds up the counts of its head's parts (8 heads of 256K
+// keys in 32 / 64 parts 36 / 55 us, of 1M 58 / 79).
+int evict_part_keys(long long heads, int Sk) {
+  if (Sk <= 5 * EVICT_PART || heads > (Sk > 8 * EVICT_PART ? 64 : 32)) return Sk;
+  const long long most = heads > 20 ? 640 / heads : 32;
+  const long long keys = ceil_div(ceil_div(Sk, EVICT_PART), most) * EVICT_PART;
+  return (int)(keys < EVICT_PART_MOST ? keys : EVICT_PART_MOST);
+}
+
+size_t evict_workspace(long long heads, int Sk) {
+  const size_t keys = (size_t)evict_part_keys(heads, Sk), parts = (size_t)ceil_div(Sk, (long long)keys);
+  return parts == 1 ? 0 : (size_t)heads * parts * EVICT_PART_BYTES;
 }
 
 struct Range {
@@ -315,9 +326,7 @@ int attn_key_weights(const void* q, const void* k, const float* lse, const int32
 
 size_t attn_evict_workspace_bytes(int B, int Hkv, int Sk) {
   if (B <= 0 || Hkv <= 0 || Sk <= 0) return 0;
-  const long long heads = (long long)B * Hkv;
-  const int parts = evict_parts(heads, Sk);
-  return parts == 1 ? 0 : (size_t)heads * parts * EVICT_PART_BYTES;
+  return evict_workspace((long long)B * Hkv, Sk);
 }
 
 int attn_evict(const void* k, const void* v, const float* acc, const int32_t* lens, void* k_out, void* v_out,
@@ -367,11 +376,11 @@ int attn_evict(const void* k, const void* v, const float* acc, const int32_t* le
   p.keep = keep;
   p.recent = recent;
   p.out_cap = out_cap;
-  p.parts = evict_parts((long long)heads, Sk);
+  p.part_keys = evict_part_keys((long long)heads, Sk);
+  p.parts = (int)ceil_div(Sk, p.part_keys);
   p.gather = p.parts == 1 && (long long)keep * (p.row_bytes / 16) <= EVICT_GATHER;
-  if ((long long)heads * p.parts > MAX_GROUPS / 4) return ATTN_EUNSUPPORTED;
   if (p.parts > 1) {
-    const size_t need = heads * p.parts * EVICT_PART_BYTES;
+    const size_t need = evict_workspace((long long)heads, Sk);
     if (!workspace || misaligned(workspace, 16) || workspace_bytes < need) return ATTN_EINVAL;
     p.scratch = (uint8_t*)workspace;
     const Range ws = range(workspace, need);

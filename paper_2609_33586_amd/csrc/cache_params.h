@@ -67,9 +67,11 @@ struct WeightsParams {
   float c1, decay;
 };
 
-// Keys of a selection's part, and what its launches hand on about one.
+// A selection's parts have a multiple of EVICT_PART keys each, EVICT_PART_MOST of them
+// at most; what its launches hand on about one.
 constexpr int EVICT_PART = 4096;
-constexpr int EVICT_PART_BYTES = 4 * (1024 + 2 + EVICT_PART + 2);
+constexpr int EVICT_PART_MOST = 15 * EVICT_PART;
+constexpr int EVICT_PART_BYTES = 4 * (2 * 1024 + 512 + 4);
 
 // The keys that stay in each cache.
 struct EvictParams {
@@ -84,7 +86,8 @@ struct EvictParams {
   int32_t* lens_out;
   int B, Hkv, Sk, Sk_cap, keep, recent, out_cap, row_bytes;
   uint8_t* scratch;  // [B Hkv][parts] of EVICT_PART_BYTES (several parts only)
-  int parts;         // of EVICT_PART keys, a workgroup each
+  int parts;         // of part_keys keys, a workgroup each
+  int part_keys;
   int gather;        // the selecting workgroup copies the rows, too: no second launch
 };
 

@@ -5,7 +5,7 @@
 // indexes; then their rows of K, V and acc are gathered into the compact caches,
 // 16 bytes a thread, by that workgroup if they are few, else by a launch of their
 // own.  Where few heads have long caches, parts of the keys have a workgroup each,
-// in three launches.  (The rules: cache_api.cpp.)
+// in four launches.  (The rules: cache_api.cpp.)
 //
 // The selection is a radix search for the weight of rank keep - recent in three
 // rounds over 11, 11 and 10 bits, each a histogram in LDS of the keys that agree
@@ -22,7 +22,7 @@
 // included; of 32K keys by one workgroup 25 us: 6 for the first digits, whose
 // counts in LDS follow each other where weights are equal, 4 and 1.3 for the others,
 // 5 for the indexes, each instruction a key taking 0.25 us of a compute unit; in
-// parts 5 + 5 + 7 us, and 4 for the gather.
+// parts 4 + 5 + 5 + 6 us, whatever the weights are, and 5 for the gather.
 #include "cache_params.h"
 
 #include <hip/hip_runtime.h>
@@ -40,6 +40,8 @@ constexpr int BINS = 2048;
 constexpr int HELD_FEW = 8192, HELD_MANY = 32768;
 constexpr int STEP = 256;    // keys of a wave and step: four a lane
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Weights as unsigned numbers in their order: +0 and -0 alike, NaN above all.
@@ -237,178 +239,205 @@ __device__ __forceinline__ void select_keys(const EvictParams& p, int bh, int n,
   }
 }
 
-// The same by EVICT_PART keys a workgroup, in three launches: the first digits of
-// every part's weights are counted; every workgroup adds up its head's counts and
-// writes down its part's candidates, the keys with the digits found; every
-// workgroup finds the remaining digits from its head's candidates, and places its
-// own part's keys, those of the parts before it being counted from their
-// candidates.  What the launches hand on, for each part:
+// The same by a workgroup for each part of a head's keys, in four launches: three
+// count the digits of a part's weights, each after the digits before them have been
+// found from the counts of all the head's parts; the last finds the lowest digits and
+// places the part's keys.  What a workgroup reads depends on the number of keys and
+// parts alone: all of them equal or all different take the same time.  (Three launches, the
+// last of which passed over the keys of the whole head that agree with the first digits,
+// took 21 us for 8 heads of 33000 spread weights, where these take 23, but 72 for
+// equal ones, and grew with the square of the keys: 64 heads of one million equal ones
+// 36 ms, now 0.34.)  What the launches hand on, for each part:
 struct Part {
-  uint32_t counts[BINS / 2];     // of two bins, the even one's low
-  uint32_t above, candidates;    // keys with higher first digits, and with these
-  uint32_t rest[EVICT_PART];     // the candidates' remaining digits, in order of the keys
-  uint32_t digits, left;         // the first digits, what is wanted of the head's candidates
+  uint32_t counts[2][BINS / 2];  // of two bins of the first and second digits, the even one's low
+  uint32_t low[BINS / 4];        // of the third
+  uint32_t digits, left;         // the digits so far, what is wanted of the keys with them
+  uint32_t above;                // keys of the parts before this one with higher digits so far
+  uint32_t unused;
 };
 static_assert(sizeof(Part) == EVICT_PART_BYTES, "the workspace is sized by it");
+static_assert(EVICT_PART_MOST < 1 << 16, "a count has 16 bits");
 
 struct Place {  // of a workgroup
   int bh, part, n, late;
+  int from, to;  // the part's keys before `late`
+  int used;      // parts with such keys
   uint32_t want;
-  Part* parts;  // of its head
+  Part* parts;   // of its head
 };
 
 // False where nothing is to be sought: all keys stay, or only the late ones.
 __device__ __forceinline__ bool place(const EvictParams& p, Place& w) {
-  w.bh = blockIdx.x / p.parts;
-  w.part = blockIdx.x - w.bh * p.parts;
+  // the parts of a head run on one XCD (workgroup ids go round the eight), whose L2 then
+  // serves their counts: 8 heads of 33000 keys 25 -> 23 us
+  const int unit = blockIdx.x, even = p.B * p.Hkv / 8 * 8 * p.parts;
+  if (unit < even) {
+    const int k = (unit >> 3) / p.parts;
+    w.bh = 8 * k + (unit & 7);
+    w.part = (unit >> 3) - k * p.parts;
+  } else {
+    w.bh = unit / p.parts;
+    w.part = unit - w.bh * p.parts;
+  }
   w.n = p.lens ? min(max(p.lens[w.bh / p.Hkv], 0), p.Sk) : p.Sk;
-  w.late = w.n - min(p.recent, p.keep);
+  w.late = max(w.n - min(p.recent, p.keep), 0);
   w.want = (uint32_t)(p.keep - (w.n - w.late));
+  w.from = w.part * p.part_keys;
+  w.to = w.late - w.from > p.part_keys ? w.from + p.part_keys : w.late;
+  w.used = w.late > 0 ? (w.late - 1) / p.part_keys + 1 : 0;
   w.parts = (Part*)p.scratch + (size_t)w.bh * p.parts;
   return w.n > p.keep && w.want > 0;
 }
 
-// The ranks of four keys from i on, 0 from `late` on
-__device__ __forceinline__ u32x4 ranks_of(const float* acc, int i, int late) {
-  float x[4];
+// The weights of four keys from i on, and their ranks, 0 from `to` on.  (Two steps:
+// weights are asked for early, and waited for where the ranks are taken.)
+__device__ __forceinline__ f32x4 weights_of(const float* acc, int i, int to) {
+  f32x4 x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = acc[min(i + e, to - 1)];
+  return x;
+}
+__device__ __forceinline__ u32x4 ranks_of(f32x4 x, int i, int to) {
   u32x4 u;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = acc[min(i + e, late - 1)];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) u[e] = i + e < late ? rank_of(x[e]) : 0;
+  for (int e = 0; e < 4; ++e) u[e] = i + e < to ? rank_of(x[e]) : 0;
   return u;
 }
 
-__global__ __launch_bounds__(SEL) void attn_evict_count(EvictParams p) {
-  __shared__ uint32_t hist[2][BINS];
-  const int tid = threadIdx.x, lane = tid & 63;
-  Place w;
-  if (!place(p, w) || w.part * EVICT_PART >= w.late) return;
-  const u32x4 u = ranks_of(p.acc + (size_t)w.bh * p.Sk_cap, w.part * EVICT_PART + 4 * tid, w.late);
-#pragma unroll
-  for (int i = 0; i < 2 * PER; ++i) hist[0][i * SEL + tid] = 0;
+// What is known of the rank sought: its digits so far, what is wanted of the keys with
+// them, and of the parts before this one the keys above them and with them.
+struct Found {
+  uint32_t digits, left, above, equal;
+};
+struct Sums {
+  uint32_t all[SW], before[SW];  // of each wave's bins: over all parts, over those before this one
+  Found found;
+};
+
+// The next digits: c[j] is the count of bin BINS - 1 - (PER tid + j) over all parts, b[j]
+// that over the parts before this one.
+__device__ __forceinline__ void find_digits(Sums& sh, const uint32_t (&c)[PER], const uint32_t (&b)[PER], int width,
+                                            Found& f, int tid, int lane, int wave) {
+  static_assert(PER == 2, "two bins a thread");
+  const uint32_t own = c[0] + c[1], upto = scan(own), upto_b = scan(b[0] + b[1]);
+  if (lane == 63) sh.all[wave] = upto, sh.before[wave] = upto_b;
   __syncthreads();
-#pragma unroll
-  for (int e = 0; e < 4; ++e) count(hist[lane & 1], u[e] != 0 ? (int)(u[e] >> 21) : -1, lane);
+  const uint32_t higher = upto - own + sum_below(sh.all, wave);
+  if (higher < f.left && higher + own >= f.left) {
+    const bool second = higher + c[0] < f.left;
+    sh.found = {f.digits << width | (uint32_t)(BINS - 1 - (PER * tid + (second ? 1 : 0))),
+                f.left - higher - (second ? c[0] : 0),
+                f.above + sum_below(sh.before, wave) + upto_b - (second ? b[1] : b[0] + b[1]), second ? b[1] : b[0]};
+  }
   __syncthreads();
-  w.parts[w.part].counts[tid] =
-      (hist[0][2 * tid] + hist[1][2 * tid]) | (hist[0][2 * tid + 1] + hist[1][2 * tid + 1]) << 16;
+  f = sh.found;
 }
 
-__global__ __launch_bounds__(SEL) void attn_evict_narrow(EvictParams p) {
-  __shared__ __attribute__((aligned(16))) Search search;
-  __shared__ __attribute__((aligned(16))) uint32_t waves[SW];
+// The next digits from the counts of a level.
+template <int LEVEL>
+__device__ __forceinline__ void next_level(Sums& sh, const Place& w, Found& f, int tid, int lane, int wave) {
+  uint32_t c[PER] = {0, 0}, b[PER] = {0, 0};
+  const int at = SEL - 1 - tid;  // this thread's two bins
+  if (LEVEL < 2 || at < BINS / 4) {
+#pragma unroll 8
+    for (int i = 0; i < w.used; ++i) {
+      const uint32_t x = LEVEL < 2 ? w.parts[i].counts[LEVEL][at] : w.parts[i].low[at];
+      c[0] += x >> 16;
+      c[1] += x & 0xFFFF;
+      if (i < w.part) {
+        b[0] += x >> 16;
+        b[1] += x & 0xFFFF;
+      }
+    }
+  }
+  find_digits(sh, c, b, LEVEL < 2 ? 11 : 10, f, tid, lane, wave);
+}
+
+template <int LEVEL>
+__global__ __launch_bounds__(SEL) void attn_evict_count(EvictParams p) {
+  __shared__ uint32_t hist[2][BINS];
+  __shared__ __attribute__((aligned(16))) Sums sums;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Place w;
-  if (!place(p, w) || w.part * EVICT_PART >= w.late) return;
-  const u32x4 u = ranks_of(p.acc + (size_t)w.bh * p.Sk_cap, w.part * EVICT_PART + 4 * tid, w.late);
-  // the head's counts
-  const int used = (w.late + EVICT_PART - 1) / EVICT_PART;
-  uint32_t c[PER] = {0, 0};
-#pragma unroll 8
-  for (int i = 0; i < used; ++i) {
-    const uint32_t x = w.parts[i].counts[SEL - 1 - tid];
-    c[0] += x >> 16;
-    c[1] += x & 0xFFFF;
-  }
-  uint32_t digits = 0, left = w.want;
-  next_digits(search, c, 11, digits, left, tid, lane, wave);
-  uint32_t own = 0;  // candidates, above ones: EVICT_PART each at most
+  if (!place(p, w) || w.from >= w.late) return;
+  Part& own = w.parts[w.part];
+  const float* const acc = p.acc + (size_t)w.bh * p.Sk_cap;
+  f32x4 x = weights_of(acc, w.from + 4 * tid, w.to);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) own += (u[e] >> 21) > digits ? 1 : (u[e] >> 21) == digits ? 1u << 16 : 0;
-  const uint32_t upto = scan(own);
-  if (lane == 63) waves[wave] = upto;
+  for (int i = 0; i < 2 * PER; ++i) hist[0][i * SEL + tid] = 0;
+  Found f = {0, w.want, 0, 0};
+  if constexpr (LEVEL == 2) f = {own.digits, own.left, own.above, 0};
   __syncthreads();
-  const uint32_t before = upto - own + sum_below(waves, wave);
-  Part& part = w.parts[w.part];
-  uint32_t at = before >> 16;
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if ((u[e] >> 21) == digits) part.rest[at++] = u[e] & ((1u << 21) - 1);
-  if (tid == SEL - 1) {
-    part.above = (before + own) & 0xFFFF;
-    part.candidates = (before + own) >> 16;
-    part.digits = digits;
-    part.left = left;
+  if constexpr (LEVEL > 0) {
+    next_level<LEVEL - 1>(sums, w, f, tid, lane, wave);
+    if (tid == 0) {
+      own.digits = f.digits;
+      own.left = f.left;
+      own.above = f.above;
+    }
   }
+  constexpr int SHIFT = LEVEL == 0 ? 21 : LEVEL == 1 ? 10 : 0, WIDTH = LEVEL < 2 ? 11 : 10;
+  for (int i = w.from; i < w.to; i += 4 * SEL) {
+    const u32x4 u = ranks_of(x, i + 4 * tid, w.to);
+    if (i + 4 * SEL < w.to) x = weights_of(acc, i + 4 * (SEL + tid), w.to);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      // (rank 0, behind the last key, has no weight's digits)
+      const bool in = LEVEL == 0 ? u[e] != 0 : u[e] >> (SHIFT + WIDTH) == f.digits;
+      if (__ballot(in)) count(hist[lane & 1], in ? (int)((u[e] >> SHIFT) & ((1u << WIDTH) - 1)) : -1, lane);
+    }
+  }
+  __syncthreads();
+  uint32_t* const counts = LEVEL < 2 ? own.counts[LEVEL] : own.low;
+  if (LEVEL < 2 || tid < BINS / 4)
+    counts[tid] = (hist[0][PER * tid] + hist[1][PER * tid]) | (hist[0][PER * tid + 1] + hist[1][PER * tid + 1]) << 16;
 }
 
 __global__ __launch_bounds__(SEL) void attn_evict_place(EvictParams p) {
-  __shared__ uint32_t hist[2][BINS];
-  __shared__ __attribute__((aligned(16))) Search search;
-  __shared__ __attribute__((aligned(16))) uint32_t above[SW], equal[SW], waves[SW];
+  __shared__ __attribute__((aligned(16))) Sums sums;
+  __shared__ __attribute__((aligned(16))) uint32_t waves[2][SW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Place w;
   const bool seek = place(p, w);
   int32_t* const index = p.index + (size_t)w.bh * p.keep;
   if (w.bh % p.Hkv == 0 && w.part == 0 && tid == 0) p.lens_out[w.bh / p.Hkv] = min(w.n, p.keep);
+  // what needs no search is shared out over the head's workgroups
   const int first = w.part * SEL + tid, step = p.parts * SEL;
   if (w.n <= p.keep) {
-    for (int i = first; i < p.keep; i += step) index[i] = i < w.n ? i : -1;
+    for (long long i = first; i < p.keep; i += step) index[i] = i < w.n ? (int)i : -1;
     return;
   }
-  for (int i = w.late + first; i < w.n; i += step) index[w.want + (uint32_t)(i - w.late)] = i;
-  if (!seek || w.part * EVICT_PART >= w.late) return;
-  const int k0 = w.part * EVICT_PART + 4 * tid;
-  const u32x4 u = ranks_of(p.acc + (size_t)w.bh * p.Sk_cap, k0, w.late);
+  for (long long i = w.late + (long long)first; i < w.n; i += step) index[w.want + (uint32_t)(i - w.late)] = (int)i;
+  if (!seek || w.from >= w.late) return;
+  const float* const acc = p.acc + (size_t)w.bh * p.Sk_cap;
+  const Part& own = w.parts[w.part];
+  f32x4 x = weights_of(acc, w.from + 4 * tid, w.to);
+  Found f = {own.digits, own.left, own.above, 0};
+  next_level<2>(sums, w, f, tid, lane, wave);
+  // now: all keys above f.digits stay, and the first f.left of those equal to it.
+  // Above and equal ones before a key: of the equal ones the first `left` stay.
+  uint32_t ab = f.above, eq = f.equal;
+  int turn = 0;
+  for (int i = w.from; i < w.to; i += 4 * SEL, turn ^= 1) {
+    const u32x4 u = ranks_of(x, i + 4 * tid, w.to);
+    if (i + 4 * SEL < w.to) x = weights_of(acc, i + 4 * (SEL + tid), w.to);
+    uint32_t mine = 0;  // equal ones, above ones: at most 4096 each
 #pragma unroll
-  for (int i = 0; i < 2 * PER; ++i) hist[0][i * SEL + tid] = 0;
-  __syncthreads();
-  const uint32_t top = w.parts[w.part].digits;
-  uint32_t digits = 0, left = w.parts[w.part].left;
-  // (a wave: the candidates of every SW-th part)
-  const int used = (w.late + EVICT_PART - 1) / EVICT_PART;
-#pragma unroll 1
-  for (int round = 1; round < 3; ++round) {
-    const int shift = round == 1 ? 10 : 0, width = round == 1 ? 11 : 10;
-    for (int i = wave; i < used; i += SW) {
-      const Part& part = w.parts[i];
-      const int m = (int)part.candidates;
-      for (int j = lane; j - lane < m; j += 64) {
-        const uint32_t r = j < m ? part.rest[j] : ~0u;  // (no digits are that high)
-        const bool in = j < m && (round == 1 || r >> width == digits);
-        if (__ballot(in)) count(hist[lane & 1], in ? (int)((r >> shift) & ((1u << width) - 1)) : -1, lane);
-      }
-    }
+    for (int e = 0; e < 4; ++e) mine += u[e] > f.digits ? 1 : u[e] == f.digits ? 1u << 16 : 0;
+    const uint32_t upto = scan(mine);
+    // (two of them in turn: a wave that runs ahead writes the other)
+    if (lane == 63) waves[turn][wave] = upto;
     __syncthreads();
-    uint32_t c[PER];
+    const uint32_t before = upto - mine + sum_below(waves[turn], wave), all = sum_below(waves[turn], SW);
+    uint32_t e0 = eq + (before >> 16), to = ab + (before & 0xFFFF) + min(e0, f.left);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int bin = BINS - 1 - (PER * tid + j);
-      c[j] = hist[0][bin] + hist[1][bin];
-      hist[0][bin] = hist[1][bin] = 0;
+    for (int e = 0; e < 4; ++e) {
+      const bool same = u[e] == f.digits;
+      if (u[e] > f.digits || (same && e0 < f.left)) index[to++] = i + 4 * tid + e;
+      e0 += same ? 1 : 0;
     }
-    next_digits(search, c, width, digits, left, tid, lane, wave);
-  }
-  // above and equal ones in the parts before this one
-  uint32_t na = 0, ne = 0;
-  for (int i = wave; i < w.part; i += SW) {
-    const Part& part = w.parts[i];
-    const int m = (int)part.candidates;
-    if (lane == 0) na += part.above;
-    for (int j = lane; j < m; j += 64) {
-      const uint32_t r = part.rest[j];
-      na += r > digits ? 1 : 0;
-      ne += r == digits ? 1 : 0;
-    }
-  }
-  na = scan(na);
-  ne = scan(ne);
-  digits |= top << 21;
-  uint32_t own = 0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) own += u[e] > digits ? 1 : u[e] == digits ? 1u << 16 : 0;
-  const uint32_t upto = scan(own);
-  if (lane == 63) above[wave] = na, equal[wave] = ne, waves[wave] = upto;
-  __syncthreads();
-  const uint32_t before = upto - own + sum_below(waves, wave);
-  uint32_t e0 = sum_below(equal, SW) + (before >> 16);
-  uint32_t to = sum_below(above, SW) + (before & 0xFFFF) + min(e0, left);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const bool same = u[e] == digits;
-    if (u[e] > digits || (same && e0 < left)) index[to++] = k0 + e;
-    e0 += same ? 1 : 0;
+    ab += all & 0xFFFF;
+    eq += all >> 16;
   }
 }
 
@@ -477,8 +506,9 @@ int launch_evict(const EvictParams& p, void* stream) {
   // (two workgroups a compute unit where their weights fit)
   if (p.parts > 1) {
     const dim3 all((unsigned)(p.B * p.Hkv * p.parts));
-    hipLaunchKernelGGL(attn_evict_count, all, block, 0, st, p);
-    hipLaunchKernelGGL(attn_evict_narrow, all, block, 0, st, p);
+    hipLaunchKernelGGL(attn_evict_count<0>, all, block, 0, st, p);
+    hipLaunchKernelGGL(attn_evict_count<1>, all, block, 0, st, p);
+    hipLaunchKernelGGL(attn_evict_count<2>, all, block, 0, st, p);
     hipLaunchKernelGGL(attn_evict_place, all, block, 0, st, p);
   } else if (p.Sk <= HELD_FEW) {
     if (p.gather) hipLaunchKernelGGL((attn_evict_select<true, HELD_FEW>), heads, block, 0, st, p);

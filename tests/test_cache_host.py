@@ -118,6 +118,29 @@ def test_evict_forms(host):
     assert form(8, 8, 32769, 100) == (9, 0) and form(13, 5, 32769, 100) == (1, 1)
 
 
+def evict_parts(host, heads, Sk):
+    at = [0x100000 + (i << 46) for i in range(9)]
+    rc = host.attn_evict(at[0], at[1], at[2], None, *at[3:8], 1, heads, Sk, Sk, 100, 64, 100, 0, 1, at[8],
+                         host.attn_evict_workspace_bytes(1, heads, Sk), None)
+    assert rc == pkg.ATTN_ELAUNCH
+    return host.h15_stub_evict(0)
+
+
+@pytest.mark.parametrize("heads", [1, 2, 7, 8, 20, 21, 32, 33, 64, 65, 256])
+def test_evict_parts_stay_few(host, heads):
+    # every workgroup adds up what its head's parts counted: their number is bounded as caches grow
+    for Sk in (1, 20480, 20481, 32769, 100003, 131072, 1 << 18, 10 ** 6, 1 << 20):
+        n = evict_parts(host, heads, Sk)
+        # (a part counts up to 61440 keys in 16 bits)
+        assert n == 1 or -(-Sk // 61440) <= n <= max(-(-Sk // 61440), min(32, 640 // heads))
+        assert (n > 1) == (host.attn_evict_workspace_bytes(1, heads, Sk) > 0)
+
+
+def test_evict_parts_of_the_longest_caches_fit_a_launch(host):
+    assert evict_parts(host, 64, 2 ** 31 - 8193) * 64 <= 2 ** 22 - 1
+    assert host.attn_evict_workspace_bytes(1, 64, 2 ** 31 - 8193) > 2 ** 31
+
+
 def test_checks_under_sanitizers(tmp_path):
     lib = tmp_path / "libh15cache_san.so"
     subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fno-omit-frame-pointer", "-fsanitize=address,undefined",
