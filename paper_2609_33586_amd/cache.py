@@ -98,6 +98,13 @@ def _call_opts(descale, stream):
     return attn_opts(float(qd), float(kd), float(vd), handle, 0.0, 0)
 
 
+def _refuse(**sizes):
+    """Sizes go to the library in 32 bits, and ctypes cuts off what lies beyond (negative ones the library refuses)."""
+    for name, n in sizes.items():
+        if not -2 ** 31 <= n < 2 ** 31:
+            raise ValueError(f"{name} is out of range: {n}")
+
+
 def _lens_ptr(lens, B, dev):
     return None if lens is None else _tensor("lens", lens, (B,), dev, _torch.int32).data_ptr()
 
@@ -160,6 +167,8 @@ def attn_decode_prefix(q, kp, vp, k, v, *, causal: bool, scale: float, exp_mode:
         vpptr = _operand("vp", vp, shape, dev, first, dt).data_ptr()
     P = P_cap if P is None else int(P)
     Sk = Sk_cap if Sk is None else int(Sk)
+    if (P | Sk | prefix_split_keys | split_keys) >> 31:
+        _refuse(P=P, Sk=Sk, prefix_split_keys=prefix_split_keys, split_keys=split_keys)
     if out is None or lse is None:
         out, lse = _outputs(q, out, lse, want_lse, stream)
     else:
@@ -196,6 +205,8 @@ def attn_key_weights(q, k, lse, acc, *, causal: bool, scale: float, decay: float
     _tensor("lse", lse, (B, Hq, Sq), dev, _torch.float32)
     _tensor("acc", acc, (B, Hkv, cap), dev, _torch.float32)
     Sk = cap if Sk is None else int(Sk)
+    if Sk >> 31:
+        _refuse(Sk=Sk)
     wptr, wbytes, workspace = _space(workspace, lambda: L.attn_key_weights_workspace_bytes(B, Hq, Hkv, Sq, Sk, d), dev,
                                      stream)
     if descale is not None:
@@ -228,7 +239,9 @@ def attn_evict(k, v, acc, *, keep: int, recent: int, lens=None, Sk: int | None =
     dt = _dtype_of(k)
     _operand("v", v, shape, dev, first, dt)
     _tensor("acc", acc, (B, Hkv, cap), dev, f32)
-    Sk, keep = cap if Sk is None else int(Sk), int(keep)
+    Sk, keep, recent = cap if Sk is None else int(Sk), int(keep), int(recent)
+    if (Sk | keep | recent) >> 31:
+        _refuse(Sk=Sk, keep=keep, recent=recent)
     rows = max(keep, 1)
     given = k_out if k_out is not None else v_out
     out_cap = rows if given is None else _four("k_out", given)[2]
@@ -245,7 +258,7 @@ def attn_evict(k, v, acc, *, keep: int, recent: int, lens=None, Sk: int | None =
     opts = _call_opts(None, stream)
     rc = L.attn_evict(k.data_ptr(), v.data_ptr(), acc.data_ptr(), _lens_ptr(lens, B, dev), k_out.data_ptr(),
                       v_out.data_ptr(), acc_out.data_ptr(), index.data_ptr(), lens_out.data_ptr(), B, Hkv, Sk, cap,
-                      out_cap, d, keep, int(recent), dt, wptr, wbytes, ctypes.byref(opts))
+                      out_cap, d, keep, recent, dt, wptr, wbytes, ctypes.byref(opts))
     if rc != ATTN_OK:
         raise AttnError(rc, "attn_evict")
     return k_out, v_out, acc_out, index, lens_out

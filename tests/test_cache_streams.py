@@ -118,3 +118,23 @@ def test_memory_comes_from_the_stream_that_the_call_runs_on(pool, name):
 def test_calls_on_the_current_stream_take_its_memory(pool, name):
     CALLS[name][0](None)
     assert len(pool) > 0 and all(t.owner is pool.current and t.waits == [] for t in pool)
+
+
+# (as h15cache.h counts them, in 32 bits: a number beyond would come out as another one)
+@pytest.mark.parametrize("name,call", [
+    ("P", lambda x: pkg.attn_decode_prefix(Q, P, P, KV, KV, exp_mode=1, prefix_split_keys=0, split_keys=0, P=x, **KW)),
+    ("Sk", lambda x: pkg.attn_decode_prefix(Q, P, P, KV, KV, exp_mode=1, prefix_split_keys=0, split_keys=0, Sk=x, **KW)),
+    ("prefix_split_keys", lambda x: pkg.attn_decode_prefix(Q, P, P, KV, KV, exp_mode=1, prefix_split_keys=x, split_keys=0,
+                                                           **KW)),
+    ("split_keys", lambda x: pkg.attn_decode_prefix(Q, P, P, KV, KV, exp_mode=1, prefix_split_keys=0, split_keys=x, **KW)),
+    ("Sk", lambda x: pkg.attn_key_weights(Q, KV, LSE, ACC, Sk=x, **KW)),
+    ("Sk", lambda x: pkg.attn_evict(KV, KV, ACC, keep=20, recent=3, Sk=x)),
+    ("keep", lambda x: pkg.attn_evict(KV, KV, ACC, keep=x, recent=3)),
+    ("recent", lambda x: pkg.attn_evict(KV, KV, ACC, keep=20, recent=x)),
+])
+def test_sizes_beyond_32_bits_are_refused(pool, name, call):
+    for x in (2 ** 31, 2 ** 32, 2 ** 32 + 128, -2 ** 31 - 1, -2 ** 32 + 5):
+        with pytest.raises(ValueError, match=f"^{name} "):
+            call(x)
+    call(128)
+    assert all(t.shape.numel() < 2 ** 31 for t in pool)
