@@ -22,6 +22,11 @@
  * lens: keys in each sequence's own cache, int32 [B] on the device (NULL: Sk
  * in every one).  The values are read by the kernels: one below 0 counts as 0,
  * one above Sk as Sk.  Rows of a cache from lens[b] on are never read.
+ *
+ * Operands are finite, as in attn_decode.  Infinities and NaN in a sequence's
+ * rows of q, k and v reach no other sequence (those of the prefix reach all),
+ * but within it: in v, also the rows that do not see that key, with the
+ * weight 0; the lattice weights give a logit of NaN the least weight there is.
  */
 #ifndef H15CACHE_H
 #define H15CACHE_H
@@ -60,8 +65,10 @@ extern "C" {
  * NULL).  exp_mode: ATTN_EXP_EXACT, H15, SQ4 or SQ8; the rescale threshold
  * must be 0.
  *
- * workspace: attn_decode_prefix_workspace_bytes() bytes, 16-byte aligned; it
- * needs no initialising; two calls in flight at once must not share it.
+ * workspace: attn_decode_prefix_workspace_bytes() bytes, 16-byte aligned, for
+ * more than one part (also where a short prefix is taken together with the own
+ * caches, and nothing is written to it); it needs no initialising; two calls
+ * in flight at once must not share it.
  *
  * Errors: ATTN_EINVAL for a null pointer, a size that is not positive
  * (P, Sk: negative, or both 0), P > P_cap, Sk > Sk_cap, Hq % Hkv != 0, a scale
@@ -96,10 +103,18 @@ int attn_decode_prefix_split_keys(int B, int Hq, int Hkv, int Sq, int P, int Sk,
  *
  * for j < n = lens[b]; acc beyond is left as it was.  Position i sees the keys
  * j <= n - Sq + i when causal, every key otherwise.  lse is what an attention
- * call returned for these rows (any entry point and exp_mode; with a prefix
- * the weights are shares of the whole, own keys only being counted); a row
- * with lse = -inf gives nothing, whatever its q holds.  decay = 1 accumulates;
- * with decay = 0 the old values are not read.  decay must be finite and >= 0.
+ * call returned for these rows (any entry point; with a prefix the weights are
+ * shares of the whole, own keys only being counted); a row with lse = -inf
+ * gives nothing, whatever its q holds.
+ *
+ * The exponential is the exact one: with lse of ATTN_EXP_EXACT these are the
+ * weights of that call, and a row's add up to 1.  With lse of a lattice mode
+ * they are not the lattice weights, which differ from them by the map's own
+ * error (a factor of 0.84 to 1.26 for H15, 0.92 to 1.16 for SQ4, 0.96 to 1.11
+ * for SQ8), and a row adds up to the ratio of the two normalisers.
+ *
+ * decay = 1 accumulates; with decay = 0 the old values are not read.  decay
+ * must be finite and >= 0.
  *
  * Sums are in FP32 (of FP32 logits), in a fixed order: results are
  * deterministic.

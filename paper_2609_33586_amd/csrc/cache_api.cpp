@@ -87,7 +87,8 @@ bool chained(int P, int row_bytes, const PrefixParams& p) {
 // one for each slot (two workgroups a compute unit, one of them the prefix's), so
 // that no long one starts last (32 heads over 8; in their own order / so: 128 caches of
 // up to 2K keys after 8K BF16 156 / 150 us, 64 92 / 87; up to 8K after 32K FP8 180 / 170,
-// 2K level).  With a slot each there is nothing to order.
+// 2K level).  With a slot each there is nothing to order; more than 256 caches, whose
+// lengths a workgroup does not rank with a thread each, keep their own order.
 bool by_length(const PrefixParams& p) {
   const int slots = 512 - (p.p_groups < 256 ? p.p_groups : 256);
   return p.lens && p.B > 1 && p.B <= 256 && p.o_groups > slots;
@@ -161,6 +162,8 @@ extern "C" {
 
 int attn_decode_prefix_split_keys(int B, int Hq, int Hkv, int Sq, int P, int Sk, int d, int dtype,
                                   int* prefix_split_keys, int* split_keys) {
+  // (parts are counted in tiles, whatever a tile's bytes are: a cut of one type is
+  // one of all, and lattice weights, which depend on it, compare across them)
   (void)d;
   (void)dtype;
   if (!prefix_split_keys || !split_keys) return ATTN_EINVAL;

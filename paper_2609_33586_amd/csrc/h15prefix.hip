@@ -22,11 +22,14 @@
 // A workgroup of an own cache may take a short prefix first, in the keys form:
 // one launch and nothing to merge.  (The rules between these: cache_api.cpp.)
 //
-// What bounds it: HBM for BF16 (32 sequences of 32 heads over 8 KV heads, 8K
-// prefix, up to 1K own keys: 29 us + 4 of the merge for 115 MB; 64 such with 32K
-// and 2K keys each: 143 us for 671 MB, 4.7 TB/s).  A keys round of 128 BF16 keys
-// takes 3900 cycles, of which 750 wait for K; two workgroups share a compute
-// unit.  FP8 with many rows: a rows tile takes 5900 cycles, 1500 for Q K^T, 1900
+// What bounds it: HBM where there is enough to read (BF16, 64 sequences of 32 heads
+// over 8 KV heads, 32K prefix and 2K own keys: 143 us for 671 MB, 4.7 TB/s).  With
+// fewer keys the rounds of a workgroup, one after the other (32 such sequences, 8K
+// prefix, up to 1K own keys: 29 us + 4 of the merge for 115 MB): its 512 workgroups
+// start within 0.2 us, two on a compute unit, and ask for 33 MB at once; those of the
+// prefix have their first keys after 2.4 us, the own ones after 5 on average and 10
+// at most; a round of 128 keys then takes 2 us (3900 cycles, of which 750 wait for K),
+// the last of 8 ends after 18 and 20..26 us, the reduction takes 1 to 2.  FP8 with many rows: a rows tile takes 5900 cycles, 1500 for Q K^T, 1900
 // for the weights and 1800 for P V (1024 of the matrix core each) in turn, next
 // to one workgroup of own caches (64 sequences, 32K prefix, 2K own keys: 66 us +
 // 6 for 230 MB).  Widening each FP8 tile once for the four waves, through
@@ -35,15 +38,17 @@
 // 25 -> 36 us).  Two FP8 tiles in LDS at a time, with a tile's time for their copies
 // and one barrier, V's reads in half as many waits, and a higher wave priority of one
 // kind of workgroup were level (66 -> 66..72 us): the waits are filled by the other
-// workgroup.  Short caches wait: 4 chats of 500 + 60 keys BF16 d = 64 take 8.8 us
-// in one launch, 11 with the call.
+// workgroup.  Short caches wait: 4 chats of 500 + 60 keys BF16 d = 64 take 8.9 us
+// in one launch (10.5 with the call), three rounds in series on 8 workgroups.
 //
 // Arithmetic: that of attn_decode for BF16.  FP8 operands are widened to BF16,
 // which holds every e4m3 value, and meet in the BF16 matrix core: the FP8
 // products sum to about 2^-13 of sum |q k| (64 deep, attn_decode's) or 2^-16
 // (16 deep), and P, rounded to BF16 here (half a step of 2^-8 of it at most),
-// would be off by up to 2^-4 in e4m3, 2.6% rms a weight.  Lattice weights are
-// exact in BF16.
+// would be off by up to 2^-4 in e4m3, 2.6% rms a weight.  The matrix core takes
+// no wider P; the weights' sum takes them unrounded.  With the hardware exponential O
+// is off by 2.1e-3 of its norm (500 keys; 32K 2.3e-3), of which rounding O itself
+// to BF16 is 1.7e-3.  Lattice weights are exact in BF16.
 #include "cache_params.h"
 #include "unit_device.h"
 
