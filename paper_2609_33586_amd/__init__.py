@@ -224,7 +224,11 @@ def attn_fwd(q, k, v, *, causal: bool, scale: float, exp_mode: int, out=None, ls
              want_lse: bool = True):
     """attn_fwd on the default stream with unit descales."""
     B, Hq, Hkv, S, d, dt = _check(q, k, v)
-    out, lse = _outputs(q, out, lse, want_lse)
+    stream = None
+    if (out is None or lse is None) and _current_stream():  # (not 0: another than the default one)
+        import torch
+        stream = torch.cuda.default_stream()
+    out, lse = _outputs(q, out, lse, want_lse, stream)
     rc = lib().attn_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                         lse.data_ptr() if lse is not None else None, B, Hq, Hkv, S, d,
                         int(bool(causal)), float(scale), dt, int(exp_mode))

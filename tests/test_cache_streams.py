@@ -138,3 +138,13 @@ def test_sizes_beyond_32_bits_are_refused(pool, name, call):
             call(x)
     call(128)
     assert all(t.shape.numel() < 2 ** 31 for t in pool)
+
+
+def test_attn_fwd_takes_its_outputs_where_it_runs(pool, monkeypatch):
+    # on the default stream, whatever the current one is
+    default = Stream(0)
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda *a: default)
+    for t in pkg.attn_fwd(Q, Q, Q, exp_mode=1, **KW):
+        assert t.owner is default and t.waits == [pool.current]
+    pool.current = default
+    assert all(t.owner is default for t in pkg.attn_fwd(Q, Q, Q, exp_mode=1, **KW))

@@ -86,3 +86,22 @@ def test_pending_work_of_the_current_stream_keeps_its_memory(call):
     torch.cuda.synchronize()
     for b in fresh:
         assert bool((b == 9).all())
+
+
+def test_attn_fwd_runs_on_the_default_stream_with_memory_of_its_own():
+    q = OPERANDS["forward"]
+    kw = dict(causal=True, scale=scale_of(128), exp_mode=H15)
+    want = pkg.attn_fwd(q, q, q, **kw)
+    side, a = torch.cuda.Stream(), torch.randn(4096, 4096, device="cuda")
+    sizes = [t.numel() * t.element_size() for t in want]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        blocks = [torch.full((n,), 7, dtype=torch.uint8, device="cuda") for n in sizes]
+        for _ in range(40):  # keeps the side stream busy
+            a = a @ a * 1e-3
+        copies = [b.clone() for b in blocks]
+        del blocks
+        got = pkg.attn_fwd(q, q, q, **kw)
+    torch.cuda.synchronize()
+    assert all(bool((c == 7).all()) for c in copies)
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
