@@ -65,11 +65,13 @@ def _operand(name, t, shape, dev, first, dt):
     return t
 
 
-def _current_gpu(name, t) -> int:
-    """The number of t's device, which has to be the current one."""
+def _current_gpu(name, t, stream) -> int:
+    """The number of t's device, which has to be the current one, and the stream's, if one is given."""
     dev = t.get_device()
     if dev < 0 or dev != _device():
         raise ValueError(f"{name} must be on the current GPU")
+    if stream is not None and stream.device_index != dev:
+        raise ValueError(f"stream must belong to GPU {dev}")
     return dev
 
 
@@ -150,7 +152,7 @@ def attn_decode_prefix(q, kp, vp, k, v, *, causal: bool, scale: float, exp_mode:
     if (k is None) != (v is None) or (kp is None) != (vp is None):
         raise ValueError("k and v, kp and vp: both or neither")
     B, Hq, Sq, d = shape = _four("q", q)
-    dev, first = _current_gpu("q", q), q.dtype
+    dev, first = _current_gpu("q", q, stream), q.dtype
     dt = _dtype_of(q)
     Hkv = P_cap = Sk_cap = 0
     kptr = vptr = kpptr = vpptr = None
@@ -199,7 +201,7 @@ def attn_key_weights(q, k, lse, acc, *, causal: bool, scale: float, decay: float
     returned.  descale: (q, k) or (q, k, v) factors of FP8 operands."""
     L = _lib()
     B, Hq, Sq, d = shape = _four("q", q)
-    dev = _current_gpu("q", q)
+    dev = _current_gpu("q", q, stream)
     dt = _dtype_of(q)
     Hkv, cap = _cache("k", k, B, d, dev, q.dtype, dt)
     _tensor("lse", lse, (B, Hq, Sq), dev, _torch.float32)
@@ -235,7 +237,7 @@ def attn_evict(k, v, acc, *, keep: int, recent: int, lens=None, Sk: int | None =
     Rows of the outputs from lens_out[b] on are left as they were."""
     L = _lib()
     B, Hkv, cap, d = shape = _four("k", k)
-    dev, first, f32, i32 = _current_gpu("k", k), k.dtype, _torch.float32, _torch.int32
+    dev, first, f32, i32 = _current_gpu("k", k, stream), k.dtype, _torch.float32, _torch.int32
     dt = _dtype_of(k)
     _operand("v", v, shape, dev, first, dt)
     _tensor("acc", acc, (B, Hkv, cap), dev, f32)

@@ -12,8 +12,8 @@ from paper_2609_33586_amd import cache
 
 
 class Stream:
-    def __init__(self, handle):
-        self.cuda_stream = handle
+    def __init__(self, handle, device=0):
+        self.cuda_stream, self.device_index = handle, device
 
 
 class Tensor:
@@ -148,3 +148,10 @@ def test_attn_fwd_takes_its_outputs_where_it_runs(pool, monkeypatch):
         assert t.owner is default and t.waits == [pool.current]
     pool.current = default
     assert all(t.owner is default for t in pkg.attn_fwd(Q, Q, Q, exp_mode=1, **KW))
+
+
+@pytest.mark.parametrize("name", ["attn_decode_prefix", "attn_key_weights", "attn_evict"])
+def test_streams_of_another_device_are_refused(pool, name):
+    with pytest.raises(ValueError, match="stream must belong to GPU 0"):
+        CALLS[name][0](Stream(3, device=1))
+    assert not pool  # before anything is taken
