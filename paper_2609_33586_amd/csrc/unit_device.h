@@ -117,12 +117,13 @@ __device__ __forceinline__ void read_v8(i32x2v (&r)[4], uint32_t a0, uint32_t a1
       : "memory");
 }
 
-// Eight e4m3 values as BF16 (exact: BF16 holds every one).
-__device__ __forceinline__ bf16x8 widen(int lo, int hi) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+// Eight e4m3 values as BF16 (exact: BF16 holds every one), times a scale of two
+// (2^-126 and more; products below that become 0).
+__device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale = 1.0f) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
