@@ -347,3 +347,9 @@ def attn_decode_probe(q, k, v, *, causal: bool, scale: float, exp_mode: int, spl
 
 from .cache import (attn_decode_prefix, attn_decode_prefix_split_keys, attn_decode_prefix_workspace_bytes,  # noqa: E402
                     attn_evict, attn_evict_workspace_bytes, attn_key_weights, attn_key_weights_workspace_bytes)
+
+# ---- between projections and attention (include/h15qkv.h) --------------------
+
+from .qkv import (ATTN_FP32, attn_cache_append, attn_decode_blocks, attn_decode_blocks_split_keys,  # noqa: E402
+                  attn_decode_blocks_workspace_bytes, attn_rope, attn_rope_bwd, attn_rope_bwd_workspace_bytes,
+                  attn_rope_frequencies)

@@ -26,6 +26,11 @@ CACHE_API_SRC = PKG / "csrc" / "cache_api.cpp"
 PREFIX_SRC = PKG / "csrc" / "h15prefix.hip"
 WEIGHTS_SRC = PKG / "csrc" / "h15weights.hip"
 EVICT_SRC = PKG / "csrc" / "h15evict.hip"
+# the operators between projections and attention and over 8-bit blocks: entry points and kernels
+QKV_API_SRC = PKG / "csrc" / "qkv_api.cpp"
+ROPE_SRC = PKG / "csrc" / "h15rope.hip"
+APPEND_SRC = PKG / "csrc" / "h15append.hip"
+BLOCKS_SRC = PKG / "csrc" / "h15blocks.hip"
 INCLUDE = ROOT / "include"
 LIB_PATH = PKG / "libh15attn.so"
 ARCH = "gfx950"
@@ -57,6 +62,10 @@ UNITS = [
     ("prefix", PREFIX_SRC, []),
     ("weights", WEIGHTS_SRC, []),
     ("evict", EVICT_SRC, []),
+    ("qkv_api", QKV_API_SRC, []),
+    ("rope", ROPE_SRC, []),
+    ("append", APPEND_SRC, []),
+    ("blocks", BLOCKS_SRC, []),
 ]
 
 

@@ -1,0 +1,533 @@
+// Attention over a cache of 8-bit codes with a scale of two for each block of
+// tokens and head (attn_decode_blocks): Sq BF16 query rows per head and sequence
+// against the first lens[b] slots of its cache, cut into parts that a second
+// launch merges.
+//
+// Codes become BF16 operands by the conversion that also multiplies by a scale
+// of two, so that the scales cost a read of two bytes a block and nothing in the
+// inner loops.  K's rows meet them one scale a lane, V's transposed operands one
+// for each 16 keys, which never straddle a block.
+//
+// Two forms of a workgroup (4 waves), those of attn_decode_prefix:
+//   keys  32 query rows; each wave takes its own 64 keys of a round, copies them
+//         into its own LDS slots and exchanges only the maxima of its units with
+//         the others (one barrier a round); a weight is rounded relative to the
+//         running maximum at its own tile, the prefix maximum of the round's units;
+//   rows  128 query rows, 32 a wave; the waves share each tile of 128 keys.
+#include "qkv_params.h"
+#include "part_device.h"
+
+namespace {
+
+constexpr int NW = 4;  // waves per workgroup
+
+template <int D>
+struct BCfg {
+  static constexpr int RB = D, NCH = D / 16;  // bytes and chunks of a row of codes
+  static constexpr int UNIT = 64, NB = 2;     // keys of a wave and round (keys form), blocks of 32
+  static constexpr int TPR = NW * UNIT / BC;  // tiles in a round
+  static constexpr int SLOT = UNIT * RB;      // one wave's K (or V) of a round
+  static constexpr int TILE = BC * RB;
+  // K (and V) area of LDS: the slots of a round (a tile is half of it), or half
+  // of the waves' O rows in the keys form's final reduction
+  static constexpr int RED = NW * 16 * D * 4;
+  static constexpr int AREA = NW * SLOT > RED ? NW * SLOT : RED;
+};
+
+// Query rows as operands in the order of the codes' 16-byte chunks.
+template <int D>
+__device__ __forceinline__ void load_q(RowOperand<DT_FP8, D>& q, const uint8_t* row, int g) {
+#pragma unroll
+  for (int t = 0; t < q.CHUNKS; ++t) {
+    const uint8_t* at = row + 64 * t + 32 * g;
+    q.x[2 * t] = __builtin_bit_cast(bf16x8, *(const i32x4*)at);
+    q.x[2 * t + 1] = __builtin_bit_cast(bf16x8, *(const i32x4*)(at + 16));
+  }
+}
+
+// acc + chunk t of the keys (16 bytes a lane), times their scale, times the rows q
+template <int D>
+__device__ __forceinline__ f32x16 product(i32x4 k, float scale, const RowOperand<DT_FP8, D>& q, int t, f32x16 acc) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(k[0], k[1], scale), q.x[2 * t], acc, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(k[2], k[3], scale), q.x[2 * t + 1], acc, 0, 0, 0);
+}
+
+// O^T += V^T P^T over 64 keys, two column blocks at once
+template <int D>
+__device__ __forceinline__ void add_pv(f32x16& o0, f32x16& o1, uint32_t a0, uint32_t a1, const bf16x8 (&pb)[4],
+                                       const float (&scale)[4]) {
+  i32x2v r[8];
+  read_v8<D>(r, a0, a1);
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) {
+    o0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(r[ks][0], r[ks][1], scale[ks]), pb[ks], o0, 0, 0, 0);
+    o1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(r[4 + ks][0], r[4 + ks][1], scale[ks]), pb[ks], o1, 0, 0, 0);
+  }
+}
+
+// A workgroup's share: query rows of one sequence and KV head against one part
+// of its keys.
+struct Work {
+  const uint8_t* k;  // the part's first key row, and its value row
+  const uint8_t* v;
+  const uint8_t* scales;  // of the head
+  int used;   // bytes of them that belong to slots that are filled
+  int j0;     // the part's first key
+  int nk;     // its keys that some row sees
+  int part, b, h;
+  int row0, nrows;  // its rows of the sequence's R
+  int open;   // the keys from here on (in the part) are not seen by every row
+  int last0;  // last key (in the part) that position 0 sees, or nk - 1
+};
+
+// The scales of a lane's keys (low byte: K's, high: V's) at key `key` of the head;
+// blocks without a filled slot read as 0.
+__device__ __forceinline__ int scale_pair(const BlocksParams& p, const __amdgpu_buffer_rsrc_t rsrc, int key) {
+  return __builtin_amdgcn_raw_buffer_load_b16(rsrc, (key >> p.shift) * 2, 0, 0);
+}
+__device__ __forceinline__ float scale_of(int byte) { return __uint_as_float((uint32_t)min(max(byte, 1), 254) << 23); }
+
+// V's scale of 16 keys from the lane that holds their first
+__device__ __forceinline__ float v_scale(int pair, int lane) {
+  return scale_of((__builtin_amdgcn_readlane(pair, lane) >> 8) & 255);
+}
+
+__device__ __forceinline__ size_t out_row(const BlocksParams& p, const Work& w, int r) {
+  return ((size_t)w.b * p.Hq + (size_t)w.h * p.G) * (size_t)p.Sq + w.row0 + r;
+}
+
+// Last key of the part that row r of the workgroup sees
+__device__ __forceinline__ int row_limit(const BlocksParams& p, const Work& w, int r) {
+  return p.causal ? min(w.last0 + (w.row0 + r) % p.Sq, w.nk - 1) : w.nk - 1;
+}
+
+template <int D, int MODE>
+__device__ __forceinline__ void keys_form(const BlocksParams& p, const Work& w, uint8_t* ksm, uint8_t* vsm,
+                                          float (*mx_lds)[32][NW], float (*m_lds)[NW], float (*l_lds)[NW]) {
+  using C = BCfg<D>;
+  constexpr int NB = C::NB, UNIT = C::UNIT, TPR = C::TPR, SLOT = C::SLOT, RB = C::RB;
+  constexpr int NDB = D / 32, LOADS = SLOT / 1024, RHALF = 16;
+  const int tid = threadIdx.x, lane = tid & 63, i32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rowc = min(i32, w.nrows - 1);
+  RowOperand<DT_FP8, D> q;
+  load_q<D>(q, p.q + out_row(p, w, rowc) * (2 * D), g);
+  const int limit = row_limit(p, w, rowc);
+  // rows beyond the part read as zero without touching memory; scalar offsets
+  // stop at the resource's size, where every lane is out of range
+  const uint32_t part_bytes = (uint32_t)w.nk * RB;
+  const auto krsrc = rows_rsrc(w.k, part_bytes), vrsrc = rows_rsrc(w.v, part_bytes);
+  const auto srsrc = rows_rsrc(w.scales, w.used);
+  uint8_t* const kslot = ksm + wave * SLOT;
+  uint8_t* const vslot = vsm + wave * SLOT;
+  // the chunk swizzles repeat after every fourth copy at the latest
+  uint32_t koff[4], voff[2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = copy_row<C::NCH>(i, lane);
+    koff[i] = (r - i * (64 / C::NCH)) * RB + (((lane % C::NCH) ^ k_swz<DT_FP8, D>(r)) << 4);
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = copy_row<C::NCH>(i, lane);
+    voff[i] = (r - i * (64 / C::NCH)) * RB + (((lane % C::NCH) ^ v_swz<DT_FP8, D>(r)) << 4);
+  }
+  auto first_key = [&](int c) { return c * (TPR * BC) + wave * UNIT; };
+  auto stage = [&](const __amdgpu_buffer_rsrc_t rsrc, uint8_t* slot, const uint32_t* off, int mask,
+                   int c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const uint32_t soff = min((uint32_t)first_key(c) * RB + i * 1024, part_bytes);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, LDS_PTR(void, slot + i * 1024), 16, off[i & mask], soff, 0, 0);
+    }
+  };
+  int pair[NB];
+  auto load_scales = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) pair[kb] = scale_pair(p, srsrc, w.j0 + first_key(c) + 32 * kb + i32);
+  };
+  uint32_t vaddr[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+    vaddr[db] = v_address<DT_FP8, D>((uint32_t)(size_t)LDS_PTR(const uint8_t, vslot), db, lane);
+
+  f32x16 oacc[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) oacc[db] = f32x16{0.0f};
+  float m_seen = -INFINITY, m_wave = -INFINITY, l_part = 0.0f;
+  const int kswz = k_swz<DT_FP8, D>(i32);
+  const int wt = wave >> 1;  // tile of the round
+
+  __builtin_amdgcn_sched_barrier(0);
+  load_scales(0);
+  __builtin_amdgcn_sched_barrier(0);
+  stage(krsrc, kslot, koff, 3, 0);
+  __builtin_amdgcn_sched_barrier(0);
+  stage(vrsrc, vslot, voff, 1, 0);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int t = 0; t < q.CHUNKS * q.PER; ++t) asm volatile("" : "+v"(q.x[t]));
+  const int nrounds = (w.nk + TPR * BC - 1) / (TPR * BC);
+#pragma unroll 1
+  for (int c = 0; c < nrounds; ++c) {
+    const int kw0 = first_key(c);
+    const bool need_mask = kw0 + UNIT > w.open || kw0 + UNIT > w.nk;
+    const int lim = limit - kw0 - 4 * g;
+    // this round's scales and K have landed once at most the V copies behind them
+    // are outstanding
+    wait_vmcnt<LOADS>();
+    float ks[NB], vs[2 * NB];
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) {
+      ks[kb] = scale_of(pair[kb] & 255);
+      vs[2 * kb] = v_scale(pair[kb], 0);
+      vs[2 * kb + 1] = v_scale(pair[kb], 16);
+    }
+    f32x16 sv[NB];
+#pragma unroll
+    for (int t = 0; t < q.CHUNKS; ++t)
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb) {
+        const i32x4 kk = *(const i32x4*)(kslot + (32 * kb + i32) * RB + (((2 * t + g) ^ kswz) << 4));
+        sv[kb] = product<D>(kk, ks[kb], q, t, t == 0 ? f32x16{0.0f} : sv[kb]);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    load_scales(c + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    stage(krsrc, kslot, koff, 3, c + 1);
+    settle_unit(sv);
+    if (need_mask) mask_unit(sv, lim, -INFINITY);
+    float ma, mb;
+    with_partner(unit_max(sv), ma, mb);
+    if (g == 0) mx_lds[c & 1][i32][wave] = __builtin_fmaxf(ma, mb);
+    // (the two copies of mx_lds alternate: a wave that runs ahead writes the other)
+    lds_barrier();
+    float anchor = m_seen;
+    {
+      const f32x4 x = *(const f32x4*)&mx_lds[c & 1][i32][0];
+      const float t0 = __builtin_fmaxf(x[0], x[1]), t1 = __builtin_fmaxf(x[2], x[3]);
+      m_seen = max3(m_seen, t0, t1);
+      anchor = wt == 0 ? __builtin_fmaxf(anchor, t0) : m_seen;
+    }
+    // a row that has seen no key yet keeps m = -inf, l = 0, O = 0
+    const float alpha = anchor == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m_wave - anchor) * p.c1);
+    m_wave = anchor;
+    l_part *= alpha;
+    uint32_t wpk[NB][8];
+    weigh<MODE, NB>(sv, wpk, anchor == -INFINITY ? 0.0f : anchor, p.c1, p.ck, need_mask, lim, l_part);
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) oacc[db][j] *= alpha;
+    }
+    bf16x8 pb[2 * NB];
+#pragma unroll
+    for (int k = 0; k < 2 * NB; ++k) pb[k] = p_operand<MODE>(sv[k >> 1], wpk[k >> 1], k & 1);
+    wait_vmcnt<LOADS + NB>();  // V has landed, the next round's scales and K may be outstanding
+#pragma unroll
+    for (int db = 0; db < NDB; db += 2) add_pv<D>(oacc[db], oacc[db + 1], vaddr[db], vaddr[db + 1], pb, vs);
+    stage(vrsrc, vslot, voff, 1, c + 1);
+  }
+  // every copy has landed (the last round's went to no key) and every wave is
+  // done with its slots before they are reused
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+
+  // ---- the waves' sums, each relative to its own anchor, added up: rows 0..15
+  // of every wave's O in vsm, rows 16..31 in ksm
+  {
+    float la, lb;
+    with_partner(l_part, la, lb);
+    if (g == 0) {
+      m_lds[i32][wave] = m_wave;
+      l_lds[i32][wave] = la + lb;
+    }
+  }
+  if (i32 < w.nrows) {
+    const int ri = i32 & (RHALF - 1);
+    float* red = (float*)(i32 < RHALF ? vsm : ksm) + (wave * RHALF + ri) * D;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int jq = 0; jq < 4; ++jq)
+        *(f32x4*)(red + 4 * ((8 * db + 2 * jq + g) ^ ri)) =
+            f32x4{oacc[db][4 * jq], oacc[db][4 * jq + 1], oacc[db][4 * jq + 2], oacc[db][4 * jq + 3]};
+  }
+  lds_barrier();
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int r0 = half * RHALF;
+    if (r0 >= w.nrows) break;
+    const float* red = (const float*)(half == 0 ? vsm : ksm);
+#pragma unroll
+    for (int i = 0; i < RHALF * (D / 4) / (NW * 64); ++i) {
+      const int idx = i * NW * 64 + tid, rr = idx / (D / 4), ch = idx % (D / 4), r = r0 + rr;
+      if (r >= w.nrows) continue;
+      const f32x4 mw = *(const f32x4*)m_lds[r], lw = *(const f32x4*)l_lds[r];
+      const float m = __builtin_fmaxf(__builtin_fmaxf(mw[0], mw[1]), __builtin_fmaxf(mw[2], mw[3]));
+      float l = 0.0f;
+      f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int x = 0; x < NW; ++x) {
+        const float f = mw[x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mw[x] - m) * p.c1);
+        l += f * lw[x];
+        const f32x4 o = *(const f32x4*)(red + (x * RHALF + rr) * D + 4 * (ch ^ rr));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += f * o[e];
+      }
+      const size_t orow = out_row(p, w, r);
+      if (p.parts == 1) {
+        store_row4(p.o + orow * D + 4 * ch, acc, inverse(l, 1.0f));
+        if (p.lse && ch == 0) p.lse[orow] = row_lse(m, l, p.c1);
+      } else {
+        const size_t at = orow * (size_t)p.parts + w.part;
+        *(f32x4*)(p.part_o + at * D + 4 * ch) = acc;
+        if (ch == 0) *(f32x2*)(p.part_ml + at * 2) = f32x2{m, l};
+      }
+    }
+  }
+}
+
+template <int D, int MODE>
+__device__ __forceinline__ void rows_form(const BlocksParams& p, const Work& w, uint8_t* ksm, uint8_t* vsm) {
+  using C = BCfg<D>;
+  constexpr int RB = C::RB, NDB = D / 32, LOADS = C::TILE / (NW * 1024), NSC = BC / 32;
+  const int tid = threadIdx.x, lane = tid & 63, i32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool active = wave * WROWS < w.nrows;
+  const int rowc = min(wave * WROWS + i32, w.nrows - 1);
+  const size_t orow = out_row(p, w, rowc);
+  RowOperand<DT_FP8, D> q;
+  load_q<D>(q, p.q + orow * (2 * D), g);
+  const int limit = row_limit(p, w, rowc);
+  const uint32_t part_bytes = (uint32_t)w.nk * RB;
+  const auto krsrc = rows_rsrc(w.k, part_bytes), vrsrc = rows_rsrc(w.v, part_bytes);
+  const auto srsrc = rows_rsrc(w.scales, w.used);
+  // a wave copies a quarter of each tile: LOADS consecutive KB
+  uint32_t koff[4], voff[2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = copy_row<C::NCH>(wave * LOADS + i, lane);
+    koff[i] = (r - (wave * LOADS + i) * (64 / C::NCH)) * RB + (((lane % C::NCH) ^ k_swz<DT_FP8, D>(r)) << 4);
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = copy_row<C::NCH>(wave * LOADS + i, lane);
+    voff[i] = (r - (wave * LOADS + i) * (64 / C::NCH)) * RB + (((lane % C::NCH) ^ v_swz<DT_FP8, D>(r)) << 4);
+  }
+  auto stage = [&](const __amdgpu_buffer_rsrc_t rsrc, uint8_t* area, const uint32_t* off, int mask,
+                   int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const uint32_t at = (wave * LOADS + i) * 1024;
+      const uint32_t soff = min((uint32_t)t * C::TILE + at, part_bytes);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, LDS_PTR(void, area + at), 16, off[i & mask], soff, 0, 0);
+    }
+  };
+  int pair[NSC];
+  auto load_scales = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kb = 0; kb < NSC; ++kb) pair[kb] = scale_pair(p, srsrc, w.j0 + t * BC + 32 * kb + i32);
+  };
+  uint32_t vaddr[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+    vaddr[db] = v_address<DT_FP8, D>((uint32_t)(size_t)LDS_PTR(const uint8_t, vsm), db, lane);
+  f32x16 oacc[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) oacc[db] = f32x16{0.0f};
+  float m = -INFINITY, l = 0.0f;
+  const int kswz = k_swz<DT_FP8, D>(i32);
+
+  load_scales(0);
+  stage(krsrc, ksm, koff, 3, 0);
+#pragma unroll
+  for (int t = 0; t < q.CHUNKS * q.PER; ++t) asm volatile("" : "+v"(q.x[t]));
+  const int ntiles = (w.nk + BC - 1) / BC;
+#pragma unroll 1
+  for (int t = 0; t < ntiles; ++t) {
+    // this wave's part of K has landed; past the barrier everyone's has, and
+    // everyone is done with the last tile's V
+    wait_vmcnt<0>();
+    lds_barrier();
+    stage(vrsrc, vsm, voff, 1, t);
+    const int kw0 = t * BC;
+    const bool need_mask = kw0 + BC > w.open || kw0 + BC > w.nk;
+    const int lim = limit - kw0 - 4 * g;
+    f32x16 lo[2], hi[2];  // keys 0..63 and 64..127
+    float ks[NSC], vlo[4], vhi[4];
+#pragma unroll
+    for (int kb = 0; kb < NSC; ++kb) {
+      ks[kb] = scale_of(pair[kb] & 255);
+      float* const vs = kb < 2 ? vlo + 2 * kb : vhi + 2 * (kb - 2);
+      vs[0] = v_scale(pair[kb], 0);
+      vs[1] = v_scale(pair[kb], 16);
+    }
+    if (active) {
+#pragma unroll
+      for (int kt = 0; kt < q.CHUNKS; ++kt)
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+          const i32x4 kk = *(const i32x4*)(ksm + (32 * kb + i32) * RB + (((2 * kt + g) ^ kswz) << 4));
+          f32x16& s = kb < 2 ? lo[kb & 1] : hi[kb & 1];
+          s = product<D>(kk, ks[kb], q, kt, kt == 0 ? f32x16{0.0f} : s);
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    lds_barrier();  // everyone has read K
+    load_scales(t + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    stage(krsrc, ksm, koff, 3, t + 1);
+    uint32_t wlo[2][8], whi[2][8];
+    if (active) {
+      settle_unit(lo);
+      settle_unit(hi);
+      if (need_mask) {
+        mask_unit(lo, lim, -INFINITY);
+        mask_unit(hi, lim - 64, -INFINITY);
+      }
+      float ma, mb;
+      with_partner(__builtin_fmaxf(unit_max(lo), unit_max(hi)), ma, mb);
+      // a row that has seen no key yet keeps m = -inf, l = 0, O = 0
+      const float anchor = max3(m, ma, mb);
+      const float alpha = anchor == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - anchor) * p.c1);
+      const float m_use = anchor == -INFINITY ? 0.0f : anchor;
+      m = anchor;
+      l *= alpha;
+      weigh<MODE, 2>(lo, wlo, m_use, p.c1, p.ck, need_mask, lim, l);
+      weigh<MODE, 2>(hi, whi, m_use, p.c1, p.ck, need_mask, lim - 64, l);
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) oacc[db][j] *= alpha;
+      }
+    }
+    wait_vmcnt<LOADS + NSC>();  // V has landed, the next tile's scales and K may be outstanding
+    lds_barrier();
+    if (active) {
+      bf16x8 pb[4], pc[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        pb[k] = p_operand<MODE>(lo[k >> 1], wlo[k >> 1], k & 1);
+        pc[k] = p_operand<MODE>(hi[k >> 1], whi[k >> 1], k & 1);
+      }
+#pragma unroll
+      for (int db = 0; db < NDB; db += 2) {
+        add_pv<D>(oacc[db], oacc[db + 1], vaddr[db], vaddr[db + 1], pb, vlo);
+        add_pv<D>(oacc[db], oacc[db + 1], vaddr[db] + 64 * RB, vaddr[db + 1] + 64 * RB, pc, vhi);
+      }
+    }
+  }
+  wait_vmcnt<0>();
+  float la, lb;
+  with_partner(l, la, lb);
+  l = la + lb;
+  if (wave * WROWS + i32 >= w.nrows) return;
+  const float inv = inverse(l, 1.0f);
+  const size_t at = orow * (size_t)p.parts + w.part;
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+#pragma unroll
+    for (int jq = 0; jq < 4; ++jq) {
+      const f32x4 x = {oacc[db][4 * jq], oacc[db][4 * jq + 1], oacc[db][4 * jq + 2], oacc[db][4 * jq + 3]};
+      const int col = 32 * db + 8 * jq + 4 * g;
+      if (p.parts == 1) store_row4(p.o + orow * D + col, x, inv);
+      else *(f32x4*)(p.part_o + at * D + col) = x;
+    }
+  if (g == 0) {
+    if (p.parts > 1) *(f32x2*)(p.part_ml + at * 2) = f32x2{m, l};
+    else if (p.lse) p.lse[orow] = row_lse(m, l, p.c1);
+  }
+}
+
+template <int D, int MODE, bool ROWS>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_blocks_kernel(
+    BlocksParams p) {
+  using C = BCfg<D>;
+  // (arrays of their own, so that the compiler tells the copies apart)
+  __shared__ __attribute__((aligned(16))) uint8_t ksm[C::AREA];
+  __shared__ __attribute__((aligned(16))) uint8_t vsm[C::AREA];
+  __shared__ __attribute__((aligned(16))) float mx_lds[2][32][NW];
+  __shared__ __attribute__((aligned(16))) float m_lds[32][NW], l_lds[32][NW];
+  Work w;
+  int unit, rb;
+  place(blockIdx.x, p.B * p.Hkv * p.parts, p.row_blocks, unit, rb);
+  int bh = unit / p.parts;
+  w.part = unit - bh * p.parts;
+  w.b = bh / p.Hkv;
+  w.h = bh - w.b * p.Hkv;
+  if (p.longest) {
+    w.b = longest(p.lens, p.B, p.Sk, w.b, (int*)mx_lds);
+    bh = w.b * p.Hkv + w.h;
+  }
+  const int n = p.lens ? min(max(p.lens[w.b], 0), p.Sk) : p.Sk;
+  w.row0 = rb * p.rows;
+  w.nrows = min(p.rows, p.R - w.row0);
+  w.j0 = w.part * p.split;
+  w.nk = max(min(p.split, n - w.j0), 0);
+  w.open = w.nk;
+  w.last0 = w.nk - 1;
+  if (p.causal) {
+    // positions of its rows: from i0 on, or all of them where they pass a head's last
+    const int i0 = w.row0 % p.Sq, i1 = i0 + w.nrows - 1;
+    w.last0 = n - p.Sq - w.j0;
+    w.nk = max(min(w.nk, w.last0 + min(i1, p.Sq - 1) + 1), 0);
+    w.open = w.last0 + (i1 < p.Sq ? i0 : 0) + 1;
+  }
+  if (w.nk == 0 && p.parts > 1) {
+    // nothing to read: the merge skips a part with l = 0
+    if ((int)threadIdx.x < w.nrows)
+      *(f32x2*)(p.part_ml + (out_row(p, w, threadIdx.x) * (size_t)p.parts + w.part) * 2) = f32x2{-INFINITY, 0.0f};
+    return;
+  }
+  const size_t at = ((size_t)bh * (size_t)p.Sk_cap + (size_t)(w.nk ? w.j0 : 0)) * D;
+  w.k = p.k + at;
+  w.v = p.v + at;
+  w.scales = p.scales + (size_t)bh * (size_t)p.blocks * 2;
+  w.used = 2 * ((n + (1 << p.shift) - 1) >> p.shift);
+  if constexpr (ROWS) rows_form<D, MODE>(p, w, ksm, vsm);
+  else keys_form<D, MODE>(p, w, ksm, vsm, mx_lds, m_lds, l_lds);
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void attn_blocks_merge(BlocksParams p) {
+  merge_parts<D>(p, 1.0f);
+}
+
+template <int D, int MODE>
+hipError_t launch_one(const BlocksParams& p, hipStream_t st) {
+  const dim3 grid((unsigned)p.groups), block(NW * 64);
+  if (p.rows == WROWS) hipLaunchKernelGGL((attn_blocks_kernel<D, MODE, false>), grid, block, 0, st, p);
+  else hipLaunchKernelGGL((attn_blocks_kernel<D, MODE, true>), grid, block, 0, st, p);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_mode(const BlocksParams& p, int mode, hipStream_t st) {
+  hipError_t e;
+  switch (mode) {
+    case MODE_EXACT: e = launch_one<D, MODE_EXACT>(p, st); break;
+    case 1: e = launch_one<D, 1>(p, st); break;
+    case 3: e = launch_one<D, 3>(p, st); break;
+    case 5: e = launch_one<D, 5>(p, st); break;
+    default: return hipErrorInvalidValue;
+  }
+  if (e != hipSuccess || p.parts == 1) return e;
+  const dim3 grid((unsigned)(((long long)p.B * p.Hq * p.Sq + 3) / 4));
+  hipLaunchKernelGGL(attn_blocks_merge<D>, grid, dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+}  // namespace
+
+namespace h15 {
+
+int launch_blocks(const BlocksParams& p, int d, int mode, void* stream) {
+  hipStream_t st = (hipStream_t)stream;
+  const hipError_t e = d == 128 ? launch_mode<128>(p, mode, st) : launch_mode<64>(p, mode, st);
+  return e == hipSuccess ? 0 : 1;
+}
+
+}  // namespace h15

@@ -1,0 +1,314 @@
+// Norms of queries and keys for each head with their position rotation
+// (attn_rope), and the gradient of both (attn_rope_bwd).
+//
+// A row has d / 16 lanes of 16 channels each, two chunks of 16 bytes, chosen so
+// that a lane has both channels of each of its 8 pairs: chunks l and l + rot / 16
+// of the rotated channels for the half layout, neighbouring chunks for the
+// interleaved one and for the channels that are not rotated.  So a rotation
+// takes no exchange between lanes, and a norm's sum three (d = 128) or two.  A
+// thread keeps its position and takes a run of heads one after the other: the
+// sines and cosines of its 8 pairs are made once for all of them.
+//
+// Angles: turns = position * freq / 2 pi in FP64 (off by 2^-53 of it, 2^-23 of a
+// turn at the farthest position), less the nearest whole number, and then the
+// sine and cosine instructions, which take turns (off by at most 1.3e-7 over
+// half a turn to either side).
+//
+// Everything between the operand and the one rounding of the output is FP32.
+#include "qkv_params.h"
+#include "attn_device.h"
+
+namespace {
+
+// A thread's place: lane l of its row, the channels of its two chunks.
+template <int D>
+struct Place {
+  static constexpr int LPR = D / 16;
+  int l, c0, c1;
+  bool rotated;
+  __device__ __forceinline__ Place(const RopeParams& p, bool turned) {
+    l = threadIdx.x % LPR;
+    rotated = turned && 16 * l < p.rot;
+    const bool halves = rotated && !p.interleaved;
+    c0 = halves ? 8 * l : 16 * l;
+    c1 = halves ? p.rot / 2 + 8 * l : 16 * l + 8;
+  }
+};
+
+// Cosines and sines of a lane's pairs 8 l .. 8 l + 7, times the amplitude.
+struct Turn {
+  float c[8], s[8];
+  __device__ __forceinline__ void set(const RopeParams& p, int l, int b, int s_at) {
+    const double at = !p.positions          ? (double)s_at
+                      : p.each_position     ? (double)p.positions[(size_t)b * p.S + s_at]
+                                            : (double)p.positions[b] + (double)s_at;
+    const double turns = at * 0.15915494309189535;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      double t = turns * p.freqs[8 * l + j];
+      t -= __builtin_rint(t);
+      c[j] = p.amplitude * __builtin_amdgcn_cosf((float)t);
+      s[j] = p.amplitude * __builtin_amdgcn_sinf((float)t);
+    }
+  }
+};
+
+// A pair's channels among a thread's 16.
+__device__ __forceinline__ constexpr int pair_a(bool inter, int j) { return inter ? 2 * j : j; }
+__device__ __forceinline__ constexpr int pair_b(bool inter, int j) { return inter ? 2 * j + 1 : 8 + j; }
+
+// x turned by the angles (BACK: by their negatives)
+template <bool INTER, bool BACK>
+__device__ __forceinline__ void rotate(float (&x)[16], const Turn& t) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int a = pair_a(INTER, j), b = pair_b(INTER, j);
+    const float xa = x[a], xb = x[b], s = BACK ? -t.s[j] : t.s[j];
+    x[a] = __builtin_fmaf(xa, t.c[j], -(xb * s));
+    x[b] = __builtin_fmaf(xb, t.c[j], xa * s);
+  }
+}
+
+__device__ __forceinline__ void widen16(float (&x)[16], u32x4 a, u32x4 b) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(a[i] << 16);
+    x[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
+    x[8 + 2 * i] = __uint_as_float(b[i] << 16);
+    x[8 + 2 * i + 1] = __uint_as_float(b[i] & 0xFFFF0000u);
+  }
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+}
+__device__ __forceinline__ u32x4 pack8(const float* x) {
+  return u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])};
+}
+
+// +-448 at most; NaN stays (the median of a NaN and two numbers is one of them)
+__device__ __forceinline__ float held(float x) { return x != x ? x : __builtin_amdgcn_fmed3f(x, -448.0f, 448.0f); }
+__device__ __forceinline__ u32x2 pack8_fp8(const float* x, float inv) {
+  u32x2 r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(held(x[4 * i] * inv), held(x[4 * i + 1] * inv), 0, false);
+    r[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(held(x[4 * i + 2] * inv), held(x[4 * i + 3] * inv), w, true);
+  }
+  return r;
+}
+
+// Sum over a row's lanes, 8 or 4 neighbours, on the VALU: lanes i ^ 1, i ^ 2, and
+// the other four of eight.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), CTRL, 0xF, 0xF, true));
+}
+template <int D>
+__device__ __forceinline__ float row_sum(float x) {
+  x += dpp<0xB1>(x);
+  x += dpp<0x4E>(x);
+  if constexpr (D == 128) x += dpp<0x141>(x);
+  return x;
+}
+
+// 1 / sqrt(mean x^2 + eps)
+template <int D>
+__device__ __forceinline__ float inverse_rms(const float (&x)[16], float eps) {
+  float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < 16; ++i) a[i & 3] = __builtin_fmaf(x[i], x[i], a[i & 3]);
+  return __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<D>((a[0] + a[1]) + (a[2] + a[3])), 1.0f / D, eps));
+}
+
+// A thread's 16 weights.
+__device__ __forceinline__ void load_weights(float (&w)[16], const void* from, bool bf16, int c0, int c1) {
+  if (bf16) {
+    const uint16_t* f = (const uint16_t*)from;
+    widen16(w, *(const u32x4*)(f + c0), *(const u32x4*)(f + c1));
+  } else {
+    const float* f = (const float*)from;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = f[c0 + i], w[8 + i] = f[c1 + i];
+  }
+}
+
+// Tensor and first head of the run of heads `r`.
+__device__ __forceinline__ int tensor_of(const RopeParams& p, int& r) {
+  int i = 0;
+  while (i < 2 && r >= p.t[i].runs) r -= p.t[i++].runs;
+  return i;
+}
+
+template <int D, int DT, bool INTER>
+__global__ __launch_bounds__(ROPE_THREADS) void attn_rope_kernel(RopeParams p) {
+  int r = blockIdx.y;
+  const RopeTensor& t = p.t[tensor_of(p, r)];
+  const Place<D> at(p, t.turned);
+  const int token = blockIdx.x * rope_tokens(D) + threadIdx.x / Place<D>::LPR;
+  if (token >= p.B * p.S) return;  // (a row's lanes leave together)
+  const int b = token / p.S, s = token - b * p.S, h0 = r * p.run, h1 = min(h0 + p.run, t.heads);
+  const uint16_t* in = t.in + (int64_t)b * t.sb + (int64_t)s * t.ss + (int64_t)h0 * t.sh;
+  u32x4 a0 = *(const u32x4*)(in + at.c0), a1 = *(const u32x4*)(in + at.c1);
+  Turn turn;
+  if (at.rotated) turn.set(p, at.l, b, s);
+  float w[16];
+  if (t.weight) load_weights(w, t.weight, p.weight_bf16, at.c0, at.c1);
+  size_t o = (((size_t)b * t.heads + h0) * (size_t)p.S + s) * D;
+#pragma unroll 1
+  for (int h = h0; h < h1; ++h, o += (size_t)p.S * D) {
+    float x[16];
+    widen16(x, a0, a1);
+    if (h + 1 < h1) {
+      in += t.sh;
+      a0 = *(const u32x4*)(in + at.c0);
+      a1 = *(const u32x4*)(in + at.c1);
+    }
+    if (t.weight) {
+      const float f = inverse_rms<D>(x, p.eps);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = x[i] * f * w[i];
+    }
+    if (at.rotated) rotate<INTER, false>(x, turn);
+    if constexpr (DT == DT_BF16) {
+      uint16_t* out = (uint16_t*)t.out + o;
+      *(u32x4*)(out + at.c0) = pack8(x);
+      *(u32x4*)(out + at.c1) = pack8(x + 8);
+    } else {
+      uint8_t* out = (uint8_t*)t.out + o;
+      *(u32x2*)(out + at.c0) = pack8_fp8(x, t.inv);
+      *(u32x2*)(out + at.c1) = pack8_fp8(x + 8, t.inv);
+    }
+  }
+}
+
+// A workgroup takes every groups-th tile of positions for its run of heads; its
+// part of a weight's gradient is one row of the workspace.
+template <int D, bool INTER>
+__global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams p) {
+  constexpr int LPR = Place<D>::LPR, TOKENS = rope_tokens(D);
+  __shared__ float sums[TOKENS][D + 4];
+  int r = blockIdx.y;
+  const RopeTensor& t = p.t[tensor_of(p, r)];
+  const Place<D> at(p, t.turned);
+  const int h0 = r * p.run, h1 = min(h0 + p.run, t.heads);
+  float w[16], dw[16];
+  if (t.weight) load_weights(w, t.weight, p.weight_bf16, at.c0, at.c1);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) dw[i] = 0.0f;
+#pragma unroll 1
+  for (int tile = blockIdx.x; tile < p.tiles; tile += p.groups) {
+    const int token = tile * TOKENS + threadIdx.x / LPR;
+    if (token >= p.B * p.S) break;
+    const int b = token / p.S, s = token - b * p.S;
+    const uint16_t* g = (const uint16_t*)t.out + (((size_t)b * t.heads + h0) * (size_t)p.S + s) * D;
+    const uint16_t* in = t.in + (int64_t)b * t.sb + (int64_t)s * t.ss + (int64_t)h0 * t.sh;
+    uint16_t* dx = t.grad + (int64_t)b * t.gb + (int64_t)s * t.gs + (int64_t)h0 * t.gh;
+    u32x4 a0 = *(const u32x4*)(g + at.c0), a1 = *(const u32x4*)(g + at.c1), x0, x1;
+    if (t.weight) x0 = *(const u32x4*)(in + at.c0), x1 = *(const u32x4*)(in + at.c1);
+    Turn turn;
+    if (at.rotated) turn.set(p, at.l, b, s);
+#pragma unroll 1
+    for (int h = h0; h < h1; ++h, dx += t.gh) {
+      float e[16], u[16];
+      widen16(e, a0, a1);
+      if (t.weight) widen16(u, x0, x1);
+      if (h + 1 < h1) {
+        g += (size_t)p.S * D;
+        a0 = *(const u32x4*)(g + at.c0);
+        a1 = *(const u32x4*)(g + at.c1);
+        if (t.weight) {
+          in += t.sh;
+          x0 = *(const u32x4*)(in + at.c0);
+          x1 = *(const u32x4*)(in + at.c1);
+        }
+      }
+      if (at.rotated) rotate<INTER, true>(e, turn);
+      if (t.weight) {
+        const float f = inverse_rms<D>(u, p.eps);
+        float m = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          u[i] *= f;
+          dw[i] = __builtin_fmaf(e[i], u[i], dw[i]);
+          e[i] *= w[i];
+          m = __builtin_fmaf(e[i], u[i], m);
+        }
+        m = row_sum<D>(m) * (1.0f / D);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) e[i] = f * __builtin_fmaf(-m, u[i], e[i]);
+      }
+      *(u32x4*)(dx + at.c0) = pack8(e);
+      *(u32x4*)(dx + at.c1) = pack8(e + 8);
+    }
+  }
+  if (!t.weight) return;
+  float* const mine = sums[threadIdx.x / LPR];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) mine[at.c0 + i] = dw[i], mine[at.c1 + i] = dw[8 + i];
+  __syncthreads();
+  if ((int)threadIdx.x < D) {
+    float a = 0.0f;
+#pragma unroll 8
+    for (int i = 0; i < TOKENS; ++i) a += sums[i][threadIdx.x];
+    p.part[((size_t)t.partials + (size_t)r * p.groups + blockIdx.x) * D + threadIdx.x] = a;
+  }
+}
+
+// A weight's gradient from its workgroups' parts: 32 channels a workgroup.
+template <int D>
+__global__ __launch_bounds__(256) void attn_rope_bwd_sum(RopeParams p) {
+  __shared__ f32x4 sums[32][8];
+  const RopeTensor& t = p.t[blockIdx.y];
+  if (!t.dweight) return;
+  const int col = threadIdx.x & 7, row = threadIdx.x >> 3, n = t.runs * p.groups;
+  const float* from = p.part + (size_t)t.partials * D + blockIdx.x * 32 + col * 4;
+  f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int i = row; i < n; i += 32) {
+    const f32x4 x = *(const f32x4*)(from + (size_t)i * D);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) a[e] += x[e];
+  }
+  sums[row][col] = a;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    float x = 0.0f;
+    for (int i = 0; i < 32; ++i) x += sums[i][threadIdx.x >> 2][threadIdx.x & 3];
+    t.dweight[blockIdx.x * 32 + threadIdx.x] = x;
+  }
+}
+
+template <int D, int DT>
+void launch_forward(const RopeParams& p, dim3 grid, hipStream_t st) {
+  if (p.interleaved) hipLaunchKernelGGL((attn_rope_kernel<D, DT, true>), grid, dim3(ROPE_THREADS), 0, st, p);
+  else hipLaunchKernelGGL((attn_rope_kernel<D, DT, false>), grid, dim3(ROPE_THREADS), 0, st, p);
+}
+
+template <int D>
+void launch_backward(const RopeParams& p, dim3 grid, hipStream_t st) {
+  if (p.interleaved) hipLaunchKernelGGL((attn_rope_bwd_kernel<D, true>), grid, dim3(ROPE_THREADS), 0, st, p);
+  else hipLaunchKernelGGL((attn_rope_bwd_kernel<D, false>), grid, dim3(ROPE_THREADS), 0, st, p);
+  if (p.t[0].dweight || p.t[1].dweight)
+    hipLaunchKernelGGL((attn_rope_bwd_sum<D>), dim3(D / 32, 2), dim3(256), 0, st, p);
+}
+}  // namespace
+
+namespace h15 {
+
+int launch_rope(const RopeParams& p, int dtype, void* stream) {
+  const dim3 grid((unsigned)p.tiles, (unsigned)(p.t[0].runs + p.t[1].runs + p.t[2].runs));
+  hipStream_t st = (hipStream_t)stream;
+  if (dtype == ATTN_BF16) p.d == 128 ? launch_forward<128, DT_BF16>(p, grid, st) : launch_forward<64, DT_BF16>(p, grid, st);
+  else p.d == 128 ? launch_forward<128, DT_FP8>(p, grid, st) : launch_forward<64, DT_FP8>(p, grid, st);
+  return hipGetLastError() == hipSuccess ? 0 : 1;
+}
+
+int launch_rope_bwd(const RopeParams& p, void* stream) {
+  const dim3 grid((unsigned)p.groups, (unsigned)(p.t[0].runs + p.t[1].runs + p.t[2].runs));
+  hipStream_t st = (hipStream_t)stream;
+  p.d == 128 ? launch_backward<128>(p, grid, st) : launch_backward<64>(p, grid, st);
+  return hipGetLastError() == hipSuccess ? 0 : 1;
+}
+
+}  // namespace h15

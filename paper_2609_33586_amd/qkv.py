@@ -1,0 +1,390 @@
+"""The operators between a layer's projections and its attention
+(``include/h15qkv.h``): norms of queries and keys with their position rotation,
+its gradient, writing into a cache of 8-bit blocks, and attention over such a
+cache.  The functions carry the C names and are reached as those of the
+package; like them they raise and never compute anything another way.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+
+from . import ATTN_BF16, ATTN_FP8_E4M3, ATTN_OK, AttnError, _dtype_of, _new, _outputs, attn_opts, cache, lib
+from .cache import _call_opts, _current_gpu, _four, _lens_ptr, _refuse, _space, _tensor
+
+ATTN_FP32 = 2  # type of norm weights, next to ATTN_BF16
+
+# every symbol h15qkv.h declares
+EXPORTS = ("attn_rope", "attn_rope_bwd", "attn_rope_bwd_workspace_bytes", "attn_cache_append", "attn_decode_blocks",
+           "attn_decode_blocks_workspace_bytes", "attn_decode_blocks_split_keys")
+
+
+class attn_strides(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("position", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class attn_rope_spec(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("each_position", ctypes.c_int), ("freqs", ctypes.c_void_p),
+                ("rot", ctypes.c_int), ("interleaved", ctypes.c_int), ("amplitude", ctypes.c_float),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("weight_dtype", ctypes.c_int),
+                ("eps", ctypes.c_float)]
+
+
+_bound = None
+_torch = None
+_Strides3 = ctypes.c_int64 * 9  # attn_strides of three tensors
+
+
+def _lib() -> ctypes.CDLL:
+    """The library with the argument types of these functions, bound on first use."""
+    global _bound, _torch
+    if _bound is not None:
+        return _bound
+    L = lib()
+    P, I, F, S = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
+    R, O = ctypes.POINTER(attn_rope_spec), ctypes.POINTER(attn_opts)
+    for name, args, res in (
+            ("attn_rope", [P, P, P, P, R, P, P, P] + [I] * 6 + [O], I),
+            ("attn_rope_bwd", [P] * 6 + [R] + [P] * 6 + [I] * 5 + [P, S, O], I),
+            ("attn_rope_bwd_workspace_bytes", [I] * 5, S),
+            ("attn_cache_append", [P] * 8 + [I] * 6 + [O], I),
+            ("attn_decode_blocks", [P] * 7 + [I] * 9 + [F, I, I, P, S, O], I),
+            ("attn_decode_blocks_workspace_bytes", [I] * 6, S),
+            ("attn_decode_blocks_split_keys", [I] * 6, I)):
+        fn = getattr(L, name)
+        fn.argtypes, fn.restype = args, res
+    import torch
+    _torch = torch
+    cache._lib()  # (its checks use its own binding of torch)
+    _bound = L
+    return L
+
+
+# ---- frequencies ------------------------------------------------------------
+
+def attn_rope_frequencies(rot: int, base: float = 10000.0, *, scaling: str | None = None, factor: float = 1.0,
+                          original: int | None = None, slow: float = 1.0, fast: float = 32.0, device=None):
+    """(freqs, amplitude) for attn_rope: radians a position of each pair, float64 [rot / 2], and the factor of the
+    rotated channels.
+
+    Unscaled: f_j = base^(-2 j / rot), amplitude 1.  A context `factor` times as
+    long as the `original` one that a model was trained for, by `scaling`:
+      "linear"  f_j / factor: positions are interpolated;
+      "base"    the base times factor^(rot / (rot - 2)): the slowest pair is
+                interpolated, the fastest kept;
+      "ramp"    f_j kept for pairs that turn more than `fast` times over the
+                original context, divided by factor for those that turn less
+                than `slow` times, and in between a mixture linear in the pair's
+                index; amplitude 0.1 ln(factor) + 1;
+      "smooth"  the same ends (usual: slow 1, fast 4), the mixture linear in the
+                number of turns; amplitude 1."""
+    import torch
+    if rot <= 0 or rot % 2 or not base > 0:
+        raise ValueError("rot must be even and positive, base positive")
+    if scaling not in (None, "linear", "base", "ramp", "smooth") or not factor >= 1.0:
+        raise ValueError("scaling must be None, 'linear', 'base', 'ramp' or 'smooth', factor 1 or more")
+    if scaling == "base":
+        if rot < 4:
+            raise ValueError("scaling 'base' takes two pairs or more")
+        base = base * factor ** (rot / (rot - 2))
+    j = torch.arange(rot // 2, dtype=torch.float64)
+    f = torch.pow(torch.tensor(float(base), dtype=torch.float64), -2.0 * j / rot)
+    amplitude = 1.0
+    if scaling == "linear":
+        f = f / factor
+    elif scaling in ("ramp", "smooth"):
+        if original is None or original <= 0 or not 0 < slow < fast:
+            raise ValueError(f"scaling '{scaling}' takes the original context's length and 0 < slow < fast")
+        turns = original * f / (2 * math.pi)
+        if scaling == "smooth":
+            keep = ((turns - slow) / (fast - slow)).clamp(0.0, 1.0)
+        else:
+            # the pair's index at which a pair turns `n` times: base^(-2 j / rot) original = 2 pi n
+            at = lambda n: rot * math.log(original / (2 * math.pi * n)) / (2 * math.log(base))  # noqa: E731
+            first, last = max(math.floor(at(fast)), 0), min(math.ceil(at(slow)), rot - 1)
+            keep = 1.0 - ((j - first) / max(last - first, 1e-3)).clamp(0.0, 1.0)
+            amplitude = 0.1 * math.log(factor) + 1.0
+        f = f * keep + f / factor * (1.0 - keep)
+    return f.to(device), amplitude
+
+
+# ---- norms and rotation -------------------------------------------------------
+
+def _strided(name, t, B, S, d, dev):
+    """Heads and the three strides of a bf16 tensor [B,S,H,d] whose rows are contiguous."""
+    shape = t.shape
+    if (len(shape) != 4 or shape[0] != B or shape[1] != S or shape[3] != d or t.get_device() != dev
+            or t.dtype != _torch.bfloat16):
+        raise ValueError(f"{name} must be a bfloat16 tensor [{B}x{S}xHx{d}] on GPU {dev}")
+    sb, ss, sh, sd = t.stride()
+    if sd != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    H = shape[2]
+    # (the stride of a dimension of one element says nothing)
+    return H, (sb if B > 1 else 0, ss if S > 1 else 0, sh if H > 1 else 0)
+
+
+def _apart(name, t):
+    """An output must not lie over itself: its dimensions, the smallest stride first, each beyond the ones before."""
+    end = 1
+    for stride, n in sorted(zip(t.stride(), t.shape)):
+        if n > 1 and stride < end:
+            raise ValueError(f"rows of {name} overlap")
+        if n > 1:
+            end = stride * (n - 1) + end
+    return t
+
+
+def _spec(B, S, d, dev, freqs, positions, interleaved, amplitude, q_weight, k_weight, eps):
+    pptr, each, fptr, rot = None, 0, None, 0
+    if freqs is not None:
+        rot = 2 * freqs.numel()
+        fptr = _tensor("freqs", freqs, (rot // 2,), dev, _torch.float64).data_ptr()
+    if positions is not None:
+        each = 1 if len(positions.shape) == 2 else 0
+        pptr = _tensor("positions", positions, (B, S) if each else (B,), dev, _torch.int32).data_ptr()
+    kind = None
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is None:
+            continue
+        if w.dtype != _torch.bfloat16 and w.dtype != _torch.float32 or kind not in (None, w.dtype):
+            raise TypeError("q_weight and k_weight must be bfloat16, or both float32")
+        kind = _tensor(name, w, (d,), dev).dtype
+    wq, wk = (None if w is None else w.data_ptr() for w in (q_weight, k_weight))
+    wt = ATTN_FP32 if kind == _torch.float32 else ATTN_BF16
+    return attn_rope_spec(pptr, each, fptr, rot, 1 if interleaved else 0, amplitude, wq, wk, wt, eps)
+
+
+def attn_rope(q, k=None, v=None, *, freqs=None, positions=None, interleaved: bool = False, amplitude: float = 1.0,
+              q_weight=None, k_weight=None, eps: float = 1e-6, descale=None, out_dtype=None, q_out=None, k_out=None,
+              v_out=None, stream=None):
+    """Norms of queries and keys for each head, their position rotation, and the attention's layout (see
+    include/h15qkv.h, attn_rope).
+
+    q: [B,S,Hq,d], k, v: [B,S,Hkv,d] bf16, views of any strides (multiples of 8)
+    with contiguous rows, such as parts of one projection's output; each may be
+    None.  freqs: float64 [rot / 2] (attn_rope_frequencies; None: no rotation);
+    positions: int32 [B,S], or [B]: those of the first rows (None: from 0).
+    q_weight, k_weight: [d] bf16 or fp32 (None: no norm).  Returns (q_out
+    [B,Hq,S,d], k_out, v_out [B,Hkv,S,d]): the given tensors, or new ones of
+    out_dtype (bfloat16, the default, or float8_e4m3fn with descale = (q, k, v)
+    factors, as attn_fwd_ex takes them)."""
+    L = _lib()
+    first = q if q is not None else k if k is not None else v
+    if first is None:
+        raise ValueError("q, k and v: one at least")
+    B, S, _, d = shape = first.shape
+    dev = _current_gpu("q", first, stream)
+    given = q_out if q_out is not None else k_out if k_out is not None else v_out
+    dtype = given.dtype if given is not None else _torch.bfloat16 if out_dtype is None else out_dtype
+    dt = _dtype_of(given) if given is not None else ATTN_FP8_E4M3 if dtype == _torch.float8_e4m3fn else ATTN_BF16
+    if given is None and dtype not in (_torch.bfloat16, _torch.float8_e4m3fn):
+        raise TypeError("out_dtype must be bfloat16 or float8_e4m3fn")
+    Hq = Hkv = 0
+    strides, ins, outs = [], [], []
+    for name, t, out in (("q", q, q_out), ("k", k, k_out), ("v", v, v_out)):
+        if t is None:
+            if out is not None:
+                raise ValueError(f"{name}_out without {name}")
+            strides += (0, 0, 0)
+            ins.append(None)
+            outs.append(None)
+            continue
+        H, st = _strided(name, t, B, S, d, dev)
+        if name == "q":
+            Hq = H
+        elif Hkv and H != Hkv:
+            raise ValueError("k and v must have the same heads")
+        else:
+            Hkv = H
+        strides += st
+        ins.append(t.data_ptr())
+        shape = (B, H, S, d)
+        if out is None:
+            out = _new(shape, dtype, first.device, stream)
+        else:
+            _tensor(name + "_out", out, shape, dev, dtype)
+        outs.append(out)
+    spec = _spec(B, S, d, dev, freqs, positions, interleaved, amplitude, q_weight, k_weight, eps)
+    opts = _call_opts(descale, stream)
+    rc = L.attn_rope(ins[0], ins[1], ins[2], _Strides3(*strides), ctypes.byref(spec),
+                     *[None if o is None else o.data_ptr() for o in outs], B, S, Hq, Hkv, d, dt, ctypes.byref(opts))
+    if rc != ATTN_OK:
+        raise AttnError(rc, "attn_rope")
+    return outs[0], outs[1], outs[2]
+
+
+def attn_rope_bwd_workspace_bytes(B: int, S: int, Hq: int, Hkv: int, d: int) -> int:
+    return int(_lib().attn_rope_bwd_workspace_bytes(int(B), int(S), int(Hq), int(Hkv), int(d)))
+
+
+def attn_rope_bwd(gq, gk=None, gv=None, *, q=None, k=None, freqs=None, positions=None, interleaved: bool = False,
+                  amplitude: float = 1.0, q_weight=None, k_weight=None, eps: float = 1e-6, dq=None, dk=None, dv=None,
+                  dq_weight=None, dk_weight=None, workspace=None, stream=None):
+    """The gradient of attn_rope (see include/h15qkv.h, attn_rope_bwd).
+
+    gq: [B,Hq,S,d], gk, gv: [B,Hkv,S,d] bf16, the gradients of attn_rope's
+    outputs; each may be None.  q, k: its inputs, required with their weights.
+    The other arguments are attn_rope's.  Returns (dq [B,S,Hq,d], dk, dv
+    [B,S,Hkv,d] bf16, dq_weight, dk_weight [d] fp32 or None): the given tensors
+    (dq, dk, dv may be views, such as parts of one gradient), or new ones."""
+    L = _lib()
+    first = gq if gq is not None else gk if gk is not None else gv
+    if first is None:
+        raise ValueError("gq, gk and gv: one at least")
+    B, _, S, d = shape = first.shape
+    dev, f32 = _current_gpu("gq", first, stream), _torch.float32
+    Hq = Hkv = 0
+    strides, grad_strides, gs, ins, outs, sums = [], [], [], [], [], []
+    for name, g, x, out, w, dw in (("q", gq, q, dq, q_weight, dq_weight), ("k", gk, k, dk, k_weight, dk_weight),
+                                   ("v", gv, None, dv, None, None)):
+        if g is None:
+            if out is not None or dw is not None:
+                raise ValueError(f"d{name} without g{name}")
+            strides += (0, 0, 0)
+            grad_strides += (0, 0, 0)
+            gs.append(None)
+            ins.append(None)
+            outs.append(None)
+            sums.append(None)
+            continue
+        shape = g.shape
+        if len(shape) != 4:
+            raise ValueError(f"g{name} must be a 4-D tensor")
+        H = shape[1]
+        _tensor("g" + name, g, (B, H, S, d), dev, _torch.bfloat16)
+        if name == "q":
+            Hq = H
+        elif Hkv and H != Hkv:
+            raise ValueError("gk and gv must have the same heads")
+        else:
+            Hkv = H
+        gs.append(g.data_ptr())
+        if w is not None:
+            if x is None:
+                raise ValueError(f"{name} is required with {name}_weight")
+            n, st = _strided(name, x, B, S, d, dev)
+            if n != H:
+                raise ValueError(f"{name} must have g{name}'s heads")
+            strides += st
+            ins.append(x.data_ptr())
+            sums.append(_new((d,), f32, first.device, stream) if dw is None
+                        else _tensor(f"d{name}_weight", dw, (d,), dev, f32))
+        else:
+            if dw is not None:
+                raise ValueError(f"d{name}_weight without {name}_weight")
+            strides += (0, 0, 0)
+            ins.append(None)
+            sums.append(None)
+        if out is None:
+            out = _new((B, S, H, d), _torch.bfloat16, first.device, stream)
+        n, st = _strided("d" + name, _apart("d" + name, out), B, S, d, dev)
+        if n != H:
+            raise ValueError(f"d{name} must have g{name}'s heads")
+        grad_strides += st
+        outs.append(out)
+    spec = _spec(B, S, d, dev, freqs, positions, interleaved, amplitude, q_weight, k_weight, eps)
+    wptr, wbytes, workspace = _space(workspace, lambda: L.attn_rope_bwd_workspace_bytes(B, S, Hq, Hkv, d) if (
+        sums[0] is not None or sums[1] is not None) else 0, dev, stream)
+    opts = _call_opts(None, stream)
+    rc = L.attn_rope_bwd(gs[0], gs[1], gs[2], ins[0], ins[1], _Strides3(*strides), ctypes.byref(spec),
+                         *[None if o is None else o.data_ptr() for o in outs], _Strides3(*grad_strides),
+                         *[None if o is None else o.data_ptr() for o in sums[:2]], B, S, Hq, Hkv, d, wptr, wbytes,
+                         ctypes.byref(opts))
+    if rc != ATTN_OK:
+        raise AttnError(rc, "attn_rope_bwd")
+    return outs[0], outs[1], outs[2], sums[0], sums[1]
+
+
+# ---- a cache of 8-bit blocks ----------------------------------------------------
+
+def _codes(name, t, B, Hkv, d, dev):
+    """Rows of a cache of e4m3 codes [B,Hkv,rows,d]."""
+    shape = t.shape
+    if len(shape) != 4 or _dtype_of(t) != ATTN_FP8_E4M3:
+        raise TypeError(f"{name} must be a 4-D tensor of float8_e4m3fn")
+    _tensor(name, t, (B, Hkv, shape[2], d), dev)
+    return shape[2]
+
+
+def _scales(t, B, Hkv, cap, block, dev):
+    if t.dtype != _torch.float8_e8m0fnu and t.dtype != _torch.uint8:
+        raise TypeError("scales must be float8_e8m0fnu (or uint8, their bytes)")
+    if not 0 < block < 2 ** 31:
+        raise ValueError(f"block is out of range: {block}")
+    return _tensor("scales", t, (B, Hkv, -(-cap // block), 2), dev).data_ptr()
+
+
+def attn_cache_append(k, v, k_cache, v_cache, scales, lens, *, block: int, counts=None, lens_out=None, stream=None):
+    """Write new keys and values into a cache of 8-bit blocks (see include/h15qkv.h, attn_cache_append).
+
+    k, v: [B,Hkv,n,d] bf16; k_cache, v_cache: [B,Hkv,cap,d] float8_e4m3fn and
+    scales: [B,Hkv,ceil(cap / block),2] float8_e8m0fnu (K's, V's), updated in
+    place; lens: int32 [B], the slots filled before; counts: int32 [B], the new
+    rows of each sequence (default n).  Returns lens_out, int32 [B], the slots
+    filled after: the given tensor, which may be lens, or a new one."""
+    L = _lib()
+    B, Hkv, n, d = shape = _four("k", k)
+    dev = _current_gpu("k", k, stream)
+    _tensor("k", k, shape, dev, _torch.bfloat16)
+    _tensor("v", v, shape, dev, _torch.bfloat16)
+    cap = _codes("k_cache", k_cache, B, Hkv, d, dev)
+    if _codes("v_cache", v_cache, B, Hkv, d, dev) != cap:
+        raise ValueError("k_cache and v_cache must have the same rows")
+    sptr = _scales(scales, B, Hkv, cap, block, dev)
+    i32 = _torch.int32
+    lptr = _tensor("lens", lens, (B,), dev, i32).data_ptr()
+    cptr = None if counts is None else _tensor("counts", counts, (B,), dev, i32).data_ptr()
+    lens_out = _new((B,), i32, k.device, stream) if lens_out is None else _tensor("lens_out", lens_out, (B,), dev, i32)
+    opts = _call_opts(None, stream)
+    rc = L.attn_cache_append(k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), sptr, lptr, cptr,
+                             lens_out.data_ptr(), B, Hkv, n, cap, d, block, ctypes.byref(opts))
+    if rc != ATTN_OK:
+        raise AttnError(rc, "attn_cache_append")
+    return lens_out
+
+
+def attn_decode_blocks_split_keys(B: int, Hq: int, Hkv: int, Sq: int, Sk: int, d: int) -> int:
+    """The library's proposed cut for attn_decode_blocks (0: one part)."""
+    return int(_lib().attn_decode_blocks_split_keys(int(B), int(Hq), int(Hkv), int(Sq), int(Sk), int(d)))
+
+
+def attn_decode_blocks_workspace_bytes(B: int, Hq: int, Sq: int, Sk: int, d: int, split_keys: int) -> int:
+    return int(_lib().attn_decode_blocks_workspace_bytes(int(B), int(Hq), int(Sq), int(Sk), int(d), int(split_keys)))
+
+
+def attn_decode_blocks(q, k, v, scales, *, block: int, causal: bool, scale: float, exp_mode: int, split_keys: int,
+                       lens=None, Sk: int | None = None, stream=None, out=None, lse=None, want_lse: bool = True,
+                       workspace=None):
+    """Attention over a cache of 8-bit blocks (see include/h15qkv.h, attn_decode_blocks).
+
+    q: [B,Hq,Sq,d] bf16; k, v: [B,Hkv,Sk_cap,d] float8_e4m3fn and scales:
+    [B,Hkv,ceil(Sk_cap / block),2] float8_e8m0fnu, as attn_cache_append writes
+    them, whose first lens[b] slots (int32 [B]; default Sk, default all) are
+    filled.  Returns (O [B,Hq,Sq,d] bf16, LSE [B,Hq,Sq] fp32 or None)."""
+    L = _lib()
+    B, Hq, Sq, d = shape = _four("q", q)
+    dev = _current_gpu("q", q, stream)
+    _tensor("q", q, shape, dev, _torch.bfloat16)
+    Hkv = _four("k", k)[1]
+    cap = _codes("k", k, B, Hkv, d, dev)
+    if _codes("v", v, B, Hkv, d, dev) != cap:
+        raise ValueError("k and v must have the same rows")
+    sptr = _scales(scales, B, Hkv, cap, block, dev)
+    Sk = cap if Sk is None else int(Sk)
+    if (Sk | split_keys) >> 31:
+        _refuse(Sk=Sk, split_keys=split_keys)
+    if out is None or lse is None:
+        out, lse = _outputs(q, out, lse, want_lse, stream)
+    else:
+        _tensor("out", out, shape, dev, _torch.bfloat16)
+        _tensor("lse", lse, shape[:3], dev, _torch.float32)
+    wptr, wbytes, workspace = _space(workspace, lambda: L.attn_decode_blocks_workspace_bytes(B, Hq, Sq, Sk, d,
+                                                                                            split_keys), dev, stream)
+    opts = _call_opts(None, stream)
+    rc = L.attn_decode_blocks(q.data_ptr(), k.data_ptr(), v.data_ptr(), sptr, _lens_ptr(lens, B, dev), out.data_ptr(),
+                              lse.data_ptr() if lse is not None else None, B, Hq, Hkv, Sq, Sk, cap, d, block,
+                              1 if causal else 0, scale, exp_mode, split_keys, wptr, wbytes, ctypes.byref(opts))
+    if rc != ATTN_OK:
+        raise AttnError(rc, "attn_decode_blocks")
+    return out, lse

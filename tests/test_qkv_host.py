@@ -1,0 +1,133 @@
+"""The host side of the operators between projections and attention
+(csrc/qkv_api.cpp) built with a host compiler alone and linked with launchers
+that launch nothing (tests/qkv_launch_stub.cpp): which form a call takes, and,
+under AddressSanitizer and UndefinedBehaviorSanitizer, that no refusal reaches a
+launcher."""
+import ctypes
+import os
+import subprocess
+import sys
+from pathlib import Path
+
+import pytest
+
+import paper_2609_33586_amd as pkg
+from oracle import build as obuild
+from paper_2609_33586_amd import qkv
+
+ROOT = Path(__file__).resolve().parent.parent
+CSRC = ROOT / "paper_2609_33586_amd" / "csrc"
+
+
+def at(i):
+    return 0x100000 + (i << 46)  # never dereferenced
+
+
+@pytest.fixture(scope="module")
+def host(tmp_path_factory):
+    lib = tmp_path_factory.mktemp("qkv_host") / "libh15qkv_host.so"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fPIC", "-shared", "-ffp-contract=off", "-Wall", "-Wextra", "-Werror",
+                    f"-I{ROOT / 'include'}", f"-I{CSRC}", str(CSRC / "qkv_api.cpp"),
+                    str(ROOT / "tests" / "qkv_launch_stub.cpp"), "-o", str(lib)], check=True)
+    L = ctypes.CDLL(str(lib))
+    P, I, F, S = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
+    L.attn_rope.argtypes = [P] * 8 + [I] * 6 + [P]
+    L.attn_rope_bwd.argtypes = [P] * 13 + [I] * 5 + [P, S, P]
+    L.attn_cache_append.argtypes = [P] * 8 + [I] * 6 + [P]
+    L.attn_decode_blocks.argtypes = [P] * 7 + [I] * 9 + [F, I, I, P, S, P]
+    L.attn_rope_bwd_workspace_bytes.restype = S
+    return L
+
+
+def spec(rot=64, wt=0, q=True, k=True):
+    s = qkv.attn_rope_spec(None, 0, at(20), rot, 0, 1.0, at(21) if q else None, at(22) if k else None, wt, 1e-6)
+    return ctypes.cast(ctypes.pointer(s), ctypes.c_void_p)
+
+
+def rope_form(L, B, S, Hq, Hkv, d):
+    assert L.attn_rope(at(0), at(1), at(2), None, spec(), at(3), at(4), at(5), B, S, Hq, Hkv, d, 0, None) == pkg.ATTN_ELAUNCH
+    return {n: L.h15_stub_rope(i) for i, n in enumerate(("tiles", "run", "groups", "q", "k", "v"))}
+
+
+@pytest.mark.parametrize("B,S,Hq,Hkv,d", [(1, 1, 1, 1, 64), (4, 1, 8, 2, 64), (1, 33, 32, 8, 128), (2, 4096, 32, 8, 128), (64, 16384, 64, 8, 64),
+                                          (1, 200, 7, 7, 128), (3, 1001, 24, 8, 128)])
+def test_rope_runs_cover_every_head(host, B, S, Hq, Hkv, d):
+    f = rope_form(host, B, S, Hq, Hkv, d)
+    assert f["tiles"] == -(-B * S // (4096 // d)) and f["run"] >= 1
+    assert f["q"] == -(-Hq // f["run"]) and f["k"] == f["v"] == -(-Hkv // f["run"])
+    assert 1 <= f["groups"] <= f["tiles"]
+
+
+@pytest.mark.parametrize("q,k", [(True, True), (True, False), (False, True), (False, False)])
+def test_backward_workspace_holds_its_rows(host, q, k):
+    for B, S, Hq, Hkv, d in ((1, 1, 1, 1, 64), (4, 2048, 32, 8, 128), (3, 777, 8, 2, 64), (64, 8192, 8, 1, 128)):
+        need = host.attn_rope_bwd_workspace_bytes(B, S, Hq, Hkv, d)
+        for have_v in (True, False):
+            rc = host.attn_rope_bwd(at(0), at(1), at(2) if have_v else None, at(3), at(4), None, spec(q=q, k=k), at(5), at(6),
+                                    at(7) if have_v else None, None, at(8), at(9), B, S, Hq, Hkv, d, at(10), need, None)
+            assert rc == pkg.ATTN_ELAUNCH
+            rows = [host.h15_stub_rope(3 + i) * host.h15_stub_rope(2) for i in range(2)]
+            end = max((host.h15_stub_rope(6 + i) + rows[i] for i, have in enumerate((q, k)) if have), default=0)
+            assert end * d * 4 <= need
+            if q and k:
+                assert host.h15_stub_rope(6) == 0 and host.h15_stub_rope(7) == rows[0]
+
+
+def test_append_reach(host):
+    def form(n, cap, block, in_place=False):
+        rc = host.attn_cache_append(at(0), at(1), at(2), at(3), at(4), at(5), None, at(5 if in_place else 6), 2, 2, n, cap, 64, block, None)
+        assert rc == pkg.ATTN_ELAUNCH
+        return tuple(host.h15_stub_append(i) for i in range(3))
+
+    # n rows from any slot on lie in so many blocks at most, never in more than there are
+    for block in (16, 32, 64, 128):
+        for n in (1, 2, block - 1, block, block + 1, 5 * block + 3):
+            most = max((s + n - 1) // block + 1 for s in range(block))
+            assert form(n, 100 * block, block) == (100, most, 0)
+            assert form(n, 2 * block - 1, block) == (2, min(most, 2), 0)
+    assert form(1, 64, 64, True) == (1, 1, 1)
+
+
+def blocks_form(L, B, Hq, Hkv, Sq, Sk, cut=0, lens=at(4), causal=1, d=128, block=64):
+    rc = L.attn_decode_blocks(at(0), at(1), at(2), at(3), lens, at(5), None, B, Hq, Hkv, Sq, Sk, Sk, d, block, causal, 0.1, 0, cut,
+                              at(7), 1 << 40, None)
+    assert rc == pkg.ATTN_ELAUNCH
+    names = ("parts", "split", "rows", "row_blocks", "groups", "causal", "longest", "blocks", "shift")
+    return {n: L.h15_stub_blocks(i) for i, n in enumerate(names)}
+
+
+def test_blocks_forms(host):
+    f = blocks_form(host, 4, 8, 2, 1, 500)
+    assert f["parts"] == 1 and f["split"] == 512 and f["rows"] == 32 and f["groups"] == 8 and f["causal"] == 0 and f["longest"] == 0
+    f = blocks_form(host, 4, 8, 2, 3, 500, 256, block=16)
+    assert f["parts"] == 2 and f["split"] == 256 and f["groups"] == 16 and f["causal"] == 1 and f["shift"] == 4 and f["blocks"] == 32
+    # up to 128 rows of a KV head: workgroups of 32, else of 128
+    assert blocks_form(host, 1, 8, 2, 32, 500)["rows"] == 32 and blocks_form(host, 1, 8, 2, 32, 500)["row_blocks"] == 4
+    assert blocks_form(host, 1, 8, 2, 33, 500)["rows"] == 128 and blocks_form(host, 1, 8, 2, 33, 500)["row_blocks"] == 2
+    assert blocks_form(host, 1, 8, 2, 33, 500, causal=0)["causal"] == 0
+    assert blocks_form(host, 64, 32, 8, 1, 500)["longest"] == 0 and blocks_form(host, 65, 32, 8, 1, 500)["longest"] == 1
+    assert blocks_form(host, 65, 32, 8, 1, 500, lens=None)["longest"] == 0 and blocks_form(host, 257, 32, 8, 1, 500)["longest"] == 0
+
+
+def test_checks_under_sanitizers(tmp_path):
+    lib = tmp_path / "libh15qkv_san.so"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fno-omit-frame-pointer", "-fsanitize=address,undefined",
+                    "-fno-sanitize-recover=all", "-fPIC", "-shared", "-ffp-contract=off", f"-I{ROOT / 'include'}", f"-I{CSRC}",
+                    str(CSRC / "attn_api.cpp"), str(CSRC / "cache_api.cpp"), str(CSRC / "qkv_api.cpp"),
+                    str(ROOT / "tests" / "sanitize_launch_stub.cpp"), "-c"], cwd=tmp_path, check=True)
+    for stub, name in (("cache", "h15_cache_stub_launches"),):
+        subprocess.run(["g++", "-std=c++17", "-O1", "-fPIC", f"-Dh15_stub_launches={name}", f"-I{ROOT / 'include'}", f"-I{CSRC}",
+                        str(ROOT / "tests" / f"{stub}_launch_stub.cpp"), "-c"], cwd=tmp_path, check=True)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-fPIC", "-shared",
+                    f"-I{ROOT / 'include'}", f"-I{CSRC}", str(ROOT / "tests" / "qkv_launch_stub.cpp"),
+                    *(str(tmp_path / f"{n}.o") for n in ("attn_api", "cache_api", "qkv_api", "sanitize_launch_stub", "cache_launch_stub")),
+                    "-o", str(lib)], check=True)
+    env = dict(os.environ, LD_PRELOAD=obuild.sanitizer_preload(), ASAN_OPTIONS="detect_leaks=0:abort_on_error=0",
+               UBSAN_OPTIONS="print_stacktrace=1", H15ATTN_LIB=str(lib))
+    code = ("import sys, pytest; rc = pytest.main(['tests/test_qkv_api.py', '-q', '-p', 'no:cacheprovider']); "
+            "import paper_2609_33586_amd as p; assert p.lib()._name == %r and p.lib().h15_stub_qkv_launches() == 0; "
+            "sys.exit(rc)" % str(lib))
+    res = subprocess.run([sys.executable, "-c", code], cwd=ROOT, env=env, capture_output=True, text=True, timeout=600)
+    out = res.stdout + res.stderr
+    assert "AddressSanitizer" not in out and "runtime error" not in out, out[-4000:]
+    assert res.returncode == 0 and " passed" in out, out[-4000:]
