@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 
 from . import ATTN_BF16, ATTN_FP8_E4M3, ATTN_OK, AttnError, _dtype_of, _new, _outputs, attn_opts, cache, lib
 from .cache import _call_opts, _current_gpu, _four, _lens_ptr, _refuse, _space, _tensor
@@ -19,10 +20,6 @@ EXPORTS = ("attn_rope", "attn_rope_bwd", "attn_rope_bwd_workspace_bytes", "attn_
            "attn_decode_blocks_workspace_bytes", "attn_decode_blocks_split_keys")
 
 
-class attn_strides(ctypes.Structure):
-    _fields_ = [("batch", ctypes.c_int64), ("position", ctypes.c_int64), ("head", ctypes.c_int64)]
-
-
 class attn_rope_spec(ctypes.Structure):
     _fields_ = [("positions", ctypes.c_void_p), ("each_position", ctypes.c_int), ("freqs", ctypes.c_void_p),
                 ("rot", ctypes.c_int), ("interleaved", ctypes.c_int), ("amplitude", ctypes.c_float),
@@ -32,20 +29,20 @@ class attn_rope_spec(ctypes.Structure):
 
 _bound = None
 _torch = None
-_Strides3 = ctypes.c_int64 * 9  # attn_strides of three tensors
+_bf16 = _f32 = _f64 = _i32 = _fp8 = None  # torch's types, bound with the library
 
 
 def _lib() -> ctypes.CDLL:
     """The library with the argument types of these functions, bound on first use."""
-    global _bound, _torch
+    global _bound, _torch, _bf16, _f32, _f64, _i32, _fp8
     if _bound is not None:
         return _bound
     L = lib()
     P, I, F, S = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
-    R, O = ctypes.POINTER(attn_rope_spec), ctypes.POINTER(attn_opts)
+    O = ctypes.POINTER(attn_opts)
     for name, args, res in (
-            ("attn_rope", [P, P, P, P, R, P, P, P] + [I] * 6 + [O], I),
-            ("attn_rope_bwd", [P] * 6 + [R] + [P] * 6 + [I] * 5 + [P, S, O], I),
+            ("attn_rope", [P] * 8 + [I] * 6 + [O], I),
+            ("attn_rope_bwd", [P] * 13 + [I] * 5 + [P, S, O], I),
             ("attn_rope_bwd_workspace_bytes", [I] * 5, S),
             ("attn_cache_append", [P] * 8 + [I] * 6 + [O], I),
             ("attn_decode_blocks", [P] * 7 + [I] * 9 + [F, I, I, P, S, O], I),
@@ -55,6 +52,7 @@ def _lib() -> ctypes.CDLL:
         fn.argtypes, fn.restype = args, res
     import torch
     _torch = torch
+    _bf16, _f32, _f64, _i32, _fp8 = torch.bfloat16, torch.float32, torch.float64, torch.int32, torch.float8_e4m3fn
     cache._lib()  # (its checks use its own binding of torch)
     _bound = L
     return L
@@ -110,49 +108,65 @@ def attn_rope_frequencies(rot: int, base: float = 10000.0, *, scaling: str | Non
 
 # ---- norms and rotation -------------------------------------------------------
 
+# (The smallest calls are bound by these checks: a decode step's rotation of four
+# chats takes the GPU 4 us.)
 def _strided(name, t, B, S, d, dev):
     """Heads and the three strides of a bf16 tensor [B,S,H,d] whose rows are contiguous."""
     shape = t.shape
-    if (len(shape) != 4 or shape[0] != B or shape[1] != S or shape[3] != d or t.get_device() != dev
-            or t.dtype != _torch.bfloat16):
+    if len(shape) != 4 or t.dtype is not _bf16 or t.get_device() != dev:
+        raise ValueError(f"{name} must be a bfloat16 tensor [{B}x{S}xHx{d}] on GPU {dev}")
+    b, s, H, e = shape
+    if b != B or s != S or e != d:
         raise ValueError(f"{name} must be a bfloat16 tensor [{B}x{S}xHx{d}] on GPU {dev}")
     sb, ss, sh, sd = t.stride()
     if sd != 1:
         raise ValueError(f"the rows of {name} must be contiguous")
-    H = shape[2]
     # (the stride of a dimension of one element says nothing)
-    return H, (sb if B > 1 else 0, ss if S > 1 else 0, sh if H > 1 else 0)
+    return H, sb if B > 1 else 0, ss if S > 1 else 0, sh if H > 1 else 0
 
 
-def _apart(name, t):
-    """An output must not lie over itself: its dimensions, the smallest stride first, each beyond the ones before."""
-    end = 1
-    for stride, n in sorted(zip(t.stride(), t.shape)):
+def _apart(name, t, H, sb, ss, sh):
+    """An output of these heads and strides must not lie over itself: its dimensions, the smallest stride first, each
+    beyond the ones before."""
+    B, S, _, d = t.shape
+    row = (H - 1) * sh + d
+    if (sh >= d or H == 1) and (ss >= row or S == 1) and (sb >= (S - 1) * ss + row or B == 1):
+        return  # batches outside positions outside heads
+    end = d
+    for stride, n in sorted(((sb, B), (ss, S), (sh, H))):
         if n > 1 and stride < end:
             raise ValueError(f"rows of {name} overlap")
-        if n > 1:
-            end = stride * (n - 1) + end
-    return t
+        end += stride * (n - 1)
+
+
+_pack_spec = struct.Struct("@PiPiifPPif").pack  # attn_rope_spec, which a call reads before it returns
+_pack_strides = struct.Struct("@9q").pack  # attn_strides of three tensors
 
 
 def _spec(B, S, d, dev, freqs, positions, interleaved, amplitude, q_weight, k_weight, eps):
-    pptr, each, fptr, rot = None, 0, None, 0
+    pptr = fptr = rot = each = 0
     if freqs is not None:
         rot = 2 * freqs.numel()
-        fptr = _tensor("freqs", freqs, (rot // 2,), dev, _torch.float64).data_ptr()
+        if freqs.dtype is not _f64 or freqs.dim() != 1 or not freqs.is_contiguous() or freqs.get_device() != dev:
+            _tensor("freqs", freqs, (rot // 2,), dev, _f64)
+        fptr = freqs.data_ptr()
     if positions is not None:
-        each = 1 if len(positions.shape) == 2 else 0
-        pptr = _tensor("positions", positions, (B, S) if each else (B,), dev, _torch.int32).data_ptr()
-    kind = None
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is None:
-            continue
-        if w.dtype != _torch.bfloat16 and w.dtype != _torch.float32 or kind not in (None, w.dtype):
-            raise TypeError("q_weight and k_weight must be bfloat16, or both float32")
-        kind = _tensor(name, w, (d,), dev).dtype
-    wq, wk = (None if w is None else w.data_ptr() for w in (q_weight, k_weight))
-    wt = ATTN_FP32 if kind == _torch.float32 else ATTN_BF16
-    return attn_rope_spec(pptr, each, fptr, rot, 1 if interleaved else 0, amplitude, wq, wk, wt, eps)
+        each = 1 if positions.dim() == 2 else 0
+        pptr = _tensor("positions", positions, (B, S) if each else (B,), dev, _i32).data_ptr()
+    wq = wk = 0
+    wt = ATTN_BF16
+    if q_weight is not None or k_weight is not None:
+        kind = None
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is None:
+                continue
+            if w.dtype is not _bf16 and w.dtype is not _f32 or kind not in (None, w.dtype):
+                raise TypeError("q_weight and k_weight must be bfloat16, or both float32")
+            kind = _tensor(name, w, (d,), dev).dtype
+        wq = 0 if q_weight is None else q_weight.data_ptr()
+        wk = 0 if k_weight is None else k_weight.data_ptr()
+        wt = ATTN_FP32 if kind is _f32 else ATTN_BF16
+    return _pack_spec(pptr, each, fptr, rot, 1 if interleaved else 0, amplitude, wq, wk, wt, eps)
 
 
 def attn_rope(q, k=None, v=None, *, freqs=None, positions=None, interleaved: bool = False, amplitude: float = 1.0,
@@ -173,49 +187,76 @@ def attn_rope(q, k=None, v=None, *, freqs=None, positions=None, interleaved: boo
     first = q if q is not None else k if k is not None else v
     if first is None:
         raise ValueError("q, k and v: one at least")
-    B, S, _, d = shape = first.shape
     dev = _current_gpu("q", first, stream)
+    if len(first.shape) != 4:
+        raise ValueError("q must be a 4-D tensor [B,S,H,d]")
+    B, S, _, d = first.shape
     given = q_out if q_out is not None else k_out if k_out is not None else v_out
-    dtype = given.dtype if given is not None else _torch.bfloat16 if out_dtype is None else out_dtype
-    dt = _dtype_of(given) if given is not None else ATTN_FP8_E4M3 if dtype == _torch.float8_e4m3fn else ATTN_BF16
-    if given is None and dtype not in (_torch.bfloat16, _torch.float8_e4m3fn):
-        raise TypeError("out_dtype must be bfloat16 or float8_e4m3fn")
-    Hq = Hkv = 0
-    strides, ins, outs = [], [], []
-    for name, t, out in (("q", q, q_out), ("k", k, k_out), ("v", v, v_out)):
-        if t is None:
-            if out is not None:
-                raise ValueError(f"{name}_out without {name}")
-            strides += (0, 0, 0)
-            ins.append(None)
-            outs.append(None)
-            continue
-        H, st = _strided(name, t, B, S, d, dev)
-        if name == "q":
-            Hq = H
-        elif Hkv and H != Hkv:
+    dtype = given.dtype if given is not None else _bf16 if out_dtype is None else out_dtype
+    if dtype is not _bf16 and dtype is not _fp8:
+        raise TypeError("attn_rope writes bfloat16 or float8_e4m3fn")
+    Hq = Hkv = a = b = c = e = f = g = h = i = j = 0
+    qp = kp = vp = qo = ko = vo = None
+    if q is not None:
+        Hq, a, b, c = _strided("q", q, B, S, d, dev)
+        qp = q.data_ptr()
+        q_out = _new((B, Hq, S, d), dtype, first.device, stream) if q_out is None else \
+            _tensor("q_out", q_out, (B, Hq, S, d), dev, dtype)
+        qo = q_out.data_ptr()
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if k is not None:
+        Hkv, e, f, g = _strided("k", k, B, S, d, dev)
+        kp = k.data_ptr()
+        k_out = _new((B, Hkv, S, d), dtype, first.device, stream) if k_out is None else \
+            _tensor("k_out", k_out, (B, Hkv, S, d), dev, dtype)
+        ko = k_out.data_ptr()
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    if v is not None:
+        n, h, i, j = _strided("v", v, B, S, d, dev)
+        if k is not None and n != Hkv:
             raise ValueError("k and v must have the same heads")
-        else:
-            Hkv = H
-        strides += st
-        ins.append(t.data_ptr())
-        shape = (B, H, S, d)
-        if out is None:
-            out = _new(shape, dtype, first.device, stream)
-        else:
-            _tensor(name + "_out", out, shape, dev, dtype)
-        outs.append(out)
+        Hkv, vp = n, v.data_ptr()
+        v_out = _new((B, Hkv, S, d), dtype, first.device, stream) if v_out is None else \
+            _tensor("v_out", v_out, (B, Hkv, S, d), dev, dtype)
+        vo = v_out.data_ptr()
+    elif v_out is not None:
+        raise ValueError("v_out without v")
     spec = _spec(B, S, d, dev, freqs, positions, interleaved, amplitude, q_weight, k_weight, eps)
-    opts = _call_opts(descale, stream)
-    rc = L.attn_rope(ins[0], ins[1], ins[2], _Strides3(*strides), ctypes.byref(spec),
-                     *[None if o is None else o.data_ptr() for o in outs], B, S, Hq, Hkv, d, dt, ctypes.byref(opts))
+    rc = L.attn_rope(qp, kp, vp, _pack_strides(a, b, c, e, f, g, h, i, j), spec, qo, ko, vo, B, S, Hq, Hkv, d,
+                     ATTN_BF16 if dtype is _bf16 else ATTN_FP8_E4M3, ctypes.byref(_call_opts(descale, stream)))
     if rc != ATTN_OK:
         raise AttnError(rc, "attn_rope")
-    return outs[0], outs[1], outs[2]
+    return q_out, k_out, v_out
 
 
 def attn_rope_bwd_workspace_bytes(B: int, S: int, Hq: int, Hkv: int, d: int) -> int:
     return int(_lib().attn_rope_bwd_workspace_bytes(int(B), int(S), int(Hq), int(Hkv), int(d)))
+
+
+def _grad(name, g, out, B, S, d, dev, first, stream):
+    """Heads of a gradient g [B,H,S,d], the tensor [B,S,H,d] for what it becomes, and that one's strides."""
+    H = _four("g" + name, g)[1]
+    _tensor("g" + name, g, (B, H, S, d), dev, _bf16)
+    if out is None:
+        out = _new((B, S, H, d), _bf16, first.device, stream)
+    n, sb, ss, sh = _strided("d" + name, out, B, S, d, dev)
+    if n != H:
+        raise ValueError(f"d{name} must have g{name}'s heads")
+    _apart("d" + name, out, H, sb, ss, sh)
+    return H, out, (sb, ss, sh)
+
+
+def _with_weight(name, x, dw, B, S, H, d, dev, first, stream):
+    """The tensor for a weight's gradient, and the strides of the rows x that it takes."""
+    if x is None:
+        raise ValueError(f"{name} is required with {name}_weight")
+    n, sb, ss, sh = _strided(name, x, B, S, d, dev)
+    if n != H:
+        raise ValueError(f"{name} must have g{name}'s heads")
+    dw = _new((d,), _f32, first.device, stream) if dw is None else _tensor(f"d{name}_weight", dw, (d,), dev, _f32)
+    return dw, sb, ss, sh
 
 
 def attn_rope_bwd(gq, gk=None, gv=None, *, q=None, k=None, freqs=None, positions=None, interleaved: bool = False,
@@ -232,68 +273,58 @@ def attn_rope_bwd(gq, gk=None, gv=None, *, q=None, k=None, freqs=None, positions
     first = gq if gq is not None else gk if gk is not None else gv
     if first is None:
         raise ValueError("gq, gk and gv: one at least")
-    B, _, S, d = shape = first.shape
-    dev, f32 = _current_gpu("gq", first, stream), _torch.float32
+    dev = _current_gpu("gq", first, stream)
+    B, _, S, d = _four("gq", first)
+    a = b = c = e = f = g = 0
+    qp = kp = qd = kd = vd = wqp = wkp = None
     Hq = Hkv = 0
-    strides, grad_strides, gs, ins, outs, sums = [], [], [], [], [], []
-    for name, g, x, out, w, dw in (("q", gq, q, dq, q_weight, dq_weight), ("k", gk, k, dk, k_weight, dk_weight),
-                                   ("v", gv, None, dv, None, None)):
-        if g is None:
-            if out is not None or dw is not None:
-                raise ValueError(f"d{name} without g{name}")
-            strides += (0, 0, 0)
-            grad_strides += (0, 0, 0)
-            gs.append(None)
-            ins.append(None)
-            outs.append(None)
-            sums.append(None)
-            continue
-        shape = g.shape
-        if len(shape) != 4:
-            raise ValueError(f"g{name} must be a 4-D tensor")
-        H = shape[1]
-        _tensor("g" + name, g, (B, H, S, d), dev, _torch.bfloat16)
-        if name == "q":
-            Hq = H
-        elif Hkv and H != Hkv:
+    if gq is not None:
+        Hq, dq, grads = _grad("q", gq, dq, B, S, d, dev, first, stream)
+        if q_weight is not None:
+            dq_weight, a, b, c = _with_weight("q", q, dq_weight, B, S, Hq, d, dev, first, stream)
+            qp, wqp = q.data_ptr(), dq_weight.data_ptr()
+        elif dq_weight is not None:
+            raise ValueError("dq_weight without q_weight")
+        qd = dq.data_ptr()
+    elif dq is not None or dq_weight is not None:
+        raise ValueError("dq or dq_weight without gq")
+    else:
+        grads = (0, 0, 0)
+    if gk is not None:
+        Hkv, dk, more = _grad("k", gk, dk, B, S, d, dev, first, stream)
+        grads += more
+        if k_weight is not None:
+            dk_weight, e, f, g = _with_weight("k", k, dk_weight, B, S, Hkv, d, dev, first, stream)
+            kp, wkp = k.data_ptr(), dk_weight.data_ptr()
+        elif dk_weight is not None:
+            raise ValueError("dk_weight without k_weight")
+        kd = dk.data_ptr()
+    elif dk is not None or dk_weight is not None:
+        raise ValueError("dk or dk_weight without gk")
+    else:
+        grads += (0, 0, 0)
+    if gv is not None:
+        n, dv, more = _grad("v", gv, dv, B, S, d, dev, first, stream)
+        grads += more
+        if gk is not None and n != Hkv:
             raise ValueError("gk and gv must have the same heads")
-        else:
-            Hkv = H
-        gs.append(g.data_ptr())
-        if w is not None:
-            if x is None:
-                raise ValueError(f"{name} is required with {name}_weight")
-            n, st = _strided(name, x, B, S, d, dev)
-            if n != H:
-                raise ValueError(f"{name} must have g{name}'s heads")
-            strides += st
-            ins.append(x.data_ptr())
-            sums.append(_new((d,), f32, first.device, stream) if dw is None
-                        else _tensor(f"d{name}_weight", dw, (d,), dev, f32))
-        else:
-            if dw is not None:
-                raise ValueError(f"d{name}_weight without {name}_weight")
-            strides += (0, 0, 0)
-            ins.append(None)
-            sums.append(None)
-        if out is None:
-            out = _new((B, S, H, d), _torch.bfloat16, first.device, stream)
-        n, st = _strided("d" + name, _apart("d" + name, out), B, S, d, dev)
-        if n != H:
-            raise ValueError(f"d{name} must have g{name}'s heads")
-        grad_strides += st
-        outs.append(out)
+        Hkv, vd = n, dv.data_ptr()
+    elif dv is not None:
+        raise ValueError("dv without gv")
+    else:
+        grads += (0, 0, 0)
     spec = _spec(B, S, d, dev, freqs, positions, interleaved, amplitude, q_weight, k_weight, eps)
-    wptr, wbytes, workspace = _space(workspace, lambda: L.attn_rope_bwd_workspace_bytes(B, S, Hq, Hkv, d) if (
-        sums[0] is not None or sums[1] is not None) else 0, dev, stream)
-    opts = _call_opts(None, stream)
-    rc = L.attn_rope_bwd(gs[0], gs[1], gs[2], ins[0], ins[1], _Strides3(*strides), ctypes.byref(spec),
-                         *[None if o is None else o.data_ptr() for o in outs], _Strides3(*grad_strides),
-                         *[None if o is None else o.data_ptr() for o in sums[:2]], B, S, Hq, Hkv, d, wptr, wbytes,
-                         ctypes.byref(opts))
+    wptr = wbytes = 0
+    if wqp is not None or wkp is not None:
+        wptr, wbytes, workspace = _space(workspace, lambda: L.attn_rope_bwd_workspace_bytes(B, S, Hq, Hkv, d), dev,
+                                         stream)
+    rc = L.attn_rope_bwd(None if gq is None else gq.data_ptr(), None if gk is None else gk.data_ptr(),
+                         None if gv is None else gv.data_ptr(), qp, kp, _pack_strides(a, b, c, e, f, g, 0, 0, 0), spec,
+                         qd, kd, vd, _pack_strides(*grads), wqp, wkp, B, S, Hq, Hkv, d, wptr, wbytes,
+                         ctypes.byref(_call_opts(None, stream)))
     if rc != ATTN_OK:
         raise AttnError(rc, "attn_rope_bwd")
-    return outs[0], outs[1], outs[2], sums[0], sums[1]
+    return dq, dk, dv, dq_weight, dk_weight
 
 
 # ---- a cache of 8-bit blocks ----------------------------------------------------
@@ -326,16 +357,16 @@ def attn_cache_append(k, v, k_cache, v_cache, scales, lens, *, block: int, count
     L = _lib()
     B, Hkv, n, d = shape = _four("k", k)
     dev = _current_gpu("k", k, stream)
-    _tensor("k", k, shape, dev, _torch.bfloat16)
-    _tensor("v", v, shape, dev, _torch.bfloat16)
+    _tensor("k", k, shape, dev, _bf16)
+    _tensor("v", v, shape, dev, _bf16)
     cap = _codes("k_cache", k_cache, B, Hkv, d, dev)
     if _codes("v_cache", v_cache, B, Hkv, d, dev) != cap:
         raise ValueError("k_cache and v_cache must have the same rows")
     sptr = _scales(scales, B, Hkv, cap, block, dev)
-    i32 = _torch.int32
-    lptr = _tensor("lens", lens, (B,), dev, i32).data_ptr()
-    cptr = None if counts is None else _tensor("counts", counts, (B,), dev, i32).data_ptr()
-    lens_out = _new((B,), i32, k.device, stream) if lens_out is None else _tensor("lens_out", lens_out, (B,), dev, i32)
+    lptr = _tensor("lens", lens, (B,), dev, _i32).data_ptr()
+    cptr = None if counts is None else _tensor("counts", counts, (B,), dev, _i32).data_ptr()
+    lens_out = _new((B,), _i32, k.device, stream) if lens_out is None else \
+        _tensor("lens_out", lens_out, (B,), dev, _i32)
     opts = _call_opts(None, stream)
     rc = L.attn_cache_append(k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), sptr, lptr, cptr,
                              lens_out.data_ptr(), B, Hkv, n, cap, d, block, ctypes.byref(opts))
@@ -365,7 +396,7 @@ def attn_decode_blocks(q, k, v, scales, *, block: int, causal: bool, scale: floa
     L = _lib()
     B, Hq, Sq, d = shape = _four("q", q)
     dev = _current_gpu("q", q, stream)
-    _tensor("q", q, shape, dev, _torch.bfloat16)
+    _tensor("q", q, shape, dev, _bf16)
     Hkv = _four("k", k)[1]
     cap = _codes("k", k, B, Hkv, d, dev)
     if _codes("v", v, B, Hkv, d, dev) != cap:
@@ -377,8 +408,8 @@ def attn_decode_blocks(q, k, v, scales, *, block: int, causal: bool, scale: floa
     if out is None or lse is None:
         out, lse = _outputs(q, out, lse, want_lse, stream)
     else:
-        _tensor("out", out, shape, dev, _torch.bfloat16)
-        _tensor("lse", lse, shape[:3], dev, _torch.float32)
+        _tensor("out", out, shape, dev, _bf16)
+        _tensor("lse", lse, shape[:3], dev, _f32)
     wptr, wbytes, workspace = _space(workspace, lambda: L.attn_decode_blocks_workspace_bytes(B, Hq, Sq, Sk, d,
                                                                                             split_keys), dev, stream)
     opts = _call_opts(None, stream)

@@ -41,7 +41,7 @@ SPEC = dict(positions=at(10), each=0, freqs=at(11), rot=64, inter=0, amplitude=1
 
 
 def spec(**kw):
-    return ctypes.byref(qkv.attn_rope_spec(*{**SPEC, **kw}.values()))
+    return ctypes.cast(ctypes.pointer(qkv.attn_rope_spec(*{**SPEC, **kw}.values())), ctypes.c_void_p)
 
 
 def strides(*nine):
@@ -205,22 +205,30 @@ def test_binding_refuses_host_tensors_and_nothing():
 
 def test_binding_checks_of_tensors(L):
     x = torch.zeros(2, 5, 3, 64, dtype=torch.bfloat16)  # (device -1: the host)
-    assert qkv._strided("x", x, 2, 5, 64, -1) == (3, (5 * 3 * 64, 3 * 64, 64))
-    assert qkv._strided("x", x[:1, :1, :1], 1, 1, 64, -1) == (1, (0, 0, 0))
+    assert qkv._strided("x", x, 2, 5, 64, -1) == (3, 5 * 3 * 64, 3 * 64, 64)
+    assert qkv._strided("x", x[:1, :1, :1], 1, 1, 64, -1) == (1, 0, 0, 0)
     for bad in (x.float(), x[0], x[:, :4], x[..., :32], x[:1]):
         with pytest.raises(ValueError, match="x must be"):
             qkv._strided("x", bad, 2, 5, 64, -1)
     with pytest.raises(ValueError, match="rows of x"):
         qkv._strided("x", torch.zeros(2, 5, 64, 64, dtype=torch.bfloat16).transpose(2, 3), 2, 5, 64, -1)
-    assert qkv._apart("x", x) is x and qkv._apart("x", x.transpose(1, 2)[:, ::2]) is not None
-    for bad in (x[:1].expand(2, 5, 3, 64), x.as_strided((2, 5, 3, 64), (960, 64, 64, 1)), x.as_strided((2, 5, 3, 64), (320, 64, 320, 1))):
+    def apart(y):
+        n, *st = qkv._strided("x", y, *y.shape[:2], 64, -1)
+        return qkv._apart("x", y, n, *st)
+
+    for good in (x, x[:, ::2], x.transpose(1, 2), x.transpose(0, 1), x.transpose(0, 2)[:, ::2], x[:1].expand(1, 5, 3, 64),
+                 x.as_strided((2, 5, 1, 64), (960, 64, 0, 1))):
+        apart(good)
+    for bad in (x[:1].expand(2, 5, 3, 64), x.as_strided((2, 5, 3, 64), (960, 64, 64, 1)),
+                x.as_strided((2, 5, 3, 64), (320, 64, 320, 1)), x.as_strided((2, 5, 3, 64), (960, 192, 56, 1))):
         with pytest.raises(ValueError, match="overlap"):
-            qkv._apart("x", bad)
+            apart(bad)
     f, w = torch.zeros(16, dtype=torch.float64), torch.zeros(64)
     good = dict(freqs=f, positions=None, interleaved=False, amplitude=1.0, q_weight=w, k_weight=None, eps=1e-6)
-    s = qkv._spec(2, 5, 64, -1, **good)
+    s = qkv.attn_rope_spec.from_buffer_copy(qkv._spec(2, 5, 64, -1, **good))  # (packed as the C struct lies)
+    assert abs(s.eps - 1e-6) < 1e-12 and s.amplitude == 1.0 and s.freqs == f.data_ptr() and s.q_weight == w.data_ptr()
     assert s.rot == 32 and s.weight_dtype == pkg.ATTN_FP32 and s.k_weight is None
-    s = qkv._spec(2, 5, 64, -1, **{**good, "positions": torch.zeros(2, 5, dtype=torch.int32), "q_weight": w.bfloat16()})
+    s = qkv.attn_rope_spec.from_buffer_copy(qkv._spec(2, 5, 64, -1, **{**good, "positions": torch.zeros(2, 5, dtype=torch.int32), "q_weight": w.bfloat16()}))
     assert s.each_position == 1 and s.weight_dtype == pkg.ATTN_BF16
     for kw in ({"freqs": f.float()}, {"positions": torch.zeros(2, 5)}, {"positions": torch.zeros(5, dtype=torch.int32)},
                {"positions": torch.zeros(2, 4, dtype=torch.int32)}, {"q_weight": w[:32]}):
