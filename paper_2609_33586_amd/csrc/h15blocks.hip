@@ -443,16 +443,234 @@ __device__ __forceinline__ void rows_form(const BlocksParams& p, const Work& w, 
   }
 }
 
-template <int D, int MODE, bool ROWS>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_blocks_kernel(
-    BlocksParams p) {
-  using C = BCfg<D>;
-  // (arrays of their own, so that the compiler tells the copies apart)
-  __shared__ __attribute__((aligned(16))) uint8_t ksm[C::AREA];
-  __shared__ __attribute__((aligned(16))) uint8_t vsm[C::AREA];
-  __shared__ __attribute__((aligned(16))) float mx_lds[2][32][NW];
-  __shared__ __attribute__((aligned(16))) float m_lds[32][NW], l_lds[32][NW];
-  Work w;
+// ---- the wide form: 512 query rows, 64 a wave, the hardware exponential.
+// Eight waves, two on a SIMD: while the four of one group are at the matrix core
+// (P V of the last step, Q K^T of this one), those of the other make weights, and
+// a barrier after each such half step keeps it so.
+template <int D>
+struct WCfg {
+  static constexpr int NW = BLOCKS_WIDE / 64;
+  static constexpr int RB = D, NCH = D / 16;
+  static constexpr int STEP = 32, NB = 1, HALF = STEP * RB;  // keys of a step, blocks of 32, bytes of its K
+  static constexpr int QRB = 2 * D;  // bytes of a query row
+  static constexpr int QAREA = BLOCKS_WIDE * QRB;
+};
+
+// 2^(c1 s + nb) of 16 scores, and their sum
+__device__ __forceinline__ float weights(const f32x16& s, float (&e)[16], float nb, float c1) {
+  float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j], c1, nb));
+    a[j & 3] = j < 4 ? e[j] : a[j & 3] + e[j];
+  }
+  return (a[0] + a[1]) + (a[2] + a[3]);
+}
+
+template <int D>
+__device__ __forceinline__ void wide_form(const BlocksParams& p, const Work& w, uint8_t* qsm, uint8_t* b0, uint8_t* b1,
+                                          uint8_t* b2) {
+  using C = WCfg<D>;
+  constexpr int RB = C::RB, NCH = C::NCH, NDB = D / 32, NB = C::NB, STEP = C::STEP, QCH = C::QRB / 16;
+  const int tid = threadIdx.x, lane = tid & 63, i32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t part_bytes = (uint32_t)w.nk * RB;
+  // a wave copies 1 KB of each step: of K those of the first group, of V the others
+  // (two of each at d = 64)
+  const bool of_v = wave >= C::NW / 2;
+  const auto rsrc = rows_rsrc(of_v ? w.v : w.k, part_bytes);
+  const auto srsrc = rows_rsrc(w.scales, w.used);
+  const int mine = wave & (C::NW / 2 - 1);
+  uint32_t off;
+  {
+    const int r = copy_row<NCH>(mine, lane), first = mine * (64 / NCH);
+    off = (r - first) * RB + (((lane % NCH) ^ (of_v ? v_swz<DT_FP8, D>(r) : k_swz<DT_FP8, D>(r))) << 4);
+  }
+  auto stage = [&](int c, uint8_t* buf, int (&pair)[NB]) __attribute__((always_inline)) {
+    const uint32_t soff = min((uint32_t)c * C::HALF + mine * 1024, part_bytes);
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) pair[kb] = scale_pair(p, srsrc, w.j0 + c * STEP + 32 * kb + i32);
+    if (C::HALF == C::NW * 512 || mine < C::HALF / 1024)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, LDS_PTR(void, buf + (of_v ? C::HALF : 0) + mine * 1024), 16, off, soff,
+                                               0, 0);
+  };
+  // the query rows, chunk 4 t + 2 g + j of a row at 4 t + 2 j + g: operand 2 t + j of half g
+#pragma unroll 4
+  for (int i = tid; i < BLOCKS_WIDE * QCH; i += C::NW * 64) {
+    const int r = i / QCH, c = i % QCH;
+    const i32x4 x = *(const i32x4*)(p.q + out_row(p, w, min(r, w.nrows - 1)) * C::QRB + 16 * c);
+    *(i32x4*)(qsm + r * C::QRB + ((((c & ~3) | ((c & 1) << 1) | ((c >> 1) & 1)) ^ k_swz<DT_BF16, D>(r)) << 4)) = x;
+  }
+  // addresses of the first chunks of K, V and the query rows: the swizzles are
+  // exclusive ors, so that the others follow from these
+  uint32_t kat = i32 * RB + ((g ^ k_swz<DT_FP8, D>(i32)) << 4), vat = C::HALF + v_address<DT_FP8, D>(0, 0, lane);
+  uint32_t qat = (wave * 64 + i32) * C::QRB + ((g ^ k_swz<DT_BF16, D>(i32)) << 4);
+  f32x16 oacc[2][NDB];
+  float m[2], l[2];
+  bf16x8 pb[2][2 * NB];     // the last step's weights, none before the first
+  i32x2v vr[NDB][2 * NB];   // and its values, with their scales
+  float vs[2 * NB];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    m[s] = -INFINITY;
+    l[s] = 0.0f;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) oacc[s][db] = f32x16{0.0f};
+#pragma unroll
+    for (int k = 0; k < 2 * NB; ++k) pb[s][k] = bf16x8{};
+  }
+#pragma unroll
+  for (int k = 0; k < 2 * NB; ++k) {
+    vs[k] = 1.0f;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) vr[db][k] = i32x2v{0, 0};
+  }
+  const int nsteps = (w.nk + STEP - 1) / STEP;
+
+  auto add_values = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int k = 0; k < 2 * NB; ++k) {
+        const bf16x8 x = widen(vr[db][k][0], vr[db][k][1], vs[k]);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          oacc[s][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pb[s][k], oacc[s][db], 0, 0, 0);
+      }
+  };
+  // One step: buf holds its K and V, `ahead` takes those of the step after next.
+  // (The buffers are arrays of their own: the compiler waits for a copy into an
+  // array that it reads.)
+  auto step = [&](int c, const uint8_t* buf, int (&pair)[NB], uint8_t* ahead, int (&pair_ahead)[NB])
+                  __attribute__((always_inline)) {
+    stage(c + 2, ahead, pair_ahead);
+    // (made anew in each step: kept, the addresses of three buffers spill)
+    asm volatile("" : "+v"(kat), "+v"(vat), "+v"(qat));
+    __builtin_amdgcn_sched_barrier(0);
+    // K's operands and the first query rows', which land during P V
+    i32x4 kk[NCH / 2][NB];
+#pragma unroll
+    for (int t = 0; t < NCH / 2; ++t)
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb)
+        kk[t][kb] = *(const i32x4*)(buf + (kat ^ (t << 5)) + 32 * RB * kb);
+    bf16x8 q[3][2];
+    auto read_q = [&](int u) __attribute__((always_inline)) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        q[u % 3][s] = *(const bf16x8*)(qsm + (qat ^ (u << 5)) + 32 * s * C::QRB);
+    };
+    read_q(0);
+    read_q(1);
+    __builtin_amdgcn_sched_barrier(0);
+    add_values();
+    __builtin_amdgcn_sched_barrier(0);
+    float ks[NB];
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) {
+      ks[kb] = scale_of(pair[kb] & 255);
+      vs[2 * kb] = v_scale(pair[kb], 0);
+      vs[2 * kb + 1] = v_scale(pair[kb], 16);
+    }
+    f32x16 sv[2][NB];
+#pragma unroll
+    for (int u = 0; u < NCH; ++u) {
+      if (u + 2 < NCH) read_q(u + 2);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb) {
+        const bf16x8 x = widen(kk[u / 2][kb][2 * (u & 1)], kk[u / 2][kb][2 * (u & 1) + 1], ks[kb]);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          sv[s][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[u % 3][s], u == 0 ? f32x16{0.0f} : sv[s][kb], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int k = 0; k < 2 * NB; ++k)
+        vr[db][k] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2v, buf + (vat ^ (db << 5)) + 16 * RB * k));
+    __builtin_amdgcn_sched_barrier(0);
+    // this wave's copies of the next step have landed (those after it may be
+    // outstanding); past the second barrier from here everyone's have
+    wait_vmcnt<NB + 1>();
+    lds_barrier();
+    const int kw0 = c * STEP;
+    const bool need_mask = kw0 + STEP > w.open || kw0 + STEP > w.nk;
+    settle_unit(sv[0]);
+    settle_unit(sv[1]);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if (need_mask) mask_unit(sv[s], row_limit(p, w, min(wave * 64 + 32 * s + i32, w.nrows - 1)) - 4 * g - kw0, -INFINITY);
+      // The anchor stays until a weight could pass 2^40 (FP32 and BF16 hold them far
+      // beyond, with the same relative steps): a row's maximum is looked for only
+      // then, as its first step does, whose anchor of -inf gives inf or NaN.
+      float e[16], sum = weights(sv[s][0], e, -m[s] * p.c1, p.c1);
+      if (__builtin_amdgcn_ballot_w64(!(sum <= 0x1p40f)) != 0) {
+        float ma, mb;
+        with_partner(unit_max(sv[s]), ma, mb);
+        const float top = max3(m[s], ma, mb);
+        const float alpha = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[s] - top) * p.c1);
+        m[s] = top;
+        l[s] *= alpha;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) oacc[s][db][j] *= alpha;
+        sum = weights(sv[s][0], e, top == -INFINITY ? 0.0f : -top * p.c1, p.c1);
+      }
+      l[s] += sum;
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) pb[s][k][j] = (__bf16)e[8 * k + j];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    lds_barrier();
+  };
+  int pair0[NB], pair1[NB], pair2[NB];
+  stage(0, b0, pair0);
+  stage(1, b1, pair1);
+  wait_vmcnt<NB + 1>();
+  lds_barrier();
+  if (of_v) lds_barrier();  // the second group is half a step behind
+#pragma unroll 1
+  for (int c = 0; c < nsteps; c += 3) {
+    step(c, b0, pair0, b2, pair2);
+    step(c + 1, b1, pair1, b0, pair0);  // (steps beyond the last key are masked whole)
+    step(c + 2, b2, pair2, b1, pair1);
+  }
+  if (!of_v) lds_barrier();
+  add_values();
+  wait_vmcnt<0>();
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    float la, lb;
+    with_partner(l[s], la, lb);
+    const float sum = la + lb, inv = inverse(sum, 1.0f);
+    const int r = wave * 64 + 32 * s + i32;
+    if (r >= w.nrows) continue;
+    const size_t orow = out_row(p, w, r), at = orow * (size_t)p.parts + w.part;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int jq = 0; jq < 4; ++jq) {
+        const f32x4 x = {oacc[s][db][4 * jq], oacc[s][db][4 * jq + 1], oacc[s][db][4 * jq + 2], oacc[s][db][4 * jq + 3]};
+        const int col = 32 * db + 8 * jq + 4 * g;
+        if (p.parts == 1) store_row4(p.o + orow * D + col, x, inv);
+        else *(f32x4*)(p.part_o + at * D + col) = x;
+      }
+    if (g == 0) {
+      if (p.parts > 1) *(f32x2*)(p.part_ml + at * 2) = f32x2{m[s], sum};
+      else if (p.lse) p.lse[orow] = row_lse(m[s], sum, p.c1);
+    }
+  }
+}
+
+// A workgroup's sequence, head, part and rows; false if there is nothing to read
+// (several parts: said so to the merge, which skips a part with l = 0).
+template <int D>
+__device__ __forceinline__ bool find_work(const BlocksParams& p, int* scratch, Work& w) {
   int unit, rb;
   place(blockIdx.x, p.B * p.Hkv * p.parts, p.row_blocks, unit, rb);
   int bh = unit / p.parts;
@@ -460,7 +678,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   w.b = bh / p.Hkv;
   w.h = bh - w.b * p.Hkv;
   if (p.longest) {
-    w.b = longest(p.lens, p.B, p.Sk, w.b, (int*)mx_lds);
+    w.b = longest(p.lens, p.B, p.Sk, w.b, scratch);
     bh = w.b * p.Hkv + w.h;
   }
   const int n = p.lens ? min(max(p.lens[w.b], 0), p.Sk) : p.Sk;
@@ -478,18 +696,46 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     w.open = w.last0 + (i1 < p.Sq ? i0 : 0) + 1;
   }
   if (w.nk == 0 && p.parts > 1) {
-    // nothing to read: the merge skips a part with l = 0
     if ((int)threadIdx.x < w.nrows)
       *(f32x2*)(p.part_ml + (out_row(p, w, threadIdx.x) * (size_t)p.parts + w.part) * 2) = f32x2{-INFINITY, 0.0f};
-    return;
+    return false;
   }
   const size_t at = ((size_t)bh * (size_t)p.Sk_cap + (size_t)(w.nk ? w.j0 : 0)) * D;
   w.k = p.k + at;
   w.v = p.v + at;
   w.scales = p.scales + (size_t)bh * (size_t)p.blocks * 2;
   w.used = 2 * ((n + (1 << p.shift) - 1) >> p.shift);
+  return true;
+}
+
+template <int D, int MODE, bool ROWS>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_blocks_kernel(
+    BlocksParams p) {
+  using C = BCfg<D>;
+  // (arrays of their own, so that the compiler tells the copies apart)
+  __shared__ __attribute__((aligned(16))) uint8_t ksm[C::AREA];
+  __shared__ __attribute__((aligned(16))) uint8_t vsm[C::AREA];
+  __shared__ __attribute__((aligned(16))) float mx_lds[2][32][NW];
+  __shared__ __attribute__((aligned(16))) float m_lds[32][NW], l_lds[32][NW];
+  Work w;
+  if (!find_work<D>(p, (int*)mx_lds, w)) return;
   if constexpr (ROWS) rows_form<D, MODE>(p, w, ksm, vsm);
   else keys_form<D, MODE>(p, w, ksm, vsm, mx_lds, m_lds, l_lds);
+}
+
+template <int D>
+__global__ __launch_bounds__(BLOCKS_WIDE) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_blocks_wide_kernel(
+    BlocksParams p) {
+  using C = WCfg<D>;
+  // (aligned further, the buffers lie first, where an instruction's offset tells
+  // them apart)
+  __shared__ __attribute__((aligned(1024))) uint8_t b0[2 * C::HALF];
+  __shared__ __attribute__((aligned(1024))) uint8_t b1[2 * C::HALF];
+  __shared__ __attribute__((aligned(1024))) uint8_t b2[2 * C::HALF];
+  __shared__ __attribute__((aligned(16))) uint8_t qsm[C::QAREA];
+  Work w;
+  if (!find_work<D>(p, (int*)qsm, w)) return;
+  wide_form<D>(p, w, qsm, b0, b1, b2);
 }
 
 template <int D>
@@ -500,7 +746,8 @@ __global__ __launch_bounds__(256) void attn_blocks_merge(BlocksParams p) {
 template <int D, int MODE>
 hipError_t launch_one(const BlocksParams& p, hipStream_t st) {
   const dim3 grid((unsigned)p.groups), block(NW * 64);
-  if (p.rows == WROWS) hipLaunchKernelGGL((attn_blocks_kernel<D, MODE, false>), grid, block, 0, st, p);
+  if (p.rows == BLOCKS_WIDE && MODE == MODE_EXACT) hipLaunchKernelGGL((attn_blocks_wide_kernel<D>), grid, dim3(BLOCKS_WIDE), 0, st, p);
+  else if (p.rows == WROWS) hipLaunchKernelGGL((attn_blocks_kernel<D, MODE, false>), grid, block, 0, st, p);
   else hipLaunchKernelGGL((attn_blocks_kernel<D, MODE, true>), grid, block, 0, st, p);
   return hipGetLastError();
 }

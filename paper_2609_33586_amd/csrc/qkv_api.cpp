@@ -161,7 +161,13 @@ int log2_block(int block) {
 int part_count(int keys, int split) { return split <= 0 || split >= keys ? 1 : (int)ceil_div(keys, split); }
 
 // Query rows of a workgroup, for R rows of a sequence and KV head.
-int blocks_rows(long long R) { return R > 4 * WROWS ? BLOCKS_ROWS : WROWS; }
+int blocks_rows(long long R, bool exact) {
+  if (exact && R >= BLOCKS_WIDE) return BLOCKS_WIDE;
+  return R > 4 * WROWS ? BLOCKS_ROWS : WROWS;
+}
+
+// Workgroups that run at once.
+int blocks_slots(int rows) { return rows == BLOCKS_WIDE ? 256 : 512; }
 
 size_t blocks_workspace(long long rows, int parts, int d) {
   return parts <= 1 ? 0 : (size_t)rows * (size_t)parts * ((size_t)d + 2) * sizeof(float);
@@ -340,10 +346,10 @@ size_t attn_decode_blocks_workspace_bytes(int B, int Hq, int Sq, int Sk, int d, 
 int attn_decode_blocks_split_keys(int B, int Hq, int Hkv, int Sq, int Sk, int d) {
   (void)d;  // (a cut of one head dimension is one of both)
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || Hq % Hkv != 0) return 0;
-  const long long R = (long long)(Hq / Hkv) * Sq, groups = (long long)B * Hkv * ceil_div(R, blocks_rows(R));
-  // two workgroups a compute unit, parts of eight tiles or more
+  const long long R = (long long)(Hq / Hkv) * Sq, groups = (long long)B * Hkv * ceil_div(R, blocks_rows(R, true));
+  // two workgroups a compute unit (of the wide form one), parts of eight tiles or more
   const long long tiles = ceil_div(Sk, BC);
-  long long parts = ceil_div(512, groups);
+  long long parts = ceil_div(blocks_slots(blocks_rows(R, true)), groups);
   if (parts > tiles / 8) parts = tiles / 8;
   return parts <= 1 ? 0 : (int)(ceil_div(tiles, parts) * BC);
 }
@@ -389,14 +395,14 @@ int attn_decode_blocks(const void* q, const void* k, const void* v, const uint8_
   p.parts = part_count(Sk, split_keys);
   // (one part of whole tiles: the cut at its end)
   p.split = p.parts == 1 ? (int)(ceil_div(Sk, BC) * BC) : split_keys;
-  p.rows = blocks_rows(p.R);
+  p.rows = blocks_rows(p.R, order == 0);
   p.row_blocks = (int)ceil_div(p.R, p.rows);
   const long long groups = (long long)B * Hkv * p.parts * p.row_blocks;
   if (groups > MAX_GROUPS || (p.parts > 1 && rows > MAX_MERGE_ROWS)) return ATTN_EUNSUPPORTED;
   p.groups = (int)groups;
   // ragged caches that are more than one for each slot are taken longest first, so
   // that no long one starts last
-  p.longest = lens && B > 1 && B <= 256 && groups > 512;
+  p.longest = lens && B > 1 && B <= 256 && groups > blocks_slots(p.rows);
   const size_t need = blocks_workspace(rows, p.parts, d);
   if (need) {
     if (!workspace || misaligned(workspace, 16) || workspace_bytes < need) return ATTN_EINVAL;

@@ -59,6 +59,8 @@ struct AppendParams {
 
 // Query rows of a workgroup whose waves share each tile of keys.
 constexpr int BLOCKS_ROWS = 4 * WROWS;
+// Query rows of the wide form's, whose waves have two blocks of WROWS each.
+constexpr int BLOCKS_WIDE = 16 * WROWS;
 
 // Attention over a cache of 8-bit blocks.
 struct BlocksParams {
@@ -75,7 +77,7 @@ struct BlocksParams {
   int Sk, Sk_cap, causal;
   int blocks, shift;  // blocks of a head's cache, log2 of their keys
   int parts, split;   // parts and their keys
-  int rows;           // query rows of a workgroup: WROWS or BLOCKS_ROWS
+  int rows;           // query rows of a workgroup: WROWS, BLOCKS_ROWS or BLOCKS_WIDE
   int row_blocks;     // of a sequence and KV head
   int longest;        // caches are taken in the order of their lengths (B <= 256)
   int groups;

@@ -58,6 +58,27 @@ def test_many_rows(d, mode, causal):
         run_and_check(2, Hq, Hkv, Sq, 400, d, [16, 32, 64, 128][i % 4], lens, f"case {i}", mode, cut, causal, 10 + i)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("block", [16, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_hundreds_of_rows(d, block, causal):
+    # a block of rows over several heads' positions, rows without a key, lengths around a step's and a tile's ends
+    for i, (B, Hq, Hkv, Sq, cap, lens, cut) in enumerate([(1, 4, 2, 150, 333, [333], 0), (2, 3, 1, 301, 700, [700, 97], 256), (1, 4, 1, 512, 600, [560], 0),
+                                                          (5, 1, 1, 300, 300, [300, 31, 32, 33, 0], 0), (3, 8, 1, 65, 200, [128, 65, 129], 128),
+                                                          (7, 2, 1, 700, 400, [400, 0, 1, 97, 129, 385, 33], 0)]):
+        run_and_check(B, Hq, Hkv, Sq, cap, d, block, lens, f"case {i}", EXACT, cut, causal, 20 + i)
+
+
+def test_anchors_of_many_rows():
+    # logits that grow along the keys, so that the running maximum moves far and often; and a tiny scale
+    q, (k, v, scales) = normal((1, 2, 600, 64), 30), block_cache(1, 1, 900, 64, 16, 31)
+    scales.view(torch.uint8)[0, 0, :, 0] = (110 + torch.arange(57, device="cuda") // 3).to(torch.uint8)
+    for cut in (0, 256):
+        for scale in (scale_of(64), 8.0, 1e-38):
+            o, lse = pkg.attn_decode_blocks(q, k, v, scales, block=16, causal=True, scale=scale, exp_mode=EXACT, split_keys=cut)
+            check_prefix(o, lse, blocks_ref(q, k, v, scales, 16, [900], True, scale, EXACT, cut), f"cut {cut} scale {scale}")
+
+
 def test_no_lens_and_Sk():
     run_and_check(2, 4, 4, 1, 200, 64, 64, None, "no lens")
     run_and_check(2, 4, 4, 3, 200, 64, 64, None, "Sk", Sk=130)
