@@ -8,12 +8,14 @@
 // inner loops.  K's rows meet them one scale a lane, V's transposed operands one
 // for each 16 keys, which never straddle a block.
 //
-// Two forms of a workgroup (4 waves), those of attn_decode_prefix:
+// Three forms of a workgroup (their rules: qkv_api.cpp), the first two, of 4 waves,
+// those of attn_decode_prefix:
 //   keys  32 query rows; each wave takes its own 64 keys of a round, copies them
 //         into its own LDS slots and exchanges only the maxima of its units with
 //         the others (one barrier a round); a weight is rounded relative to the
 //         running maximum at its own tile, the prefix maximum of the round's units;
-//   rows  128 query rows, 32 a wave; the waves share each tile of 128 keys.
+//   rows  128 query rows, 32 a wave; the waves share each tile of 128 keys;
+//   wide  512 query rows, 64 a wave: many rows of long caches.
 #include "qkv_params.h"
 #include "part_device.h"
 
@@ -446,53 +448,68 @@ __device__ __forceinline__ void rows_form(const BlocksParams& p, const Work& w, 
 // ---- the wide form: 512 query rows, 64 a wave, the hardware exponential.
 // Eight waves, two on a SIMD: while the four of one group are at the matrix core
 // (P V of the last step, Q K^T of this one), those of the other make weights, and
-// a barrier after each such half step keeps it so.
+// a barrier after each such half step keeps it so.  A step has 64 keys, so that the
+// query rows, which no registers are left for, are read from LDS once for all of them.
+//
+// What bounds it (8192 rows of 8 KV heads after 32K keys, d = 128: 883 us + 26 of the
+// merge, 1.17 PFLOP/s; the rows form 1080): the clock that the board's power allows
+// (1.94 GHz, with the matrix core busy 56% of the cycles and the VALU 58%): each of
+// the steps to here took more off the cycles than off the time.  Widening a step's
+// codes once for all waves into BF16 rows saved a third of the VALU's work and lost
+// as much to LDS (steps of 32 keys, whose rows LDS has room for: 1033 us; the same
+// with codes in LDS 1004).  One group without the half step between them: 1030.
 template <int D>
 struct WCfg {
   static constexpr int NW = BLOCKS_WIDE / 64;
-  static constexpr int RB = D, NCH = D / 16;
-  static constexpr int STEP = 32, NB = 1, HALF = STEP * RB;  // keys of a step, blocks of 32, bytes of its K
-  static constexpr int QRB = 2 * D;  // bytes of a query row
+  static constexpr int RB = D, NCH = D / 16;      // bytes and chunks of a row of codes
+  static constexpr int STEP = 64, HALF = STEP * RB;  // keys of a step, bytes of its K (or V)
+  static constexpr int LOADS = HALF / 4096;       // copies of 1 KB of a wave
+  static constexpr int QRB = 2 * D;               // bytes of a query row
   static constexpr int QAREA = BLOCKS_WIDE * QRB;
 };
 
-// 2^(c1 s + nb) of 16 scores, and their sum
-__device__ __forceinline__ float weights(const f32x16& s, float (&e)[16], float nb, float c1) {
+// 2^(c1 s + nb) of 32 scores, and their sum
+__device__ __forceinline__ float weights(const f32x16 (&s)[2], float (&e)[32], float nb, float c1) {
   float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j], c1, nb));
+  for (int j = 0; j < 32; ++j) {
+    e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j >> 4][j & 15], c1, nb));
     a[j & 3] = j < 4 ? e[j] : a[j & 3] + e[j];
   }
   return (a[0] + a[1]) + (a[2] + a[3]);
 }
 
 template <int D>
-__device__ __forceinline__ void wide_form(const BlocksParams& p, const Work& w, uint8_t* qsm, uint8_t* b0, uint8_t* b1,
-                                          uint8_t* b2) {
+__device__ __forceinline__ void wide_form(const BlocksParams& p, const Work& w, uint8_t* qsm, uint8_t* k0, uint8_t* k1,
+                                          uint8_t* v0, uint8_t* v1) {
   using C = WCfg<D>;
-  constexpr int RB = C::RB, NCH = C::NCH, NDB = D / 32, NB = C::NB, STEP = C::STEP, QCH = C::QRB / 16;
+  constexpr int RB = C::RB, NCH = C::NCH, NDB = D / 32, STEP = C::STEP, QCH = C::QRB / 16;
   const int tid = threadIdx.x, lane = tid & 63, i32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t part_bytes = (uint32_t)w.nk * RB;
-  // a wave copies 1 KB of each step: of K those of the first group, of V the others
-  // (two of each at d = 64)
-  const bool of_v = wave >= C::NW / 2;
-  const auto rsrc = rows_rsrc(of_v ? w.v : w.k, part_bytes);
-  const auto srsrc = rows_rsrc(w.scales, w.used);
+  // the first group copies K, the second V, a quarter of a step a wave
+  const bool second = wave >= C::NW / 2;
   const int mine = wave & (C::NW / 2 - 1);
+  const auto rsrc = rows_rsrc(second ? w.v : w.k, part_bytes);
+  const auto srsrc = rows_rsrc(w.scales, w.used);
   uint32_t off;
   {
-    const int r = copy_row<NCH>(mine, lane), first = mine * (64 / NCH);
-    off = (r - first) * RB + (((lane % NCH) ^ (of_v ? v_swz<DT_FP8, D>(r) : k_swz<DT_FP8, D>(r))) << 4);
+    const int kb = mine * C::LOADS, r = copy_row<NCH>(kb, lane), first = kb * (64 / NCH);
+    off = (r - first) * RB + (((lane % NCH) ^ (second ? v_swz<DT_FP8, D>(r) : k_swz<DT_FP8, D>(r))) << 4);
   }
-  auto stage = [&](int c, uint8_t* buf, int (&pair)[NB]) __attribute__((always_inline)) {
-    const uint32_t soff = min((uint32_t)c * C::HALF + mine * 1024, part_bytes);
+  auto stage = [&](int c, uint8_t* buf) __attribute__((always_inline)) {
 #pragma unroll
-    for (int kb = 0; kb < NB; ++kb) pair[kb] = scale_pair(p, srsrc, w.j0 + c * STEP + 32 * kb + i32);
-    if (C::HALF == C::NW * 512 || mine < C::HALF / 1024)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, LDS_PTR(void, buf + (of_v ? C::HALF : 0) + mine * 1024), 16, off, soff,
-                                               0, 0);
+    for (int i = 0; i < C::LOADS; ++i) {
+      const int at = (mine * C::LOADS + i) * 1024;
+      const uint32_t soff = min((uint32_t)c * C::HALF + at, part_bytes);
+      // (d = 128: eight rows on, both swizzles differ in their third bit)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, LDS_PTR(void, buf + at), 16, off ^ (64 * i), soff, 0, 0);
+    }
+  };
+  int pair[2];
+  auto load_scales = [&](int c) __attribute__((always_inline)) {
+    pair[0] = scale_pair(p, srsrc, w.j0 + c * STEP + i32);
+    pair[1] = scale_pair(p, srsrc, w.j0 + c * STEP + 32 + i32);
   };
   // the query rows, chunk 4 t + 2 g + j of a row at 4 t + 2 j + g: operand 2 t + j of half g
 #pragma unroll 4
@@ -503,13 +520,12 @@ __device__ __forceinline__ void wide_form(const BlocksParams& p, const Work& w, 
   }
   // addresses of the first chunks of K, V and the query rows: the swizzles are
   // exclusive ors, so that the others follow from these
-  uint32_t kat = i32 * RB + ((g ^ k_swz<DT_FP8, D>(i32)) << 4), vat = C::HALF + v_address<DT_FP8, D>(0, 0, lane);
+  uint32_t kat = i32 * RB + ((g ^ k_swz<DT_FP8, D>(i32)) << 4), vat = v_address<DT_FP8, D>(0, 0, lane);
   uint32_t qat = (wave * 64 + i32) * C::QRB + ((g ^ k_swz<DT_BF16, D>(i32)) << 4);
   f32x16 oacc[2][NDB];
   float m[2], l[2];
-  bf16x8 pb[2][2 * NB];     // the last step's weights, none before the first
-  i32x2v vr[NDB][2 * NB];   // and its values, with their scales
-  float vs[2 * NB];
+  bf16x8 pb[2][4];  // the last step's weights (none before the first), and its values' scales
+  float vs[4] = {1.0f, 1.0f, 1.0f, 1.0f};
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     m[s] = -INFINITY;
@@ -517,97 +533,98 @@ __device__ __forceinline__ void wide_form(const BlocksParams& p, const Work& w, 
 #pragma unroll
     for (int db = 0; db < NDB; ++db) oacc[s][db] = f32x16{0.0f};
 #pragma unroll
-    for (int k = 0; k < 2 * NB; ++k) pb[s][k] = bf16x8{};
-  }
-#pragma unroll
-  for (int k = 0; k < 2 * NB; ++k) {
-    vs[k] = 1.0f;
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) vr[db][k] = i32x2v{0, 0};
+    for (int k = 0; k < 4; ++k) pb[s][k] = bf16x8{};
   }
   const int nsteps = (w.nk + STEP - 1) / STEP;
 
-  auto add_values = [&]() __attribute__((always_inline)) {
+  // P V of the last step, its V in vbuf
+  auto add_values = [&](const uint8_t* vbuf) __attribute__((always_inline)) {
+    i32x2v r[2][4];
+    auto read_v = [&](int db) __attribute__((always_inline)) {
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
+      for (int k = 0; k < 4; ++k)
+        r[db & 1][k] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2v, vbuf + (vat ^ (db << 5)) + 16 * RB * k));
+    };
+    read_v(0);
 #pragma unroll
-      for (int k = 0; k < 2 * NB; ++k) {
-        const bf16x8 x = widen(vr[db][k][0], vr[db][k][1], vs[k]);
+    for (int db = 0; db < NDB; ++db) {
+      if (db + 1 < NDB) read_v(db + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const bf16x8 x = widen(r[db & 1][k][0], r[db & 1][k][1], vs[k]);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
           oacc[s][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pb[s][k], oacc[s][db], 0, 0, 0);
       }
+    }
   };
-  // One step: buf holds its K and V, `ahead` takes those of the step after next.
-  // (The buffers are arrays of their own: the compiler waits for a copy into an
-  // array that it reads.)
-  auto step = [&](int c, const uint8_t* buf, int (&pair)[NB], uint8_t* ahead, int (&pair_ahead)[NB])
-                  __attribute__((always_inline)) {
-    stage(c + 2, ahead, pair_ahead);
-    // (made anew in each step: kept, the addresses of three buffers spill)
+  // One step: its K is in kbuf, the last one's V in vbuf, which takes the next one's
+  // once it is done with; the next one's K goes to knext.  (The buffers are arrays
+  // of their own: the compiler waits for a copy into an array that it reads.)
+  auto step = [&](int c, const uint8_t* kbuf, uint8_t* knext, uint8_t* vbuf) __attribute__((always_inline)) {
+    // (made anew in each step: kept, the addresses of all buffers spill)
     asm volatile("" : "+v"(kat), "+v"(vat), "+v"(qat));
+    float ks[2], vnext[4];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      ks[kb] = scale_of(pair[kb] & 255);
+      vnext[2 * kb] = v_scale(pair[kb], 0);
+      vnext[2 * kb + 1] = v_scale(pair[kb], 16);
+    }
+    load_scales(c + 1);
+    if (!second) stage(c + 1, knext);
     __builtin_amdgcn_sched_barrier(0);
-    // K's operands and the first query rows', which land during P V
-    i32x4 kk[NCH / 2][NB];
+    i32x4 kk[2][2];
+    bf16x8 q[2][2];
+    auto read_k = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < NCH / 2; ++t)
-#pragma unroll
-      for (int kb = 0; kb < NB; ++kb)
-        kk[t][kb] = *(const i32x4*)(buf + (kat ^ (t << 5)) + 32 * RB * kb);
-    bf16x8 q[3][2];
+      for (int kb = 0; kb < 2; ++kb) kk[t & 1][kb] = *(const i32x4*)(kbuf + (kat ^ (t << 5)) + 32 * RB * kb);
+    };
     auto read_q = [&](int u) __attribute__((always_inline)) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-        q[u % 3][s] = *(const bf16x8*)(qsm + (qat ^ (u << 5)) + 32 * s * C::QRB);
+      for (int s = 0; s < 2; ++s) q[u & 1][s] = *(const bf16x8*)(qsm + (qat ^ (u << 5)) + 32 * s * C::QRB);
     };
+    add_values(vbuf);
+    read_k(0);
     read_q(0);
-    read_q(1);
     __builtin_amdgcn_sched_barrier(0);
-    add_values();
-    __builtin_amdgcn_sched_barrier(0);
-    float ks[NB];
-#pragma unroll
-    for (int kb = 0; kb < NB; ++kb) {
-      ks[kb] = scale_of(pair[kb] & 255);
-      vs[2 * kb] = v_scale(pair[kb], 0);
-      vs[2 * kb + 1] = v_scale(pair[kb], 16);
-    }
-    f32x16 sv[2][NB];
+    f32x16 sv[2][2];
 #pragma unroll
     for (int u = 0; u < NCH; ++u) {
-      if (u + 2 < NCH) read_q(u + 2);
+      if (u % 2 == 0 && u + 2 < NCH) read_k(u / 2 + 1);
+      if (u + 1 < NCH) read_q(u + 1);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int kb = 0; kb < NB; ++kb) {
-        const bf16x8 x = widen(kk[u / 2][kb][2 * (u & 1)], kk[u / 2][kb][2 * (u & 1) + 1], ks[kb]);
+      for (int kb = 0; kb < 2; ++kb) {
+        const i32x4& x4 = kk[(u / 2) & 1][kb];
+        const bf16x8 x = widen(x4[2 * (u & 1)], x4[2 * (u & 1) + 1], ks[kb]);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
-          sv[s][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[u % 3][s], u == 0 ? f32x16{0.0f} : sv[s][kb], 0, 0, 0);
+          sv[s][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[u & 1][s], u == 0 ? f32x16{0.0f} : sv[s][kb], 0, 0, 0);
       }
     }
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
-#pragma unroll
-      for (int k = 0; k < 2 * NB; ++k)
-        vr[db][k] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(LDS_PTR(i32x2v, buf + (vat ^ (db << 5)) + 16 * RB * k));
+    for (int k = 0; k < 4; ++k) vs[k] = vnext[k];
     __builtin_amdgcn_sched_barrier(0);
-    // this wave's copies of the next step have landed (those after it may be
-    // outstanding); past the second barrier from here everyone's have
-    wait_vmcnt<NB + 1>();
+    if (second) wait_vmcnt<2>();  // V of this step has landed; the next one's scales may be outstanding
     lds_barrier();
+    if (second) stage(c + 1, vbuf);
     const int kw0 = c * STEP;
     const bool need_mask = kw0 + STEP > w.open || kw0 + STEP > w.nk;
-    settle_unit(sv[0]);
-    settle_unit(sv[1]);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      if (need_mask) mask_unit(sv[s], row_limit(p, w, min(wave * 64 + 32 * s + i32, w.nrows - 1)) - 4 * g - kw0, -INFINITY);
+      if (need_mask) {
+        settle_unit(sv[s]);
+        mask_unit(sv[s], row_limit(p, w, min(wave * 64 + 32 * s + i32, w.nrows - 1)) - 4 * g - kw0, -INFINITY);
+      }
       // The anchor stays until a weight could pass 2^40 (FP32 and BF16 hold them far
       // beyond, with the same relative steps): a row's maximum is looked for only
       // then, as its first step does, whose anchor of -inf gives inf or NaN.
-      float e[16], sum = weights(sv[s][0], e, -m[s] * p.c1, p.c1);
+      float e[32], sum = weights(sv[s], e, -m[s] * p.c1, p.c1);
       if (__builtin_amdgcn_ballot_w64(!(sum <= 0x1p40f)) != 0) {
         float ma, mb;
+        settle_unit(sv[s]);
         with_partner(unit_max(sv[s]), ma, mb);
         const float top = max3(m[s], ma, mb);
         const float alpha = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[s] - top) * p.c1);
@@ -617,32 +634,34 @@ __device__ __forceinline__ void wide_form(const BlocksParams& p, const Work& w, 
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
           for (int j = 0; j < 16; ++j) oacc[s][db][j] *= alpha;
-        sum = weights(sv[s][0], e, top == -INFINITY ? 0.0f : -top * p.c1, p.c1);
+        sum = weights(sv[s], e, top == -INFINITY ? 0.0f : -top * p.c1, p.c1);
       }
       l[s] += sum;
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < 4; ++k)
 #pragma unroll
         for (int j = 0; j < 8; ++j) pb[s][k][j] = (__bf16)e[8 * k + j];
     }
+    if (!second) wait_vmcnt<0>();  // the next step's K has landed
     __builtin_amdgcn_sched_barrier(0);
     lds_barrier();
   };
-  int pair0[NB], pair1[NB], pair2[NB];
-  stage(0, b0, pair0);
-  stage(1, b1, pair1);
-  wait_vmcnt<NB + 1>();
+  load_scales(0);
+  if (second) stage(0, v0);
+  else stage(0, k0);
+  // (the values before the first step have the weight 0, but must not be NaN)
+  for (int i = tid; i < C::HALF / 16; i += C::NW * 64) *(i32x4*)(v1 + 16 * i) = i32x4{0, 0, 0, 0};
+  if (!second) wait_vmcnt<0>();
   lds_barrier();
-  if (of_v) lds_barrier();  // the second group is half a step behind
+  if (second) lds_barrier();  // the second group is half a step behind
 #pragma unroll 1
-  for (int c = 0; c < nsteps; c += 3) {
-    step(c, b0, pair0, b2, pair2);
-    step(c + 1, b1, pair1, b0, pair0);  // (steps beyond the last key are masked whole)
-    step(c + 2, b2, pair2, b1, pair1);
+  for (int c = 0; c < nsteps; c += 2) {
+    step(c, k0, k1, v1);
+    step(c + 1, k1, k0, v0);  // (a step beyond the last key is masked whole)
   }
-  if (!of_v) lds_barrier();
-  add_values();
+  if (!second) lds_barrier();
   wait_vmcnt<0>();
+  add_values(v1);
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     float la, lb;
@@ -729,13 +748,14 @@ __global__ __launch_bounds__(BLOCKS_WIDE) __attribute__((amdgpu_waves_per_eu(2, 
   using C = WCfg<D>;
   // (aligned further, the buffers lie first, where an instruction's offset tells
   // them apart)
-  __shared__ __attribute__((aligned(1024))) uint8_t b0[2 * C::HALF];
-  __shared__ __attribute__((aligned(1024))) uint8_t b1[2 * C::HALF];
-  __shared__ __attribute__((aligned(1024))) uint8_t b2[2 * C::HALF];
+  __shared__ __attribute__((aligned(1024))) uint8_t k0[C::HALF];
+  __shared__ __attribute__((aligned(1024))) uint8_t k1[C::HALF];
+  __shared__ __attribute__((aligned(1024))) uint8_t v0[C::HALF];
+  __shared__ __attribute__((aligned(1024))) uint8_t v1[C::HALF];
   __shared__ __attribute__((aligned(16))) uint8_t qsm[C::QAREA];
   Work w;
   if (!find_work<D>(p, (int*)qsm, w)) return;
-  wide_form<D>(p, w, qsm, b0, b1, b2);
+  wide_form<D>(p, w, qsm, k0, k1, v0, v1);
 }
 
 template <int D>

@@ -160,9 +160,15 @@ int log2_block(int block) {
 // Parts of `keys` keys cut at `split` (0 or >= keys: one part).
 int part_count(int keys, int split) { return split <= 0 || split >= keys ? 1 : (int)ceil_div(keys, split); }
 
-// Query rows of a workgroup, for R rows of a sequence and KV head.
-int blocks_rows(long long R, bool exact) {
-  if (exact && R >= BLOCKS_WIDE) return BLOCKS_WIDE;
+// Query rows of a workgroup, for R rows of a sequence and KV head.  The wide form
+// (exact weights) has one workgroup on a compute unit and takes its rows' keys a
+// third faster once it runs; it pays where each of 256 has 2048 keys to take, of long
+// caches, whose last parts and causal ends weigh little.  Times of a call in 128 /
+// 512 rows, each with its best cut, 8 KV heads, d = 128, R rows: 8192 after 32K keys
+// 1080 / 909 us, 2048 after 16K 161 / 144 (d = 64: 105 / 97); 8192 of 4K 143 / 144, 4 sequences
+// of 512 after 8K 86 / 85; 2048 after 4K 56 / 66, 4 sequences of 2048 of 2K 76 / 94.
+int blocks_rows(long long heads, long long R, int Sk, bool exact) {
+  if (exact && Sk >= 8192 && heads * ceil_div(R, BLOCKS_WIDE) * Sk >= 256LL * 2048 && R >= BLOCKS_WIDE) return BLOCKS_WIDE;
   return R > 4 * WROWS ? BLOCKS_ROWS : WROWS;
 }
 
@@ -346,10 +352,12 @@ size_t attn_decode_blocks_workspace_bytes(int B, int Hq, int Sq, int Sk, int d, 
 int attn_decode_blocks_split_keys(int B, int Hq, int Hkv, int Sq, int Sk, int d) {
   (void)d;  // (a cut of one head dimension is one of both)
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || Hq % Hkv != 0) return 0;
-  const long long R = (long long)(Hq / Hkv) * Sq, groups = (long long)B * Hkv * ceil_div(R, blocks_rows(R, true));
+  const long long R = (long long)(Hq / Hkv) * Sq, heads = (long long)B * Hkv;
+  const int rows = blocks_rows(heads, R, Sk, true);
+  const long long groups = heads * ceil_div(R, rows);
   // two workgroups a compute unit (of the wide form one), parts of eight tiles or more
   const long long tiles = ceil_div(Sk, BC);
-  long long parts = ceil_div(blocks_slots(blocks_rows(R, true)), groups);
+  long long parts = ceil_div(blocks_slots(rows), groups);
   if (parts > tiles / 8) parts = tiles / 8;
   return parts <= 1 ? 0 : (int)(ceil_div(tiles, parts) * BC);
 }
@@ -395,7 +403,7 @@ int attn_decode_blocks(const void* q, const void* k, const void* v, const uint8_
   p.parts = part_count(Sk, split_keys);
   // (one part of whole tiles: the cut at its end)
   p.split = p.parts == 1 ? (int)(ceil_div(Sk, BC) * BC) : split_keys;
-  p.rows = blocks_rows(p.R, order == 0);
+  p.rows = blocks_rows((long long)B * Hkv, p.R, Sk, order == 0);
   p.row_blocks = (int)ceil_div(p.R, p.rows);
   const long long groups = (long long)B * Hkv * p.parts * p.row_blocks;
   if (groups > MAX_GROUPS || (p.parts > 1 && rows > MAX_MERGE_ROWS)) return ATTN_EUNSUPPORTED;

@@ -63,20 +63,36 @@ def test_many_rows(d, mode, causal):
 @pytest.mark.parametrize("causal", [True, False])
 def test_hundreds_of_rows(d, block, causal):
     # a block of rows over several heads' positions, rows without a key, lengths around a step's and a tile's ends
-    for i, (B, Hq, Hkv, Sq, cap, lens, cut) in enumerate([(1, 4, 2, 150, 333, [333], 0), (2, 3, 1, 301, 700, [700, 97], 256), (1, 4, 1, 512, 600, [560], 0),
-                                                          (5, 1, 1, 300, 300, [300, 31, 32, 33, 0], 0), (3, 8, 1, 65, 200, [128, 65, 129], 128),
-                                                          (7, 2, 1, 700, 400, [400, 0, 1, 97, 129, 385, 33], 0)]):
+    for i, (B, Hq, Hkv, Sq, cap, lens, cut) in enumerate([(1, 4, 2, 150, 333, [333], 0), (2, 3, 1, 301, 700, [700, 97], 256),
+                                                          (3, 8, 1, 65, 200, [128, 65, 129], 128)]):
         run_and_check(B, Hq, Hkv, Sq, cap, d, block, lens, f"case {i}", EXACT, cut, causal, 20 + i)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_thousands_of_keys_and_rows(d, causal):
+    # the form of 512 rows (64 caches of 8K keys' room, mostly empty): lengths around a step's and a tile's ends, one
+    # in parts; blocks of rows over several heads' positions and a last one in part
+    lens = [0] * 64
+    for b, n in ((0, 1), (1, 63), (5, 64), (6, 65), (17, 127), (18, 128), (40, 129), (41, 1500), (63, 777)):
+        lens[b] = n
+    run_and_check(64, 2, 1, 300, 8192, d, 16, lens, "two heads of 300 positions", EXACT, 0, causal, 40, sharp=False)
+    lens = [700] + [0] * 31
+    run_and_check(32, 1, 1, 520, 16384, d, 128, lens, "520 positions, parts", EXACT, 256, causal, 41, sharp=False)
 
 
 def test_anchors_of_many_rows():
     # logits that grow along the keys, so that the running maximum moves far and often; and a tiny scale
-    q, (k, v, scales) = normal((1, 2, 600, 64), 30), block_cache(1, 1, 900, 64, 16, 31)
-    scales.view(torch.uint8)[0, 0, :, 0] = (110 + torch.arange(57, device="cuda") // 3).to(torch.uint8)
-    for cut in (0, 256):
-        for scale in (scale_of(64), 8.0, 1e-38):
-            o, lse = pkg.attn_decode_blocks(q, k, v, scales, block=16, causal=True, scale=scale, exp_mode=EXACT, split_keys=cut)
-            check_prefix(o, lse, blocks_ref(q, k, v, scales, 16, [900], True, scale, EXACT, cut), f"cut {cut} scale {scale}")
+    q, (k, v, scales) = normal((1, 2, 600, 64), 30), block_cache(1, 1, 175104, 64, 16, 31)
+    n = 900
+    scales.view(torch.uint8)[0, 0, :57, 0] = (110 + torch.arange(57, device="cuda") // 3).to(torch.uint8)
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    for Sk in (n, 175104):  # 128 rows a workgroup, and 512
+        for cut in (0, 256 if Sk == n else 1280):
+            for scale in (scale_of(64), 8.0, 1e-38):
+                o, lse = pkg.attn_decode_blocks(q, k, v, scales, block=16, causal=True, scale=scale, exp_mode=EXACT, split_keys=cut,
+                                                lens=lens, Sk=Sk)
+                check_prefix(o, lse, blocks_ref(q, k, v, scales, 16, [n], True, scale, EXACT, cut), f"Sk {Sk} cut {cut} scale {scale}")
 
 
 def test_no_lens_and_Sk():

@@ -88,8 +88,8 @@ def test_append_reach(host):
     assert form(1, 64, 64, True) == (1, 1, 1)
 
 
-def blocks_form(L, B, Hq, Hkv, Sq, Sk, cut=0, lens=at(4), causal=1, d=128, block=64):
-    rc = L.attn_decode_blocks(at(0), at(1), at(2), at(3), lens, at(5), None, B, Hq, Hkv, Sq, Sk, Sk, d, block, causal, 0.1, 0, cut,
+def blocks_form(L, B, Hq, Hkv, Sq, Sk, cut=0, lens=at(4), causal=1, d=128, block=64, mode=0):
+    rc = L.attn_decode_blocks(at(0), at(1), at(2), at(3), lens, at(5), None, B, Hq, Hkv, Sq, Sk, Sk, d, block, causal, 0.1, mode, cut,
                               at(7), 1 << 40, None)
     assert rc == pkg.ATTN_ELAUNCH
     names = ("parts", "split", "rows", "row_blocks", "groups", "causal", "longest", "blocks", "shift")
@@ -105,6 +105,13 @@ def test_blocks_forms(host):
     assert blocks_form(host, 1, 8, 2, 32, 500)["rows"] == 32 and blocks_form(host, 1, 8, 2, 32, 500)["row_blocks"] == 4
     assert blocks_form(host, 1, 8, 2, 33, 500)["rows"] == 128 and blocks_form(host, 1, 8, 2, 33, 500)["row_blocks"] == 2
     assert blocks_form(host, 1, 8, 2, 33, 500, causal=0)["causal"] == 0
+    # of 512 where each of 256 of them has 2048 keys of long caches, with the exact weights
+    f = blocks_form(host, 1, 32, 8, 512, 16384)
+    assert f["rows"] == 512 and f["row_blocks"] == 4 and f["groups"] == 32
+    assert blocks_form(host, 1, 32, 8, 512, 16384, mode=1)["rows"] == 128
+    assert blocks_form(host, 1, 32, 8, 512, 16383)["rows"] == 128 and blocks_form(host, 1, 32, 8, 2048, 8191)["rows"] == 128
+    assert blocks_form(host, 256, 1, 1, 511, 8192)["rows"] == 128 and blocks_form(host, 256, 1, 1, 512, 8192)["rows"] == 512
+    assert blocks_form(host, 1, 32, 8, 512, 16384, 2048)["groups"] == 256
     assert blocks_form(host, 64, 32, 8, 1, 500)["longest"] == 0 and blocks_form(host, 65, 32, 8, 1, 500)["longest"] == 1
     assert blocks_form(host, 65, 32, 8, 1, 500, lens=None)["longest"] == 0 and blocks_form(host, 257, 32, 8, 1, 500)["longest"] == 0
 
