@@ -187,7 +187,7 @@ def test_blocks_sizes(L):
     cut = pkg.attn_decode_blocks_split_keys
     for args in ((0, 32, 8, 1, 100), (1, 32, 7, 1, 100000), (1, 32, 8, 0, 100), (1, 32, 8, 1, 0), (64, 32, 8, 1, 8192)):
         assert cut(*args, 128) == 0, args
-    for args in ((1, 32, 8, 1, 32768), (16, 32, 8, 1, 8192), (1, 8, 8, 300, 65536), (3, 24, 8, 4, 5003)):
+    for args in ((1, 32, 8, 1, 32768), (16, 32, 8, 1, 8192), (1, 8, 8, 300, 65536), (3, 24, 8, 4, 5003), (64, 32, 8, 1, 16384)):
         assert cut(*args, 128) > 0 and cut(*args, 128) % 128 == 0, args
 
 
