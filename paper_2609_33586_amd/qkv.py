@@ -125,10 +125,9 @@ def _strided(name, t, B, S, d, dev):
     return H, sb if B > 1 else 0, ss if S > 1 else 0, sh if H > 1 else 0
 
 
-def _apart(name, t, H, sb, ss, sh):
-    """An output of these heads and strides must not lie over itself: its dimensions, the smallest stride first, each
+def _apart(name, B, S, H, d, sb, ss, sh):
+    """An output of these sizes and strides must not lie over itself: its dimensions, the smallest stride first, each
     beyond the ones before."""
-    B, S, _, d = t.shape
     row = (H - 1) * sh + d
     if (sh >= d or H == 1) and (ss >= row or S == 1) and (sb >= (S - 1) * ss + row or B == 1):
         return  # batches outside positions outside heads
@@ -156,15 +155,13 @@ def _spec(B, S, d, dev, freqs, positions, interleaved, amplitude, q_weight, k_we
     wq = wk = 0
     wt = ATTN_BF16
     if q_weight is not None or k_weight is not None:
-        kind = None
-        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-            if w is None:
-                continue
-            if w.dtype is not _bf16 and w.dtype is not _f32 or kind not in (None, w.dtype):
-                raise TypeError("q_weight and k_weight must be bfloat16, or both float32")
-            kind = _tensor(name, w, (d,), dev).dtype
-        wq = 0 if q_weight is None else q_weight.data_ptr()
-        wk = 0 if k_weight is None else k_weight.data_ptr()
+        kind = (k_weight if q_weight is None else q_weight).dtype
+        if kind is not _bf16 and kind is not _f32 or k_weight is not None and k_weight.dtype is not kind:
+            raise TypeError("q_weight and k_weight must be bfloat16, or both float32")
+        if q_weight is not None:
+            wq = _tensor("q_weight", q_weight, (d,), dev).data_ptr()
+        if k_weight is not None:
+            wk = _tensor("k_weight", k_weight, (d,), dev).data_ptr()
         wt = ATTN_FP32 if kind is _f32 else ATTN_BF16
     return _pack_spec(pptr, each, fptr, rot, 1 if interleaved else 0, amplitude, wq, wk, wt, eps)
 
@@ -235,27 +232,31 @@ def attn_rope_bwd_workspace_bytes(B: int, S: int, Hq: int, Hkv: int, d: int) -> 
     return int(_lib().attn_rope_bwd_workspace_bytes(int(B), int(S), int(Hq), int(Hkv), int(d)))
 
 
-def _grad(name, g, out, B, S, d, dev, first, stream):
+def _grad(gname, g, dname, out, B, S, d, dev, first, stream):
     """Heads of a gradient g [B,H,S,d], the tensor [B,S,H,d] for what it becomes, and that one's strides."""
-    H = _four("g" + name, g)[1]
-    _tensor("g" + name, g, (B, H, S, d), dev, _bf16)
+    shape = g.shape
+    if len(shape) != 4 or g.dtype is not _bf16 or not g.is_contiguous() or g.get_device() != dev:
+        raise ValueError(f"{gname} must be a contiguous bfloat16 tensor [{B}xHx{S}x{d}] on GPU {dev}")
+    b, H, s, e = shape
+    if b != B or s != S or e != d:
+        raise ValueError(f"{gname} must be a contiguous bfloat16 tensor [{B}xHx{S}x{d}] on GPU {dev}")
     if out is None:
         out = _new((B, S, H, d), _bf16, first.device, stream)
-    n, sb, ss, sh = _strided("d" + name, out, B, S, d, dev)
+    n, sb, ss, sh = _strided(dname, out, B, S, d, dev)
     if n != H:
-        raise ValueError(f"d{name} must have g{name}'s heads")
-    _apart("d" + name, out, H, sb, ss, sh)
-    return H, out, (sb, ss, sh)
+        raise ValueError(f"{dname} must have {gname}'s heads")
+    _apart(dname, B, S, H, d, sb, ss, sh)
+    return H, out, sb, ss, sh
 
 
-def _with_weight(name, x, dw, B, S, H, d, dev, first, stream):
+def _with_weight(name, x, wname, dw, B, S, H, d, dev, first, stream):
     """The tensor for a weight's gradient, and the strides of the rows x that it takes."""
     if x is None:
         raise ValueError(f"{name} is required with {name}_weight")
     n, sb, ss, sh = _strided(name, x, B, S, d, dev)
     if n != H:
         raise ValueError(f"{name} must have g{name}'s heads")
-    dw = _new((d,), _f32, first.device, stream) if dw is None else _tensor(f"d{name}_weight", dw, (d,), dev, _f32)
+    dw = _new((d,), _f32, first.device, stream) if dw is None else _tensor(wname, dw, (d,), dev, _f32)
     return dw, sb, ss, sh
 
 
@@ -275,44 +276,36 @@ def attn_rope_bwd(gq, gk=None, gv=None, *, q=None, k=None, freqs=None, positions
         raise ValueError("gq, gk and gv: one at least")
     dev = _current_gpu("gq", first, stream)
     B, _, S, d = _four("gq", first)
-    a = b = c = e = f = g = 0
+    a = b = c = e = f = g = r = s = t = u = w = x = y = z = o = 0  # strides of q, k; dq, dk, dv
     qp = kp = qd = kd = vd = wqp = wkp = None
     Hq = Hkv = 0
     if gq is not None:
-        Hq, dq, grads = _grad("q", gq, dq, B, S, d, dev, first, stream)
+        Hq, dq, r, s, t = _grad("gq", gq, "dq", dq, B, S, d, dev, first, stream)
         if q_weight is not None:
-            dq_weight, a, b, c = _with_weight("q", q, dq_weight, B, S, Hq, d, dev, first, stream)
+            dq_weight, a, b, c = _with_weight("q", q, "dq_weight", dq_weight, B, S, Hq, d, dev, first, stream)
             qp, wqp = q.data_ptr(), dq_weight.data_ptr()
         elif dq_weight is not None:
             raise ValueError("dq_weight without q_weight")
         qd = dq.data_ptr()
     elif dq is not None or dq_weight is not None:
         raise ValueError("dq or dq_weight without gq")
-    else:
-        grads = (0, 0, 0)
     if gk is not None:
-        Hkv, dk, more = _grad("k", gk, dk, B, S, d, dev, first, stream)
-        grads += more
+        Hkv, dk, u, w, x = _grad("gk", gk, "dk", dk, B, S, d, dev, first, stream)
         if k_weight is not None:
-            dk_weight, e, f, g = _with_weight("k", k, dk_weight, B, S, Hkv, d, dev, first, stream)
+            dk_weight, e, f, g = _with_weight("k", k, "dk_weight", dk_weight, B, S, Hkv, d, dev, first, stream)
             kp, wkp = k.data_ptr(), dk_weight.data_ptr()
         elif dk_weight is not None:
             raise ValueError("dk_weight without k_weight")
         kd = dk.data_ptr()
     elif dk is not None or dk_weight is not None:
         raise ValueError("dk or dk_weight without gk")
-    else:
-        grads += (0, 0, 0)
     if gv is not None:
-        n, dv, more = _grad("v", gv, dv, B, S, d, dev, first, stream)
-        grads += more
+        n, dv, y, z, o = _grad("gv", gv, "dv", dv, B, S, d, dev, first, stream)
         if gk is not None and n != Hkv:
             raise ValueError("gk and gv must have the same heads")
         Hkv, vd = n, dv.data_ptr()
     elif dv is not None:
         raise ValueError("dv without gv")
-    else:
-        grads += (0, 0, 0)
     spec = _spec(B, S, d, dev, freqs, positions, interleaved, amplitude, q_weight, k_weight, eps)
     wptr = wbytes = 0
     if wqp is not None or wkp is not None:
@@ -320,7 +313,7 @@ def attn_rope_bwd(gq, gk=None, gv=None, *, q=None, k=None, freqs=None, positions
                                          stream)
     rc = L.attn_rope_bwd(None if gq is None else gq.data_ptr(), None if gk is None else gk.data_ptr(),
                          None if gv is None else gv.data_ptr(), qp, kp, _pack_strides(a, b, c, e, f, g, 0, 0, 0), spec,
-                         qd, kd, vd, _pack_strides(*grads), wqp, wkp, B, S, Hq, Hkv, d, wptr, wbytes,
+                         qd, kd, vd, _pack_strides(r, s, t, u, w, x, y, z, o), wqp, wkp, B, S, Hq, Hkv, d, wptr, wbytes,
                          ctypes.byref(_call_opts(None, stream)))
     if rc != ATTN_OK:
         raise AttnError(rc, "attn_rope_bwd")

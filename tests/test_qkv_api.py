@@ -214,7 +214,7 @@ def test_binding_checks_of_tensors(L):
         qkv._strided("x", torch.zeros(2, 5, 64, 64, dtype=torch.bfloat16).transpose(2, 3), 2, 5, 64, -1)
     def apart(y):
         n, *st = qkv._strided("x", y, *y.shape[:2], 64, -1)
-        return qkv._apart("x", y, n, *st)
+        return qkv._apart("x", *y.shape[:2], n, 64, *st)
 
     for good in (x, x[:, ::2], x.transpose(1, 2), x.transpose(0, 1), x.transpose(0, 2)[:, ::2], x[:1].expand(1, 5, 3, 64),
                  x.as_strided((2, 5, 1, 64), (960, 64, 0, 1))):
