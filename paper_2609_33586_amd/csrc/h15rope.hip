@@ -16,9 +16,9 @@
 //
 // Everything between the operand and the one rounding of the output is FP32.
 //
-// What bounds it: HBM (2 x 4096 positions, 32 heads over 8, d = 128, norms: 201 MB in 43 us,
-// 4.7 TB/s, where a copy reaches 4.9; its gradient at 4 x 2048 positions: 285 MB in 61 us
-// and 3 for the sums), and the launch for a few positions (one of each of 64
+// What bounds it: HBM (2 x 4096 positions, 32 heads over 8, d = 128, norms: 201 MB in 37.5 us,
+// 5.4 TB/s, where a large copy reaches 4.9; its gradient at 4 x 2048 positions: 285 MB in
+// 62 us, 4 of them for the weights' sums), and the launch for a few positions (one of each of 64
 // sequences 4.2 us).  Holding the gradient to 128 registers for a fourth wave on each
 // SIMD costs more than the wave gives (64 us for 55 with inputs in cache).
 #include "qkv_params.h"
@@ -84,6 +84,11 @@ __device__ __forceinline__ void widen16(float (&x)[16], u32x4 a, u32x4 b) {
     x[8 + 2 * i + 1] = __uint_as_float(b[i] & 0xFFFF0000u);
   }
 }
+
+// 16 bytes that are read once (a prompt of 201 MB in and out 43.3 us without the hint,
+// 37.5 so, 39.9 with the outputs' stores hinted, too, which the attention reads next; its
+// gradient 67.7 / 62)
+__device__ __forceinline__ u32x4 stream_in(const uint16_t* p) { return __builtin_nontemporal_load((const u32x4*)p); }
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
@@ -155,7 +160,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_kernel(RopeParams p) {
   if (token >= p.B * p.S) return;  // (a row's lanes leave together)
   const int b = token / p.S, s = token - b * p.S, h0 = r * p.run, h1 = min(h0 + p.run, t.heads);
   const uint16_t* in = t.in + (int64_t)b * t.sb + (int64_t)s * t.ss + (int64_t)h0 * t.sh;
-  u32x4 a0 = *(const u32x4*)(in + at.c0), a1 = *(const u32x4*)(in + at.c1);
+  u32x4 a0 = stream_in(in + at.c0), a1 = stream_in(in + at.c1);
   Turn turn;
   if (at.rotated) turn.set(p, at.l, b, s);
   float w[16];
@@ -167,8 +172,8 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_kernel(RopeParams p) {
     widen16(x, a0, a1);
     if (h + 1 < h1) {
       in += t.sh;
-      a0 = *(const u32x4*)(in + at.c0);
-      a1 = *(const u32x4*)(in + at.c1);
+      a0 = stream_in(in + at.c0);
+      a1 = stream_in(in + at.c1);
     }
     if (t.weight) {
       const float f = inverse_rms<D>(x, p.eps);
@@ -210,8 +215,8 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams 
     const uint16_t* g = (const uint16_t*)t.out + (((size_t)b * t.heads + h0) * (size_t)p.S + s) * D;
     const uint16_t* in = t.in + (int64_t)b * t.sb + (int64_t)s * t.ss + (int64_t)h0 * t.sh;
     uint16_t* dx = t.grad + (int64_t)b * t.gb + (int64_t)s * t.gs + (int64_t)h0 * t.gh;
-    u32x4 a0 = *(const u32x4*)(g + at.c0), a1 = *(const u32x4*)(g + at.c1), x0, x1;
-    if (t.weight) x0 = *(const u32x4*)(in + at.c0), x1 = *(const u32x4*)(in + at.c1);
+    u32x4 a0 = stream_in(g + at.c0), a1 = stream_in(g + at.c1), x0, x1;
+    if (t.weight) x0 = stream_in(in + at.c0), x1 = stream_in(in + at.c1);
     Turn turn;
     if (at.rotated) turn.set(p, at.l, b, s);
 #pragma unroll 1
@@ -221,12 +226,12 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams 
       if (t.weight) widen16(u, x0, x1);
       if (h + 1 < h1) {
         g += (size_t)p.S * D;
-        a0 = *(const u32x4*)(g + at.c0);
-        a1 = *(const u32x4*)(g + at.c1);
+        a0 = stream_in(g + at.c0);
+        a1 = stream_in(g + at.c1);
         if (t.weight) {
           in += t.sh;
-          x0 = *(const u32x4*)(in + at.c0);
-          x1 = *(const u32x4*)(in + at.c1);
+          x0 = stream_in(in + at.c0);
+          x1 = stream_in(in + at.c1);
         }
       }
       if (at.rotated) rotate<INTER, true>(e, turn);
