@@ -22,6 +22,7 @@
 namespace {
 
 constexpr int NW = 4;  // waves per workgroup
+constexpr int AUX_NT = 2;  // non-temporal, among a buffer load's cache bits
 
 template <int D>
 struct BCfg {
@@ -103,7 +104,8 @@ __device__ __forceinline__ int row_limit(const BlocksParams& p, const Work& w, i
   return p.causal ? min(w.last0 + (w.row0 + r) % p.Sq, w.nk - 1) : w.nk - 1;
 }
 
-template <int D, int MODE>
+// STREAM: the keys are read once and fill more than the caches hold (p.stream).
+template <int D, int MODE, bool STREAM>
 __device__ __forceinline__ void keys_form(const BlocksParams& p, const Work& w, uint8_t* ksm, uint8_t* vsm,
                                           float (*mx_lds)[32][NW], float (*m_lds)[NW], float (*l_lds)[NW]) {
   using C = BCfg<D>;
@@ -140,7 +142,8 @@ __device__ __forceinline__ void keys_form(const BlocksParams& p, const Work& w, 
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const uint32_t soff = min((uint32_t)first_key(c) * RB + i * 1024, part_bytes);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, LDS_PTR(void, slot + i * 1024), 16, off[i & mask], soff, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, LDS_PTR(void, slot + i * 1024), 16, off[i & mask], soff, 0,
+                                               STREAM ? AUX_NT : 0);
     }
   };
   int pair[NB];
@@ -729,7 +732,9 @@ __device__ __forceinline__ bool find_work(const BlocksParams& p, int* scratch, W
   return true;
 }
 
-template <int D, int MODE, bool ROWS>
+enum { FORM_KEYS = 0, FORM_KEYS_STREAM = 1, FORM_ROWS = 2 };
+
+template <int D, int MODE, int FORM>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_blocks_kernel(
     BlocksParams p) {
   using C = BCfg<D>;
@@ -740,8 +745,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __shared__ __attribute__((aligned(16))) float m_lds[32][NW], l_lds[32][NW];
   Work w;
   if (!find_work<D>(p, (int*)mx_lds, w)) return;
-  if constexpr (ROWS) rows_form<D, MODE>(p, w, ksm, vsm);
-  else keys_form<D, MODE>(p, w, ksm, vsm, mx_lds, m_lds, l_lds);
+  if constexpr (FORM == FORM_ROWS) rows_form<D, MODE>(p, w, ksm, vsm);
+  else keys_form<D, MODE, FORM == FORM_KEYS_STREAM>(p, w, ksm, vsm, mx_lds, m_lds, l_lds);
 }
 
 template <int D>
@@ -769,8 +774,9 @@ template <int D, int MODE>
 hipError_t launch_one(const BlocksParams& p, hipStream_t st) {
   const dim3 grid((unsigned)p.groups), block(NW * 64);
   if (p.rows == BLOCKS_WIDE && MODE == MODE_EXACT) hipLaunchKernelGGL((attn_blocks_wide_kernel<D>), grid, dim3(BLOCKS_WIDE), 0, st, p);
-  else if (p.rows == WROWS) hipLaunchKernelGGL((attn_blocks_kernel<D, MODE, false>), grid, block, 0, st, p);
-  else hipLaunchKernelGGL((attn_blocks_kernel<D, MODE, true>), grid, block, 0, st, p);
+  else if (p.rows != WROWS) hipLaunchKernelGGL((attn_blocks_kernel<D, MODE, FORM_ROWS>), grid, block, 0, st, p);
+  else if (p.stream) hipLaunchKernelGGL((attn_blocks_kernel<D, MODE, FORM_KEYS_STREAM>), grid, block, 0, st, p);
+  else hipLaunchKernelGGL((attn_blocks_kernel<D, MODE, FORM_KEYS>), grid, block, 0, st, p);
   return hipGetLastError();
 }
 

@@ -80,6 +80,7 @@ struct BlocksParams {
   int rows;           // query rows of a workgroup: WROWS, BLOCKS_ROWS or BLOCKS_WIDE
   int row_blocks;     // of a sequence and KV head
   int longest;        // caches are taken in the order of their lengths (B <= 256)
+  int stream;         // keys are read with a streaming hint (keys form)
   int groups;
   float c1, ck;
 };

@@ -34,7 +34,7 @@ int h15_stub_append(int what) {
 }
 int h15_stub_blocks(int what) {
   const int v[] = {g_blocks.parts, g_blocks.split, g_blocks.rows, g_blocks.row_blocks, g_blocks.groups,
-                   g_blocks.causal, g_blocks.longest, g_blocks.blocks, g_blocks.shift};
+                   g_blocks.causal, g_blocks.longest, g_blocks.blocks, g_blocks.shift, g_blocks.stream};
   return v[what];
 }
 }

@@ -156,6 +156,13 @@ def test_many_ragged_caches():
         run_and_check(B, Hkv, Hkv, 1, 200, 64, 64, lens, f"{B} caches", sharp=False)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("mode", [EXACT, H15, SQ4, SQ8])
+def test_caches_with_room_for_many_keys(d, mode):
+    # (the form for more keys than the caches hold goes by the room)
+    run_and_check(3, 4, 2, 2, 131072 * 128 // d * 2 // 3, d, 32, [700, 0, 1025], f"{mode}", mode, 256, sharp=False)
+
+
 def test_equals_decode_of_the_same_numbers():
     # with one scale for all, the BF16 decode of the numbers that the codes stand for, up to the order of sums
     q, (k, v, scales) = normal((2, 8, 4, 128), 9), block_cache(2, 2, 600, 128, 64, 10)

@@ -92,7 +92,7 @@ def blocks_form(L, B, Hq, Hkv, Sq, Sk, cut=0, lens=at(4), causal=1, d=128, block
     rc = L.attn_decode_blocks(at(0), at(1), at(2), at(3), lens, at(5), None, B, Hq, Hkv, Sq, Sk, Sk, d, block, causal, 0.1, mode, cut,
                               at(7), 1 << 40, None)
     assert rc == pkg.ATTN_ELAUNCH
-    names = ("parts", "split", "rows", "row_blocks", "groups", "causal", "longest", "blocks", "shift")
+    names = ("parts", "split", "rows", "row_blocks", "groups", "causal", "longest", "blocks", "shift", "stream")
     return {n: L.h15_stub_blocks(i) for i, n in enumerate(names)}
 
 
@@ -112,6 +112,10 @@ def test_blocks_forms(host):
     assert blocks_form(host, 1, 32, 8, 512, 16383)["rows"] == 128 and blocks_form(host, 1, 32, 8, 2048, 8191)["rows"] == 128
     assert blocks_form(host, 256, 1, 1, 511, 8192)["rows"] == 128 and blocks_form(host, 256, 1, 1, 512, 8192)["rows"] == 512
     assert blocks_form(host, 1, 32, 8, 512, 16384, 2048)["groups"] == 256
+    # keys that one workgroup reads, 128 MB of them and more: with the hint
+    assert blocks_form(host, 16, 32, 8, 1, 4095)["stream"] == 0 and blocks_form(host, 16, 32, 8, 1, 4096)["stream"] == 1
+    assert blocks_form(host, 16, 32, 8, 8, 4096)["stream"] == 1 and blocks_form(host, 16, 32, 8, 9, 4096)["stream"] == 0
+    assert blocks_form(host, 16, 32, 8, 1, 4096, d=64)["stream"] == 0
     assert blocks_form(host, 64, 32, 8, 1, 500)["longest"] == 0 and blocks_form(host, 65, 32, 8, 1, 500)["longest"] == 1
     assert blocks_form(host, 65, 32, 8, 1, 500, lens=None)["longest"] == 0 and blocks_form(host, 257, 32, 8, 1, 500)["longest"] == 0
 
