@@ -91,8 +91,9 @@ typedef struct attn_rope_spec {
  * output that overlaps an input or another output; ATTN_EUNSUPPORTED for d
  * not in {64, 128}, rot not a multiple of 16, an unknown dtype or
  * weight_dtype, a stride that is negative or no multiple of 8, a pointer that
- * is not 16-byte aligned (positions: 4, freqs: 8), or more than 2^31 - 1
- * positions in all or rows (of one head and position) in one output. */
+ * is not 16-byte aligned (positions: 4, freqs: 8), more than 2^31 - 1 rows (of
+ * one head and position) in one output, more than 2^24 - 1 times 4096 / d
+ * positions in all, or Hq + 2 Hkv > 65535. */
 int attn_rope(const void* q, const void* k, const void* v, const attn_strides* strides, const attn_rope_spec* spec,
               void* q_out, void* k_out, void* v_out, int B, int S, int Hq, int Hkv, int d, int dtype,
               const attn_opts* opts);
@@ -205,12 +206,13 @@ int attn_cache_append(const void* k, const void* v, void* k_cache, void* v_cache
  *
  * Errors: ATTN_EINVAL for a null pointer (lens and lse may be), a size that is
  * not positive, Sk > Sk_cap, Hq % Hkv != 0, a scale that is not positive and
- * finite, a cut that is negative or no multiple of attn_tile_bc(), or a missing
- * or short workspace; ATTN_EUNSUPPORTED for d not in {64, 128}, another block,
- * another exp_mode, q, k, v or o not 16-byte aligned (lse, lens: 4, scales:
- * 2), a rescale threshold other than 0, B * Hq * Sq > 2^30 (2^26 - 1 with more
- * than one part), one head's cache beyond 2^31 - 1 bytes, or more than 2^24 - 1
- * workgroups. */
+ * finite, a cut that is negative or no multiple of attn_tile_bc(), a missing or
+ * short workspace, or an output or workspace that overlaps an input or another
+ * output; ATTN_EUNSUPPORTED for d not in {64, 128}, another block, another
+ * exp_mode, q, k, v or o not 16-byte aligned (lse, lens: 4, scales: 2), a
+ * rescale threshold other than 0, B * Hq * Sq > 2^30 (2^26 - 4 with more than
+ * one part), one head's cache beyond 2^31 - 1 bytes, or more workgroups than
+ * have 2^32 - 256 threads. */
 int attn_decode_blocks(const void* q, const void* k, const void* v, const uint8_t* scales, const int32_t* lens,
                        void* o, float* lse, int B, int Hq, int Hkv, int Sq, int Sk, int Sk_cap, int d, int block,
                        int causal, float scale, int exp_mode, int split_keys, void* workspace,

@@ -20,8 +20,8 @@ long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 bool misaligned(const void* x, uintptr_t to) { return ((uintptr_t)x & (to - 1)) != 0; }
 
 // Work-items of a launch are counted in 32 bits: workgroups of 256 threads, and
-// rows of a merge, which have 64 each.
-constexpr long long MAX_GROUPS = (1LL << 24) - 1, MAX_MERGE_ROWS = (1LL << 26) - 1;
+// rows of a merge, four to a workgroup.
+constexpr long long MAX_GROUPS = (1LL << 24) - 1, MAX_MERGE_ROWS = 4 * MAX_GROUPS;
 
 struct Range {
   uintptr_t from, to;
@@ -42,12 +42,12 @@ bool any_overlap(const Range (&out)[N], const Range (&in)[M]) {
 
 // Strides of [B][S][H][d], the given ones or the contiguous ones; false if they
 // are not usable.
-bool strides_of(const attn_strides* given, int S, int H, int d, attn_strides* s) {
+bool strides_of(const attn_strides* given, int B, int S, int H, int d, attn_strides* s) {
   *s = given ? *given : attn_strides{(int64_t)S * H * d, (int64_t)H * d, d};
-  const int64_t most = INT64_MAX >> 34;  // (times sizes of up to 2^31, in bytes)
-  const int64_t all[] = {s->batch, s->position, s->head};
-  for (int64_t x : all)
-    if (x < 0 || x > most || x % 8 != 0) return false;
+  const int64_t most = INT64_MAX >> 4;  // (three of them in bytes)
+  const int64_t all[] = {s->batch, s->position, s->head}, n[] = {B, S, H};
+  for (int i = 0; i < 3; ++i)
+    if (all[i] < 0 || all[i] > most / n[i] || all[i] % 8 != 0) return false;
   return true;
 }
 
@@ -117,7 +117,7 @@ int check_rope(const attn_rope_spec* spec, int B, int S, int Hq, int Hkv, const 
   p->S = S;
   p->d = d;
   const RopeShape r = rope_shape(B, S, Hq, Hkv, d);
-  if (r.tiles > MAX_GROUPS || (long long)r.runs[0] + 2 * r.runs[1] > 65535) return ATTN_EUNSUPPORTED;
+  if (r.tiles > MAX_GROUPS || Hq + 2LL * Hkv > 65535) return ATTN_EUNSUPPORTED;
   p->tiles = (int)r.tiles;
   p->run = r.run;
   p->groups = r.groups;
@@ -215,7 +215,8 @@ int attn_rope(const void* q, const void* k, const void* v, const attn_strides* s
     attn_strides s = {};
     if (in[i]) {
       if (!finite_pos(descale[i])) return ATTN_EINVAL;
-      if (misaligned(in[i], 16) || misaligned(out[i], 16) || !strides_of(strides ? strides + i : nullptr, S, heads[i], d, &s))
+      if (misaligned(in[i], 16) || misaligned(out[i], 16) ||
+          !strides_of(strides ? strides + i : nullptr, B, S, heads[i], d, &s))
         return ATTN_EUNSUPPORTED;
       ins[i] = reach(in[i], s, B, S, heads[i], d);
     } else {
@@ -270,10 +271,10 @@ int attn_rope_bwd(const void* gq, const void* gk, const void* gv, const void* q,
     const bool norm = t.weight != nullptr;
     if (norm && (!in[i] || !dweight[i])) return ATTN_EINVAL;
     if (g[i] && (misaligned(g[i], 16) || misaligned(out[i], 16) ||
-                 !strides_of(grad_strides ? grad_strides + i : nullptr, S, heads[i], d, &gs)))
+                 !strides_of(grad_strides ? grad_strides + i : nullptr, B, S, heads[i], d, &gs)))
       return ATTN_EUNSUPPORTED;
     if (norm && (misaligned(in[i], 16) || misaligned(dweight[i], 4) ||
-                 !strides_of(strides ? strides + i : nullptr, S, heads[i], d, &s)))
+                 !strides_of(strides ? strides + i : nullptr, B, S, heads[i], d, &s)))
       return ATTN_EUNSUPPORTED;
     ins[i] = range(g[i], (size_t)B * S * heads[i] * d * 2);
     ins[3 + i] = norm ? reach(in[i], s, B, S, heads[i], d) : range(nullptr, 0);
@@ -419,7 +420,8 @@ int attn_decode_blocks(const void* q, const void* k, const void* v, const uint8_
   p.rows = blocks_rows((long long)B * Hkv, p.R, Sk, order == 0);
   p.row_blocks = (int)ceil_div(p.R, p.rows);
   const long long groups = (long long)B * Hkv * p.parts * p.row_blocks;
-  if (groups > MAX_GROUPS || (p.parts > 1 && rows > MAX_MERGE_ROWS)) return ATTN_EUNSUPPORTED;
+  if (groups > MAX_GROUPS / (p.rows == BLOCKS_WIDE ? 2 : 1) || (p.parts > 1 && rows > MAX_MERGE_ROWS))
+    return ATTN_EUNSUPPORTED;
   p.groups = (int)groups;
   // ragged caches that are more than one for each slot are taken longest first, so
   // that no long one starts last
@@ -431,6 +433,11 @@ int attn_decode_blocks(const void* q, const void* k, const void* v, const uint8_
     p.part_o = (float*)workspace;
     p.part_ml = p.part_o + (size_t)rows * p.parts * d;
   }
+  const size_t heads = (size_t)B * Hkv, codes = heads * Sk_cap * d;
+  const Range in[] = {range(q, (size_t)rows * d * 2), range(k, codes), range(v, codes),
+                      range(scales, heads * p.blocks * 2), range(lens, (size_t)B * 4)};
+  const Range out[] = {range(o, (size_t)rows * d * 2), range(lse, (size_t)rows * 4), range(need ? workspace : nullptr, need)};
+  if (any_overlap(out, in)) return ATTN_EINVAL;
   const int mode = order == 0 ? (int)MODE_EXACT : 2 * order - 1;
   return launch_blocks(p, d, mode, opts ? opts->stream : nullptr) == 0 ? ATTN_OK : ATTN_ELAUNCH;
 }

@@ -91,8 +91,8 @@ def attn_rope_frequencies(rot: int, base: float = 10000.0, *, scaling: str | Non
     if scaling == "linear":
         f = f / factor
     elif scaling in ("ramp", "smooth"):
-        if original is None or original <= 0 or not 0 < slow < fast:
-            raise ValueError(f"scaling '{scaling}' takes the original context's length and 0 < slow < fast")
+        if original is None or original <= 0 or not 0 < slow < fast or not base > 1:
+            raise ValueError(f"scaling '{scaling}' takes the original context's length, 0 < slow < fast, and a base above 1")
         turns = original * f / (2 * math.pi)
         if scaling == "smooth":
             keep = ((turns - slow) / (fast - slow)).clamp(0.0, 1.0)
@@ -190,8 +190,8 @@ def attn_rope(q, k=None, v=None, *, freqs=None, positions=None, interleaved: boo
     B, S, _, d = first.shape
     given = q_out if q_out is not None else k_out if k_out is not None else v_out
     dtype = given.dtype if given is not None else _bf16 if out_dtype is None else out_dtype
-    if dtype is not _bf16 and dtype is not _fp8:
-        raise TypeError("attn_rope writes bfloat16 or float8_e4m3fn")
+    if dtype is not _bf16 and dtype is not _fp8 or out_dtype is not None and out_dtype is not dtype:
+        raise TypeError("attn_rope writes bfloat16 or float8_e4m3fn, all outputs the same")
     Hq = Hkv = a = b = c = e = f = g = h = i = j = 0
     qp = kp = vp = qo = ko = vo = None
     if q is not None:

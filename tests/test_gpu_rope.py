@@ -65,6 +65,15 @@ def test_strides():
     run_and_check(one, None, None, "strides of one element", freqs=f)
 
 
+def test_batches_far_apart():
+    # (as those of long projections: beyond 2^31 elements)
+    far = 2 ** 31 + 64
+    x = torch.empty((far + 5 * 6 * 64,), dtype=BF16, device="cuda")
+    view = x.as_strided((2, 5, 6, 64), (far, 6 * 64, 64, 1))
+    view.copy_(normal((2, 5, 6, 64), 5))
+    run_and_check(*view.split([4, 1, 1], 2), "far apart", freqs=freqs_of(64)[0], wq=1 + 0.3 * normal((64,), 6, torch.float32))
+
+
 @pytest.mark.parametrize("inter", [False, True])
 def test_far_positions(inter):
     # (angles of 2^31 radians: reduced in 64 bits, they are as exact as FP64 has them)

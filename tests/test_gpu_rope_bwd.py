@@ -62,6 +62,18 @@ def test_many_positions_and_a_fused_gradient():
     assert all(torch.equal(a, b) for a, b in zip(got, again))  # (a fixed order of sums)
 
 
+def test_batches_far_apart():
+    # (as those of long projections: beyond 2^31 elements, those of a fused gradient too)
+    far = 2 ** 31 + 64
+    x, out = (torch.empty((far + 5 * 6 * 64,), dtype=BF16, device="cuda").as_strided((2, 5, 6, 64), (far, 6 * 64, 64, 1))
+              for _ in range(2))
+    x.copy_(normal((2, 5, 6, 64), 5))
+    w = 1 + 0.3 * normal((64,), 6, torch.float32)
+    dq, dk, dv = out.split([4, 1, 1], 2)
+    run_and_check(x.split([4, 1, 1], 2), gradients(2, 5, 4, 1, 64, 7), "far apart", freqs=pkg.attn_rope_frequencies(64, device="cuda")[0],
+                  wq=w, wk=w, dq=dq, dk=dk, dv=dv)
+
+
 def test_only_some_tensors():
     x, g = projection(2, 40, 4, 2, 128, 3), gradients(2, 40, 4, 2, 128, 4)
     f, w = pkg.attn_rope_frequencies(128, device="cuda")[0], 1 + 0.3 * normal((128,), 5, torch.float32)

@@ -63,7 +63,8 @@ BAD_SPEC_UNS = ({"rot": 8}, {"rot": 126}, {"wt": 1}, {"wt": 3}, {"positions": at
                 {"kw": at(13) + 8})
 BAD_SIZES_INV = ({"B": 0}, {"S": 0}, {"d": 0}, {"Hq": 0}, {"Hkv": 0}, {"Hq": -1})
 BAD_SIZES_UNS = ({"d": 96}, {"d": 256}, {"B": 1 << 16, "S": 1 << 15}, {"B": 1 << 14, "S": 1 << 14, "Hq": 8}, {"Hq": 1 << 20, "Hkv": 1 << 20},
-                 {"B": 1 << 15, "S": 1 << 15, "Hq": 1, "Hkv": 1})
+                 {"B": 1 << 15, "S": 1 << 15, "Hq": 1, "Hkv": 1}, {"B": 1, "S": 32 * (2 ** 24 - 1) + 1, "Hq": 1, "Hkv": 1},
+                 {"B": 1, "S": 1, "Hq": 65534, "Hkv": 1})
 
 
 def test_rope_refusals(L):
@@ -97,6 +98,10 @@ def test_rope_refusals(L):
                     assert rope(L, **{out: at(i) + inputs[name] - 16}) == INV, (out, name)
         for i in range(10, 14):
             assert rope(L, **{out: at(i)}) == INV, (out, i)
+    # the last stride that sizes allow, and the next (in elements; an output beyond 2^63 bytes is an address of no one)
+    assert rope(L, q=at(0), B=1, S=3, st=strides(0, (2 ** 59 - 1) // 3 // 8 * 8 + 8, 128, *good[3:])) == UNS
+    # a projection's batches further apart than 2^29 elements are taken: this call is refused for its output alone
+    assert rope(L, qo=at(0) + 2 * (1 << 33), st=strides(1 << 33, 512, 128, *good[3:])) == INV
     assert rope(L, qo=at(0) + 2 * 100, st=strides(1 << 20, 512, 128, *good[3:])) == UNS
     assert rope(L, qo=at(0) + 2 * (1 << 20), st=strides(1 << 20, 512, 128, *good[3:])) == INV
 
@@ -173,12 +178,20 @@ def test_blocks_refusals(L):
         assert blocks(L, **kw) == INV, kw
     for kw in ({"d": 96}, {"block": 0}, {"block": 8}, {"block": 96}, {"block": 256}, {"mode": pkg.ATTN_EXP_ROWMAX_POT}, {"mode": 9},
                {"o_": opts(tau=8.0)}, {"cap": 1 << 24}, {"B": 1 << 15, "Hq": 1 << 14, "Sq": 4}, {"B": 1 << 12, "Hq": 1 << 13, "Hkv": 1 << 13},
-               {"B": 1 << 13, "Hq": 1 << 13, "Hkv": 1, "cut": 128}):
+               {"B": 1 << 13, "Hq": 1 << 13, "Hkv": 1, "cut": 128}, {"B": 1, "Hq": 2 ** 26 - 3, "Hkv": 1, "cut": 128},
+               {"B": 1 << 12, "Hq": 1, "Hkv": 1, "Sq": 512, "Sk": 1 << 19, "cap": 1 << 19, "cut": 128, "mode": 0}):
         assert blocks(L, **kw) == UNS, kw
     need = pkg.attn_decode_blocks_workspace_bytes(2, 4, 1, 300, 128, 128)
     assert need == 2 * 4 * 3 * (128 + 2) * 4
     for ws, wsb in ((None, need), (at(7) + 8, need), (at(7), need - 1)):
         assert blocks(L, cut=128, ws=ws, wsb=wsb) == INV
+    # an output or the workspace on an input or another output, from its first or up to its last byte
+    sizes = (2 * 4 * 256, 2 * 2 * 320 * 128, 2 * 2 * 320 * 128, 2 * 2 * 5 * 2, 8, 2 * 4 * 256, 2 * 4 * 4, need)
+    for out, i in (("o", 5), ("lse", 6), ("ws", 7)):
+        for j in range(8):
+            if j != i:
+                assert blocks(L, cut=128, **{out: at(j)}) == INV, (out, j)
+                assert blocks(L, cut=128, **{out: at(j) + (sizes[j] - 1) // 16 * 16}) == INV, (out, j)
 
 
 def test_blocks_sizes(L):
@@ -277,7 +290,8 @@ def test_frequencies():
     keep = (turns - 1) / 3
     assert bool(mid.any()) and torch.allclose(f[mid], (p * keep + p / 4 * (1 - keep))[mid], rtol=1e-13)
     for bad in (dict(rot=3), dict(rot=0), dict(rot=64, base=0.0), dict(rot=64, scaling="other"), dict(rot=64, scaling="linear", factor=0.5),
-                dict(rot=64, scaling="ramp", factor=2.0), dict(rot=64, scaling="smooth", factor=2.0, original=100, slow=4.0, fast=1.0),
+                dict(rot=64, scaling="ramp", factor=2.0),
+                dict(rot=64, base=1.0, scaling="ramp", factor=2.0, original=100), dict(rot=64, scaling="smooth", factor=2.0, original=100, slow=4.0, fast=1.0),
                 dict(rot=2, scaling="base", factor=2.0)):
         with pytest.raises(ValueError):
             pkg.attn_rope_frequencies(bad.pop("rot"), bad.pop("base", 10000.0), **bad)
