@@ -17,9 +17,14 @@ class Strided(Tensor):
         return tuple(s)
 
 
+@pytest.fixture
+def bound():
+    """The binding's own library, before another stands in for the package's."""
+    return qkv._lib()
+
+
 @pytest.fixture(autouse=True)
-def library(pool, monkeypatch):  # noqa: F811
-    qkv._lib()
+def library(bound, pool, monkeypatch):  # noqa: F811
     monkeypatch.setattr(qkv, "_bound", Library())
     empty = torch.empty
 
@@ -29,6 +34,7 @@ def library(pool, monkeypatch):  # noqa: F811
         return t
 
     monkeypatch.setattr(torch, "empty", strided)
+    monkeypatch.setattr(torch, "empty_strided", lambda shape, strides, **kw: strided(shape, **kw))
 
 
 Q, KV = Strided(2, 5, 4, 64), Strided(2, 5, 2, 64)  # [B, S, H, d]
