@@ -10,8 +10,8 @@ import ctypes
 import math
 import struct
 
-from . import ATTN_BF16, ATTN_FP8_E4M3, ATTN_OK, AttnError, _dtype_of, _new, _outputs, attn_opts, cache, lib
-from .cache import _call_opts, _current_gpu, _four, _lens_ptr, _refuse, _space, _tensor
+from . import ATTN_BF16, ATTN_FP8_E4M3, ATTN_OK, AttnError, _dtype_of, _new, _outputs, cache, lib
+from .cache import _current_gpu, _current_stream, _four, _lens_ptr, _refuse, _space, _tensor
 
 ATTN_FP32 = 2  # type of norm weights, next to ATTN_BF16
 
@@ -29,17 +29,17 @@ class attn_rope_spec(ctypes.Structure):
 
 _bound = None
 _torch = None
-_bf16 = _f32 = _f64 = _i32 = _fp8 = None  # torch's types, bound with the library
+_bf16 = _f32 = _f64 = _i32 = _fp8 = _e8m0 = None  # torch's types, bound with the library
 
 
 def _lib() -> ctypes.CDLL:
     """The library with the argument types of these functions, bound on first use."""
-    global _bound, _torch, _bf16, _f32, _f64, _i32, _fp8
+    global _bound, _torch, _bf16, _f32, _f64, _i32, _fp8, _e8m0
     if _bound is not None:
         return _bound
     L = lib()
     P, I, F, S = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
-    O = ctypes.POINTER(attn_opts)
+    O = P  # (structures are given as the bytes that they consist of)
     for name, args, res in (
             ("attn_rope", [P] * 8 + [I] * 6 + [O], I),
             ("attn_rope_bwd", [P] * 13 + [I] * 5 + [P, S, O], I),
@@ -53,6 +53,7 @@ def _lib() -> ctypes.CDLL:
     import torch
     _torch = torch
     _bf16, _f32, _f64, _i32, _fp8 = torch.bfloat16, torch.float32, torch.float64, torch.int32, torch.float8_e4m3fn
+    _e8m0 = torch.float8_e8m0fnu
     cache._lib()  # (its checks use its own binding of torch)
     _bound = L
     return L
@@ -145,8 +146,15 @@ def _apart(name, B, S, H, d, sb, ss, sh):
         end += stride * (n - 1)
 
 
-_pack_spec = struct.Struct("@PiPiifPPif").pack  # attn_rope_spec, which a call reads before it returns
+# Structures that a call reads before it returns, as their bytes: a third of the time of ctypes' own.
+_pack_spec = struct.Struct("@PiPiifPPif").pack  # attn_rope_spec
 _pack_strides = struct.Struct("@9q").pack  # attn_strides of three tensors
+_pack_opts = struct.Struct("@fffPfi").pack  # attn_opts
+
+
+def _opts(stream, descale=(1.0, 1.0, 1.0)):
+    qd, kd, vd = descale
+    return _pack_opts(qd, kd, vd, stream.cuda_stream if stream is not None else _current_stream(), 0.0, 0)
 
 
 def _spec(B, S, d, dev, freqs, positions, interleaved, amplitude, q_weight, k_weight, eps):
@@ -157,7 +165,7 @@ def _spec(B, S, d, dev, freqs, positions, interleaved, amplitude, q_weight, k_we
             _tensor("freqs", freqs, (rot // 2,), dev, _f64)
         fptr = freqs.data_ptr()
     if positions is not None:
-        each = 1 if positions.dim() == 2 else 0
+        each = 1 if len(positions.shape) == 2 else 0
         pptr = _tensor("positions", positions, (B, S) if each else (B,), dev, _i32).data_ptr()
     wq = wk = 0
     wt = ATTN_BF16
@@ -229,7 +237,7 @@ def attn_rope(q, k=None, v=None, *, freqs=None, positions=None, interleaved: boo
         raise ValueError("v_out without v")
     spec = _spec(B, S, d, dev, freqs, positions, interleaved, amplitude, q_weight, k_weight, eps)
     rc = L.attn_rope(qp, kp, vp, _pack_strides(a, b, c, e, f, g, h, i, j), spec, qo, ko, vo, B, S, Hq, Hkv, d,
-                     ATTN_BF16 if dtype is _bf16 else ATTN_FP8_E4M3, ctypes.byref(_call_opts(descale, stream)))
+                     ATTN_BF16 if dtype is _bf16 else ATTN_FP8_E4M3, _opts(stream) if descale is None else _opts(stream, descale))
     if rc != ATTN_OK:
         raise AttnError(rc, "attn_rope")
     return q_out, k_out, v_out
@@ -321,7 +329,7 @@ def attn_rope_bwd(gq, gk=None, gv=None, *, q=None, k=None, freqs=None, positions
     rc = L.attn_rope_bwd(None if gq is None else gq.data_ptr(), None if gk is None else gk.data_ptr(),
                          None if gv is None else gv.data_ptr(), qp, kp, _pack_strides(a, b, c, e, f, g, 0, 0, 0), spec,
                          qd, kd, vd, _pack_strides(r, s, t, u, w, x, y, z, o), wqp, wkp, B, S, Hq, Hkv, d, wptr, wbytes,
-                         ctypes.byref(_call_opts(None, stream)))
+                         _opts(stream))
     if rc != ATTN_OK:
         raise AttnError(rc, "attn_rope_bwd")
     return dq, dk, dv, dq_weight, dk_weight
@@ -329,17 +337,27 @@ def attn_rope_bwd(gq, gk=None, gv=None, *, q=None, k=None, freqs=None, positions
 
 # ---- a cache of 8-bit blocks ----------------------------------------------------
 
+def _bf16_rows(name, t):
+    """The sizes of a contiguous bf16 tensor [.,.,.,d]."""
+    shape = _four(name, t)
+    if t.dtype is not _bf16:
+        raise ValueError(f"{name} must be a bfloat16 tensor")
+    return shape
+
+
 def _codes(name, t, B, Hkv, d, dev):
     """Rows of a cache of e4m3 codes [B,Hkv,rows,d]."""
     shape = t.shape
-    if len(shape) != 4 or _dtype_of(t) != ATTN_FP8_E4M3:
+    if len(shape) != 4 or t.dtype is not _fp8 and _dtype_of(t) != ATTN_FP8_E4M3:
         raise TypeError(f"{name} must be a 4-D tensor of float8_e4m3fn")
-    _tensor(name, t, (B, Hkv, shape[2], d), dev)
-    return shape[2]
+    b, h, rows, e = shape
+    if b != B or h != Hkv or e != d or not t.is_contiguous() or t.get_device() != dev:
+        _tensor(name, t, (B, Hkv, rows, d), dev)
+    return rows
 
 
 def _scales(t, B, Hkv, cap, block, dev):
-    if t.dtype != _torch.float8_e8m0fnu and t.dtype != _torch.uint8:
+    if t.dtype is not _e8m0 and t.dtype is not _torch.uint8:
         raise TypeError("scales must be float8_e8m0fnu (or uint8, their bytes)")
     if not 0 < block < 2 ** 31:
         raise ValueError(f"block is out of range: {block}")
@@ -355,9 +373,8 @@ def attn_cache_append(k, v, k_cache, v_cache, scales, lens, *, block: int, count
     rows of each sequence (default n).  Returns lens_out, int32 [B], the slots
     filled after: the given tensor, which may be lens, or a new one."""
     L = _lib()
-    B, Hkv, n, d = shape = _four("k", k)
+    B, Hkv, n, d = shape = _bf16_rows("k", k)
     dev = _current_gpu("k", k, stream)
-    _tensor("k", k, shape, dev, _bf16)
     _tensor("v", v, shape, dev, _bf16)
     cap = _codes("k_cache", k_cache, B, Hkv, d, dev)
     if _codes("v_cache", v_cache, B, Hkv, d, dev) != cap:
@@ -367,9 +384,8 @@ def attn_cache_append(k, v, k_cache, v_cache, scales, lens, *, block: int, count
     cptr = None if counts is None else _tensor("counts", counts, (B,), dev, _i32).data_ptr()
     lens_out = _new((B,), _i32, k.device, stream) if lens_out is None else \
         _tensor("lens_out", lens_out, (B,), dev, _i32)
-    opts = _call_opts(None, stream)
     rc = L.attn_cache_append(k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), sptr, lptr, cptr,
-                             lens_out.data_ptr(), B, Hkv, n, cap, d, block, ctypes.byref(opts))
+                             lens_out.data_ptr(), B, Hkv, n, cap, d, block, _opts(stream))
     if rc != ATTN_OK:
         raise AttnError(rc, "attn_cache_append")
     return lens_out
@@ -394,9 +410,8 @@ def attn_decode_blocks(q, k, v, scales, *, block: int, causal: bool, scale: floa
     them, whose first lens[b] slots (int32 [B]; default Sk, default all) are
     filled.  Returns (O [B,Hq,Sq,d] bf16, LSE [B,Hq,Sq] fp32 or None)."""
     L = _lib()
-    B, Hq, Sq, d = shape = _four("q", q)
+    B, Hq, Sq, d = shape = _bf16_rows("q", q)
     dev = _current_gpu("q", q, stream)
-    _tensor("q", q, shape, dev, _bf16)
     Hkv = _four("k", k)[1]
     cap = _codes("k", k, B, Hkv, d, dev)
     if _codes("v", v, B, Hkv, d, dev) != cap:
@@ -412,10 +427,9 @@ def attn_decode_blocks(q, k, v, scales, *, block: int, causal: bool, scale: floa
         _tensor("lse", lse, shape[:3], dev, _f32)
     wptr, wbytes, workspace = _space(workspace, lambda: L.attn_decode_blocks_workspace_bytes(B, Hq, Sq, Sk, d,
                                                                                             split_keys), dev, stream)
-    opts = _call_opts(None, stream)
     rc = L.attn_decode_blocks(q.data_ptr(), k.data_ptr(), v.data_ptr(), sptr, _lens_ptr(lens, B, dev), out.data_ptr(),
                               lse.data_ptr() if lse is not None else None, B, Hq, Hkv, Sq, Sk, cap, d, block,
-                              1 if causal else 0, scale, exp_mode, split_keys, wptr, wbytes, ctypes.byref(opts))
+                              1 if causal else 0, scale, exp_mode, split_keys, wptr, wbytes, _opts(stream))
     if rc != ATTN_OK:
         raise AttnError(rc, "attn_decode_blocks")
     return out, lse

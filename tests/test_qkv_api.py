@@ -250,6 +250,11 @@ def test_binding_checks_of_tensors(L):
     for kw in ({"q_weight": w.half()}, {"k_weight": w.bfloat16()}):
         with pytest.raises(TypeError):
             qkv._spec(2, 5, 64, -1, **{**good, **kw})
+    side = type("Stream", (), {"cuda_stream": 0x1234500000})
+    for o, want in ((qkv._opts(side), (1.0, 1.0, 1.0)), (qkv._opts(side, (0.5, 2, 4.0)), (0.5, 2.0, 4.0))):
+        o = pkg.attn_opts.from_buffer_copy(o)
+        assert (o.q_descale, o.k_descale, o.v_descale) == want and o.stream == 0x1234500000
+        assert o.rescale_threshold == 0.0 and o.rescale_per_wave == 0
     c, sc = torch.zeros(1, 2, 70, 64, dtype=torch.uint8), torch.zeros(1, 2, 3, 2, dtype=torch.uint8)
     assert qkv._codes("k", c, 1, 2, 64, -1) == 70 and qkv._scales(sc, 1, 2, 70, 32, -1) == sc.data_ptr()
     for bad in (c[0], c.to(torch.bfloat16)):
