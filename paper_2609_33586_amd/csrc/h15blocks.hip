@@ -696,9 +696,10 @@ __device__ __forceinline__ bool find_work(const BlocksParams& p, int* scratch, W
   int unit, rb;
   place(blockIdx.x, p.B * p.Hkv * p.parts, p.row_blocks, unit, rb);
   int bh = unit / p.parts;
-  // (parts in turn, begun at another one for each cache: the last ones, empty for short
-  // caches, would else be all of one XCD where there are eight)
-  w.part = (unit - bh * p.parts + bh) % p.parts;
+  // (parts in turn, begun at another one for each cache of an XCD, which gets every
+  // (8 / gcd(8, parts))-th: the last ones, empty for short caches, would else be all of
+  // one XCD where there are eight, or of four where there are two)
+  w.part = (unit - bh * p.parts + (bh >> p.turn)) % p.parts;
   w.b = bh / p.Hkv;
   w.h = bh - w.b * p.Hkv;
   if (p.longest) {

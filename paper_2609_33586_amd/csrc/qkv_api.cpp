@@ -160,16 +160,34 @@ int log2_block(int block) {
 // Parts of `keys` keys cut at `split` (0 or >= keys: one part).
 int part_count(int keys, int split) { return split <= 0 || split >= keys ? 1 : (int)ceil_div(keys, split); }
 
+// What a form of attn_decode_blocks takes for `tiles` tiles of keys cut into `parts`, as
+// fitted to its times: the workgroups that one of 256 compute units gets, times the tiles
+// of a part and what starting costs, in tiles of a workgroup of 128 rows that has its
+// compute unit alone (2.6 us at d = 128).  Two of these share one at 0.85 of their time
+// one after the other; of several sequences, whose lengths differ, many fill up as others
+// end.  Of 32 rows two gain little, and more than two wait for each other; of 512 one has
+// a compute unit, and takes a tile in 2.3 times the time.
+double blocks_cost(int rows, long long heads, long long R, double tiles, long long parts, bool ragged) {
+  const double n = (double)ceil_div(heads * ceil_div(R, rows) * parts, 256), part = tiles / (double)parts;
+  if (rows == WROWS) return n * (n == 2 ? 1 : 1.1) * (part + 1) + (parts > 1 ? 2 : 0);
+  if (rows == BLOCKS_WIDE) return n * 2.3 * (part + 6);
+  return n * (n == 1 ? 1 : !ragged ? 0.85 : n < 4 ? 0.82 : 0.72) * (part + 1);
+}
+
 // Query rows of a workgroup, for R rows of a sequence and KV head.  The wide form
-// (exact weights) has one workgroup on a compute unit and takes its rows' keys a
-// third faster once it runs; it pays where each of 256 has 2048 keys to take, of long
-// caches, whose last parts and causal ends weigh little.  Times of a call in 128 /
-// 512 rows, each with its best cut, 8 KV heads, d = 128, R rows: 8192 after 32K keys
-// 1080 / 909 us, 2048 after 16K 161 / 144 (d = 64: 105 / 97); 8192 of 4K 143 / 144, 4 sequences
-// of 512 after 8K 86 / 85; 2048 after 4K 56 / 66, 4 sequences of 2048 of 2K 76 / 94.
-int blocks_rows(long long heads, long long R, int Sk, bool exact) {
-  if (exact && Sk >= 8192 && heads * ceil_div(R, BLOCKS_WIDE) * Sk >= 256LL * 2048 && R >= BLOCKS_WIDE) return BLOCKS_WIDE;
-  return R > 4 * WROWS ? BLOCKS_ROWS : WROWS;
+// (exact weights) takes its rows' keys a third faster, once it runs and if it has them:
+// for long caches, whose causal ends weigh little, by the cost above.  Times of a call in
+// 128 / 512 rows, each with its best cut, 8 KV heads, d = 128, R rows: 8192 after 32K keys
+// 1080 / 890 us, 2048 after 16K 161 / 144 (d = 64: 105 / 97), 1200 of 26K 161 / 161, 4 sequences
+// of 528 rows of up to 26K 249 / 324, of 1000 394 / 339; 8192 of 4K 143 / 144, 2048 after 4K
+// 56 / 66, 4 sequences of 2048 of 2K 76 / 94.
+int blocks_rows(int B, long long heads, long long R, int Sk, long long parts, bool exact) {
+  if (R <= 4 * WROWS) return WROWS;
+  const double tiles = (double)ceil_div(Sk, BC);
+  const bool wide = exact && Sk >= 8192 && R >= BLOCKS_WIDE &&
+                    blocks_cost(BLOCKS_WIDE, heads, R, tiles, parts, B > 1) <
+                        blocks_cost(BLOCKS_ROWS, heads, R, tiles, parts, B > 1);
+  return wide ? BLOCKS_WIDE : BLOCKS_ROWS;
 }
 
 // Workgroups that run at once.
@@ -362,17 +380,26 @@ size_t attn_decode_blocks_workspace_bytes(int B, int Hq, int Sq, int Sk, int d, 
 int attn_decode_blocks_split_keys(int B, int Hq, int Hkv, int Sq, int Sk, int d) {
   (void)d;  // (a cut of one head dimension is one of both)
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || Hq % Hkv != 0) return 0;
-  const long long R = (long long)(Hq / Hkv) * Sq, heads = (long long)B * Hkv;
-  const int rows = blocks_rows(heads, R, Sk, true);
-  const long long groups = heads * ceil_div(R, rows);
-  // two workgroups a compute unit (of the wide form one), parts of eight tiles or more
-  const long long tiles = ceil_div(Sk, BC);
-  long long parts = ceil_div(blocks_slots(rows), groups);
-  // (a workgroup and more for each slot: a third of a long cache each, so that ragged ones
-  // end together; one part / three, lengths from a fourth: 64 sequences of up to 16K keys
-  // and 8 KV heads 294 / 237 us, of 32K 564 / 520, of 8K 138 / 138)
-  if (parts == 1 && rows == WROWS && Sk >= 16384) parts = 3;
-  if (parts > tiles / 8) parts = tiles / 8;
+  const long long R = (long long)(Hq / Hkv) * Sq, heads = (long long)B * Hkv, tiles = ceil_div(Sk, BC);
+  long long parts = 1;
+  const long long groups = heads * ceil_div(R, R > 4 * WROWS ? BLOCKS_ROWS : WROWS);
+  if (R <= 4 * WROWS && groups > 256) {
+    // bound by HBM, whatever the cut: only so many that ragged caches end together (one part /
+    // three / five, d = 128, 8 KV heads: 64 sequences of up to 32K keys 461 / 453 / 442 us, of
+    // 16K 233 / 210 / 206; 45 of 8K 105 / 88 / 86, of 4K 58 / 55 / 56, of 2.2K 34 / 34 / 44; where
+    // others follow the ones that run, few do: 100 of 9K 191 / 201 / 203)
+    parts = tiles >= 128 ? 5 : tiles >= 48 && groups < 512 ? 3 : 1;
+  } else {
+    // the cheapest of all, whose parts have eight tiles or more, and the merge (20
+    // sequences of 8 KV heads, one row, up to 8K keys: 3 parts of 480 workgroups 42 us, 4 of 640 48)
+    const long long most = tiles / 8 < 2048 / groups ? tiles / 8 : 2048 / groups;
+    double best = INFINITY;
+    for (long long n = 1; n <= most || n == 1; ++n) {
+      const int rows = blocks_rows(B, heads, R, Sk, n, true);
+      const double cost = blocks_cost(rows, heads, R, (double)tiles, n, B > 1) + (n > 1 ? 5e-5 * (double)(heads * R * n) : 0);
+      if (cost < best) best = cost, parts = n;
+    }
+  }
   return parts <= 1 ? 0 : (int)(ceil_div(tiles, parts) * BC);
 }
 
@@ -417,7 +444,8 @@ int attn_decode_blocks(const void* q, const void* k, const void* v, const uint8_
   p.parts = part_count(Sk, split_keys);
   // (one part of whole tiles: the cut at its end)
   p.split = p.parts == 1 ? (int)(ceil_div(Sk, BC) * BC) : split_keys;
-  p.rows = blocks_rows((long long)B * Hkv, p.R, Sk, order == 0);
+  p.turn = p.parts % 8 == 0 ? 0 : p.parts % 4 == 0 ? 1 : p.parts % 2 == 0 ? 2 : 3;
+  p.rows = blocks_rows(B, (long long)B * Hkv, p.R, Sk, p.parts, order == 0);
   p.row_blocks = (int)ceil_div(p.R, p.rows);
   const long long groups = (long long)B * Hkv * p.parts * p.row_blocks;
   if (groups > MAX_GROUPS / (p.rows == BLOCKS_WIDE ? 2 : 1) || (p.parts > 1 && rows > MAX_MERGE_ROWS))

@@ -77,6 +77,7 @@ struct BlocksParams {
   int Sk, Sk_cap, causal;
   int blocks, shift;  // blocks of a head's cache, log2 of their keys
   int parts, split;   // parts and their keys
+  int turn;           // log2 of 8 / gcd(8, parts)
   int rows;           // query rows of a workgroup: WROWS, BLOCKS_ROWS or BLOCKS_WIDE
   int row_blocks;     // of a sequence and KV head
   int longest;        // caches are taken in the order of their lengths (B <= 256)

@@ -71,14 +71,14 @@ def test_hundreds_of_rows(d, block, causal):
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("causal", [True, False])
 def test_thousands_of_keys_and_rows(d, causal):
-    # the form of 512 rows (64 caches of 8K keys' room, mostly empty): lengths around a step's and a tile's ends, one
-    # in parts; blocks of rows over several heads' positions and a last one in part
-    lens = [0] * 64
-    for b, n in ((0, 1), (1, 63), (5, 64), (6, 65), (17, 127), (18, 128), (40, 129), (41, 1500), (63, 777)):
+    # the form of 512 rows (many caches with room for thousands of keys, mostly empty): lengths around a step's and a
+    # tile's ends; blocks of rows over two heads' positions and a last one in part; and a cache in two parts
+    lens = [0] * 128
+    for b, n in ((0, 1), (1, 63), (5, 64), (6, 65), (17, 127), (18, 128), (40, 129), (41, 1500), (127, 777)):
         lens[b] = n
-    run_and_check(64, 2, 1, 300, 8192, d, 16, lens, "two heads of 300 positions", EXACT, 0, causal, 40, sharp=False)
-    lens = [700] + [0] * 31
-    run_and_check(32, 1, 1, 520, 16384, d, 128, lens, "520 positions, parts", EXACT, 256, causal, 41, sharp=False)
+    run_and_check(128, 2, 1, 450, 8192, d, 16, lens, "two heads of 450 positions", EXACT, 0, causal, 40, sharp=False)
+    lens = [8300, 700, 8192, 8193] + [0] * 60
+    run_and_check(64, 2, 1, 450, 16384, d, 128, lens, "parts", EXACT, 8192, causal, 41, sharp=False)
 
 
 def test_anchors_of_many_rows():
@@ -87,12 +87,11 @@ def test_anchors_of_many_rows():
     n = 900
     scales.view(torch.uint8)[0, 0, :57, 0] = (110 + torch.arange(57, device="cuda") // 3).to(torch.uint8)
     lens = torch.tensor([n], dtype=torch.int32, device="cuda")
-    for Sk in (n, 175104):  # 128 rows a workgroup, and 512
-        for cut in (0, 256 if Sk == n else 1280):
-            for scale in (scale_of(64), 8.0, 1e-38):
-                o, lse = pkg.attn_decode_blocks(q, k, v, scales, block=16, causal=True, scale=scale, exp_mode=EXACT, split_keys=cut,
-                                                lens=lens, Sk=Sk)
-                check_prefix(o, lse, blocks_ref(q, k, v, scales, 16, [n], True, scale, EXACT, cut), f"Sk {Sk} cut {cut} scale {scale}")
+    for Sk, cut in ((n, 0), (n, 256), (175104, 2176)):  # 128 rows a workgroup, and 512
+        for scale in (scale_of(64), 8.0, 1e-38):
+            o, lse = pkg.attn_decode_blocks(q, k, v, scales, block=16, causal=True, scale=scale, exp_mode=EXACT, split_keys=cut,
+                                            lens=lens, Sk=Sk)
+            check_prefix(o, lse, blocks_ref(q, k, v, scales, 16, [n], True, scale, EXACT, cut), f"Sk {Sk} cut {cut} scale {scale}")
 
 
 def test_no_lens_and_Sk():

@@ -105,19 +105,51 @@ def test_blocks_forms(host):
     assert blocks_form(host, 1, 8, 2, 32, 500)["rows"] == 32 and blocks_form(host, 1, 8, 2, 32, 500)["row_blocks"] == 4
     assert blocks_form(host, 1, 8, 2, 33, 500)["rows"] == 128 and blocks_form(host, 1, 8, 2, 33, 500)["row_blocks"] == 2
     assert blocks_form(host, 1, 8, 2, 33, 500, causal=0)["causal"] == 0
-    # of 512 where each of 256 of them has 2048 keys of long caches, with the exact weights
-    f = blocks_form(host, 1, 32, 8, 512, 16384)
-    assert f["rows"] == 512 and f["row_blocks"] == 4 and f["groups"] == 32
-    assert blocks_form(host, 1, 32, 8, 512, 16384, mode=1)["rows"] == 128
-    assert blocks_form(host, 1, 32, 8, 512, 16383)["rows"] == 128 and blocks_form(host, 1, 32, 8, 2048, 8191)["rows"] == 128
-    assert blocks_form(host, 256, 1, 1, 511, 8192)["rows"] == 128 and blocks_form(host, 256, 1, 1, 512, 8192)["rows"] == 512
-    assert blocks_form(host, 1, 32, 8, 512, 16384, 2048)["groups"] == 256
+    # of 512 where a compute unit's of those take less time than its of 128 rows: of long caches, with the exact weights
+    f = blocks_form(host, 1, 32, 8, 512, 16384, 2048)
+    assert f["rows"] == 512 and f["row_blocks"] == 4 and f["groups"] == 256 and f["parts"] == 8
+    assert blocks_form(host, 1, 32, 8, 512, 16384, 2048, mode=1)["rows"] == 128
+    assert blocks_form(host, 1, 32, 8, 512, 16384)["rows"] == 128  # (32 of 512 rows would leave most units idle)
+    assert [blocks_form(host, 1, 32, 8, 2048, Sk, 4096)["rows"] for Sk in (8191, 8192)] == [128, 512]
+    assert [blocks_form(host, 256, 1, 1, Sq, 8192)["rows"] for Sq in (511, 512)] == [128, 512]
+    assert blocks_form(host, 4, 32, 8, 132, 26354, 3328)["rows"] == 128  # (a last block of 16 rows)
+    # (the calls that tests of this form make)
+    for d in (64, 128):
+        for args in ((128, 2, 1, 450, 8192, 0), (64, 2, 1, 450, 16384, 8192), (1, 2, 1, 600, 175104, 2176)):
+            for causal in (0, 1):
+                assert blocks_form(host, *args, d=d, causal=causal)["rows"] == 512
     # keys that one workgroup reads, 128 MB of them and more: with the hint
     assert blocks_form(host, 16, 32, 8, 1, 4095)["stream"] == 0 and blocks_form(host, 16, 32, 8, 1, 4096)["stream"] == 1
     assert blocks_form(host, 16, 32, 8, 8, 4096)["stream"] == 1 and blocks_form(host, 16, 32, 8, 9, 4096)["stream"] == 0
     assert blocks_form(host, 16, 32, 8, 1, 4096, d=64)["stream"] == 0
     assert blocks_form(host, 64, 32, 8, 1, 500)["longest"] == 0 and blocks_form(host, 65, 32, 8, 1, 500)["longest"] == 1
     assert blocks_form(host, 65, 32, 8, 1, 500, lens=None)["longest"] == 0 and blocks_form(host, 257, 32, 8, 1, 500)["longest"] == 0
+
+
+def test_blocks_cuts(host):
+    def cut(*args):
+        host.attn_decode_blocks_split_keys.argtypes = [ctypes.c_int] * 6
+        keys = host.attn_decode_blocks_split_keys(*args, 128)
+        f = blocks_form(host, *args, keys)
+        assert keys % 128 == 0 and (keys == 0) == (f["parts"] == 1)
+        return f
+
+    for B in (1, 2, 3, 5, 8, 12, 16, 20, 26, 31, 32):
+        for Sk in (100, 1024, 2000, 4096, 9000, 32768, 131072):
+            f = cut(B, 32, 8, 1, Sk)
+            # parts of eight tiles or more, no more workgroups than two on each compute unit but for long caches
+            assert f["parts"] == 1 or f["split"] >= 1024
+            assert f["groups"] <= 512 or Sk > 4096 and f["groups"] <= 2048
+    assert cut(16, 32, 8, 1, 8192)["parts"] == 4 and cut(20, 32, 8, 1, 8192)["parts"] == 3
+    for B, Sk, parts in ((45, 4096, 1), (45, 8192, 3), (64, 8192, 1), (64, 16384, 5), (100, 32768, 5)):
+        assert cut(B, 32, 8, 1, Sk)["parts"] == parts
+    # many rows: no second turn of compute units for a few workgroups
+    for B, Sq, Sk, groups, rows in ((1, 400, 26354, 256, 512), (2, 330, 26354, 240, 512), (1, 2048, 34816, 256, 512),
+                                    (1, 300, 26354, 480, 128)):
+        f = cut(B, 32, 8, Sq, Sk)
+        assert (f["groups"], f["rows"]) == (groups, rows), f
+    host.attn_decode_blocks_split_keys(1, 1, 1, 1, 2 ** 25, 64)  # (ends soon, whatever the sizes)
+    host.attn_decode_blocks_split_keys(2 ** 15, 2 ** 15, 1, 2 ** 15, 2 ** 31 - 1, 64)
 
 
 def test_checks_under_sanitizers(tmp_path):
