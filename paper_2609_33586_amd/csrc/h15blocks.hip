@@ -460,7 +460,7 @@ __device__ __forceinline__ void rows_form(const BlocksParams& p, const Work& w, 
 // the steps to here took more off the cycles than off the time.  Widening a step's
 // codes once for all waves into BF16 rows saved a third of the VALU's work and lost
 // as much to LDS (steps of 32 keys, whose rows LDS has room for: 1033 us; the same
-// with codes in LDS 1004).  One group without the half step between them: 1030.
+// with codes in LDS 1004).  Two workgroups of 256 rows in place of the two groups: 1030.
 template <int D>
 struct WCfg {
   static constexpr int NW = BLOCKS_WIDE / 64;
