@@ -621,11 +621,12 @@ __device__ __forceinline__ void wide_form(const BlocksParams& p, const Work& w, 
         settle_unit(sv[s]);
         mask_unit(sv[s], row_limit(p, w, min(wave * 64 + 32 * s + i32, w.nrows - 1)) - 4 * g - kw0, -INFINITY);
       }
-      // The anchor stays until a weight could pass 2^40 (FP32 and BF16 hold them far
-      // beyond, with the same relative steps): a row's maximum is looked for only
-      // then, as its first step does, whose anchor of -inf gives inf or NaN.
+      // The anchor stays until a step's weights add up to more than 2^10 (FP32 and BF16
+      // hold them with the same relative steps; with 2^40 no less time, but values beyond
+      // 2^80 could overflow): a row's maximum is looked for only then, as its first step
+      // does, whose anchor of -inf gives inf or NaN.
       float e[32], sum = weights(sv[s], e, -m[s] * p.c1, p.c1);
-      if (__builtin_amdgcn_ballot_w64(!(sum <= 0x1p40f)) != 0) {
+      if (__builtin_amdgcn_ballot_w64(!(sum <= 0x1p10f)) != 0) {
         float ma, mb;
         settle_unit(sv[s]);
         with_partner(unit_max(sv[s]), ma, mb);

@@ -94,6 +94,22 @@ def test_anchors_of_many_rows():
             check_prefix(o, lse, blocks_ref(q, k, v, scales, 16, [n], True, scale, EXACT, cut), f"Sk {Sk} cut {cut} scale {scale}")
 
 
+@pytest.mark.parametrize("Sk,cut", [(900, 0), (175104, 2176)])  # 128 rows a workgroup, and 512
+def test_large_values_under_growing_logits(Sk, cut):
+    # logits (base two) that rise by 38 from the first keys to the last, and values of 2^92: neither a row's sums nor what
+    # it holds before its maximum moves may overflow
+    n, d = 900, 64
+    q, (k, v, scales) = normal((1, 2, 600, d), 50), block_cache(1, 1, Sk, d, 64, 51)
+    q[..., 0] = 1.0
+    k.view(torch.uint8)[0, 0, :n] = 0
+    k[0, 0, :n, 0] = (torch.arange(n, device="cuda") / 24).to(FP8)
+    scales.view(torch.uint8)[..., 0], scales.view(torch.uint8)[..., 1] = 127, 127 + 90
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    o, lse = pkg.attn_decode_blocks(q, k, v, scales, block=64, causal=True, scale=math.log(2.0), exp_mode=EXACT, split_keys=cut,
+                                    lens=lens)
+    check_prefix(o, lse, blocks_ref(q, k, v, scales, 64, [n], True, math.log(2.0), EXACT, cut), f"Sk {Sk}")
+
+
 def test_no_lens_and_Sk():
     run_and_check(2, 4, 4, 1, 200, 64, 64, None, "no lens")
     run_and_check(2, 4, 4, 3, 200, 64, 64, None, "Sk", Sk=130)
