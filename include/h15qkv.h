@@ -181,7 +181,8 @@ int attn_cache_append(const void* k, const void* v, void* k_cache, void* v_cache
  * attn_decode (h15attn.h) for BF16 queries over such a cache, with a length
  * for each sequence: Sq query rows per head and sequence attend to the first
  * n = lens[b] (NULL: Sk) slots.  Position i (0 <= i < Sq) sees the keys j <=
- * n - Sq + i when causal (none if that is negative), every key otherwise.  A
+ * n - Sq + i when causal (none if that is negative), every key otherwise: a
+ * sequence with fewer new rows than Sq has them last, after its padding.  A
  * row that sees no key has O = 0 and LSE = -inf.  Sq may be anything from 1
  * up: a decoded token, a few drafted ones, a chunk of a prompt that has been
  * appended before.  A length below 0 counts as 0, one above Sk as Sk; slots
