@@ -11,9 +11,11 @@
 // Three forms of a workgroup (their rules: qkv_api.cpp), the first two, of 4 waves,
 // those of attn_decode_prefix:
 //   keys  32 query rows; each wave takes its own 64 keys of a round, copies them
-//         into its own LDS slots and exchanges only the maxima of its units with
-//         the others (one barrier a round); a weight is rounded relative to the
-//         running maximum at its own tile, the prefix maximum of the round's units;
+//         into its own LDS slots and, for the lattice weights, exchanges the maxima of
+//         its units with the others (one barrier a round), as a weight is rounded
+//         relative to the running maximum at its own tile, the prefix maximum of the
+//         round's units; the exact weights' anchors are each wave's own (20 sequences
+//         of 2.2K keys, one part 20.2 -> 16.4 us, 16 of 8K in 4 parts 36.8 -> 35.8);
 //   rows  128 query rows, 32 a wave; the waves share each tile of 128 keys;
 //   wide  512 query rows, 64 a wave: many rows of long caches.
 #include "qkv_params.h"
@@ -66,6 +68,23 @@ __device__ __forceinline__ void add_pv(f32x16& o0, f32x16& o1, uint32_t a0, uint
     o0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(r[ks][0], r[ks][1], scale[ks]), pb[ks], o0, 0, 0, 0);
     o1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(r[4 + ks][0], r[4 + ks][1], scale[ks]), pb[ks], o1, 0, 0, 0);
   }
+}
+
+// An exact weight's anchor stays until a unit's weights add up to more than this (FP32
+// and BF16 hold them with the same relative steps; with 2^40 no less time, but values
+// beyond 2^80 could overflow): a row's maximum is looked for only then, as its first unit
+// does, whose anchor of -inf gives inf or NaN.
+constexpr float ANCHOR_HOLDS = 0x1p10f;
+
+// 2^(c1 s + nb) of 32 scores, and their sum
+__device__ __forceinline__ float weights(const f32x16 (&s)[2], float (&e)[32], float nb, float c1) {
+  float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j >> 4][j & 15], c1, nb));
+    a[j & 3] = j < 4 ? e[j] : a[j & 3] + e[j];
+  }
+  return (a[0] + a[1]) + (a[2] + a[3]);
 }
 
 // A workgroup's share: query rows of one sequence and KV head against one part
@@ -203,33 +222,50 @@ __device__ __forceinline__ void keys_form(const BlocksParams& p, const Work& w, 
     stage(krsrc, kslot, koff, 3, c + 1);
     settle_unit(sv);
     if (need_mask) mask_unit(sv, lim, -INFINITY);
-    float ma, mb;
-    with_partner(unit_max(sv), ma, mb);
-    if (g == 0) mx_lds[c & 1][i32][wave] = __builtin_fmaxf(ma, mb);
-    // (the two copies of mx_lds alternate: a wave that runs ahead writes the other)
-    lds_barrier();
-    float anchor = m_seen;
-    {
+    bf16x8 pb[2 * NB];
+    float alpha = 1.0f;
+    if constexpr (mode_lattice(MODE)) {
+      float ma, mb;
+      with_partner(unit_max(sv), ma, mb);
+      if (g == 0) mx_lds[c & 1][i32][wave] = __builtin_fmaxf(ma, mb);
+      // (the two copies of mx_lds alternate: a wave that runs ahead writes the other)
+      lds_barrier();
       const f32x4 x = *(const f32x4*)&mx_lds[c & 1][i32][0];
       const float t0 = __builtin_fmaxf(x[0], x[1]), t1 = __builtin_fmaxf(x[2], x[3]);
+      float anchor = __builtin_fmaxf(m_seen, t0);
       m_seen = max3(m_seen, t0, t1);
-      anchor = wt == 0 ? __builtin_fmaxf(anchor, t0) : m_seen;
+      if (wt != 0) anchor = m_seen;
+      // a row that has seen no key yet keeps m = -inf, l = 0, O = 0
+      if (anchor != -INFINITY) alpha = __builtin_amdgcn_exp2f((m_wave - anchor) * p.c1);
+      m_wave = anchor;
+      l_part *= alpha;
+      uint32_t wpk[NB][8];
+      weigh<MODE, NB>(sv, wpk, anchor == -INFINITY ? 0.0f : anchor, p.c1, p.ck, need_mask, lim, l_part);
+#pragma unroll
+      for (int k = 0; k < 2 * NB; ++k) pb[k] = p_operand<MODE>(sv[k >> 1], wpk[k >> 1], k & 1);
+    } else {
+      float e[32], sum = weights(sv, e, -m_wave * p.c1, p.c1);
+      if (__builtin_amdgcn_ballot_w64(!(sum <= ANCHOR_HOLDS)) != 0) {
+        float ma, mb;
+        with_partner(unit_max(sv), ma, mb);
+        const float top = max3(m_wave, ma, mb);
+        if (top != -INFINITY) alpha = __builtin_amdgcn_exp2f((m_wave - top) * p.c1);
+        m_wave = top;
+        l_part *= alpha;
+        sum = weights(sv, e, top == -INFINITY ? 0.0f : -top * p.c1, p.c1);
+      }
+      l_part += sum;
+#pragma unroll
+      for (int k = 0; k < 2 * NB; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) pb[k][j] = (__bf16)e[8 * k + j];
     }
-    // a row that has seen no key yet keeps m = -inf, l = 0, O = 0
-    const float alpha = anchor == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m_wave - anchor) * p.c1);
-    m_wave = anchor;
-    l_part *= alpha;
-    uint32_t wpk[NB][8];
-    weigh<MODE, NB>(sv, wpk, anchor == -INFINITY ? 0.0f : anchor, p.c1, p.ck, need_mask, lim, l_part);
     if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
         for (int j = 0; j < 16; ++j) oacc[db][j] *= alpha;
     }
-    bf16x8 pb[2 * NB];
-#pragma unroll
-    for (int k = 0; k < 2 * NB; ++k) pb[k] = p_operand<MODE>(sv[k >> 1], wpk[k >> 1], k & 1);
     wait_vmcnt<LOADS + NB>();  // V has landed, the next round's scales and K may be outstanding
 #pragma unroll
     for (int db = 0; db < NDB; db += 2) add_pv<D>(oacc[db], oacc[db + 1], vaddr[db], vaddr[db + 1], pb, vs);
@@ -471,17 +507,6 @@ struct WCfg {
   static constexpr int QAREA = BLOCKS_WIDE * QRB;
 };
 
-// 2^(c1 s + nb) of 32 scores, and their sum
-__device__ __forceinline__ float weights(const f32x16 (&s)[2], float (&e)[32], float nb, float c1) {
-  float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j >> 4][j & 15], c1, nb));
-    a[j & 3] = j < 4 ? e[j] : a[j & 3] + e[j];
-  }
-  return (a[0] + a[1]) + (a[2] + a[3]);
-}
-
 template <int D>
 __device__ __forceinline__ void wide_form(const BlocksParams& p, const Work& w, uint8_t* qsm, uint8_t* k0, uint8_t* k1,
                                           uint8_t* v0, uint8_t* v1) {
@@ -621,12 +646,8 @@ __device__ __forceinline__ void wide_form(const BlocksParams& p, const Work& w, 
         settle_unit(sv[s]);
         mask_unit(sv[s], row_limit(p, w, min(wave * 64 + 32 * s + i32, w.nrows - 1)) - 4 * g - kw0, -INFINITY);
       }
-      // The anchor stays until a step's weights add up to more than 2^10 (FP32 and BF16
-      // hold them with the same relative steps; with 2^40 no less time, but values beyond
-      // 2^80 could overflow): a row's maximum is looked for only then, as its first step
-      // does, whose anchor of -inf gives inf or NaN.
       float e[32], sum = weights(sv[s], e, -m[s] * p.c1, p.c1);
-      if (__builtin_amdgcn_ballot_w64(!(sum <= 0x1p10f)) != 0) {
+      if (__builtin_amdgcn_ballot_w64(!(sum <= ANCHOR_HOLDS)) != 0) {
         float ma, mb;
         settle_unit(sv[s]);
         with_partner(unit_max(sv[s]), ma, mb);
