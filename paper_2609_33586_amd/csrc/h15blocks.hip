@@ -16,7 +16,8 @@
 //         relative to the running maximum at its own tile, the prefix maximum of the
 //         round's units; the exact weights' anchors are each wave's own (20 sequences
 //         of 2.2K keys, one part 20.2 -> 16.4 us, 16 of 8K in 4 parts 36.8 -> 35.8);
-//   rows  128 query rows, 32 a wave; the waves share each tile of 128 keys;
+//   rows  128 query rows, 32 a wave; the waves share each tile of 128 keys (exact
+//         weights: anchors that stay as in the others, 528 .. 1200 rows 5 to 8% less);
 //   wide  512 query rows, 64 a wave: many rows of long caches.
 #include "qkv_params.h"
 #include "part_device.h"
@@ -85,6 +86,17 @@ __device__ __forceinline__ float weights(const f32x16 (&s)[2], float (&e)[32], f
     a[j & 3] = j < 4 ? e[j] : a[j & 3] + e[j];
   }
   return (a[0] + a[1]) + (a[2] + a[3]);
+}
+
+// The same as the operands of 64 keys, and their sum
+__device__ __forceinline__ float packed_weights(const f32x16 (&s)[2], bf16x8 (&w)[4], float nb, float c1) {
+  float e[32];
+  const float sum = weights(s, e, nb, c1);
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[k][j] = (__bf16)e[8 * k + j];
+  return sum;
 }
 
 // A workgroup's share: query rows of one sequence and KV head against one part
@@ -347,24 +359,21 @@ __device__ __forceinline__ void rows_form(const BlocksParams& p, const Work& w, 
   const auto krsrc = rows_rsrc(w.k, part_bytes), vrsrc = rows_rsrc(w.v, part_bytes);
   const auto srsrc = rows_rsrc(w.scales, w.used);
   // a wave copies a quarter of each tile: LOADS consecutive KB
-  uint32_t koff[4], voff[2];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = copy_row<C::NCH>(wave * LOADS + i, lane);
-    koff[i] = (r - (wave * LOADS + i) * (64 / C::NCH)) * RB + (((lane % C::NCH) ^ k_swz<DT_FP8, D>(r)) << 4);
+  // (d = 128: eight rows on, both swizzles differ in their third bit)
+  constexpr uint32_t NEXT = D == 128 ? 64 : 0;
+  static_assert(LOADS % 2 == 0, "a wave's first copy is an even one");
+  uint32_t koff, voff;
+  {
+    const int r = copy_row<C::NCH>(wave * LOADS, lane), first = wave * LOADS * (64 / C::NCH);
+    koff = (r - first) * RB + (((lane % C::NCH) ^ k_swz<DT_FP8, D>(r)) << 4);
+    voff = (r - first) * RB + (((lane % C::NCH) ^ v_swz<DT_FP8, D>(r)) << 4);
   }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = copy_row<C::NCH>(wave * LOADS + i, lane);
-    voff[i] = (r - (wave * LOADS + i) * (64 / C::NCH)) * RB + (((lane % C::NCH) ^ v_swz<DT_FP8, D>(r)) << 4);
-  }
-  auto stage = [&](const __amdgpu_buffer_rsrc_t rsrc, uint8_t* area, const uint32_t* off, int mask,
-                   int t) __attribute__((always_inline)) {
+  auto stage = [&](const __amdgpu_buffer_rsrc_t rsrc, uint8_t* area, uint32_t off, int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const uint32_t at = (wave * LOADS + i) * 1024;
       const uint32_t soff = min((uint32_t)t * C::TILE + at, part_bytes);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, LDS_PTR(void, area + at), 16, off[i & mask], soff, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, LDS_PTR(void, area + at), 16, off ^ (NEXT * (i & 1)), soff, 0, 0);
     }
   };
   int pair[NSC];
@@ -383,7 +392,7 @@ __device__ __forceinline__ void rows_form(const BlocksParams& p, const Work& w, 
   const int kswz = k_swz<DT_FP8, D>(i32);
 
   load_scales(0);
-  stage(krsrc, ksm, koff, 3, 0);
+  stage(krsrc, ksm, koff, 0);
 #pragma unroll
   for (int t = 0; t < q.CHUNKS * q.PER; ++t) asm volatile("" : "+v"(q.x[t]));
   const int ntiles = (w.nk + BC - 1) / BC;
@@ -393,7 +402,7 @@ __device__ __forceinline__ void rows_form(const BlocksParams& p, const Work& w, 
     // everyone is done with the last tile's V
     wait_vmcnt<0>();
     lds_barrier();
-    stage(vrsrc, vsm, voff, 1, t);
+    stage(vrsrc, vsm, voff, t);
     const int kw0 = t * BC;
     const bool need_mask = kw0 + BC > w.open || kw0 + BC > w.nk;
     const int lim = limit - kw0 - 4 * g;
@@ -420,8 +429,8 @@ __device__ __forceinline__ void rows_form(const BlocksParams& p, const Work& w, 
     lds_barrier();  // everyone has read K
     load_scales(t + 1);
     __builtin_amdgcn_sched_barrier(0);
-    stage(krsrc, ksm, koff, 3, t + 1);
-    uint32_t wlo[2][8], whi[2][8];
+    stage(krsrc, ksm, koff, t + 1);
+    bf16x8 pb[4], pc[4];
     if (active) {
       settle_unit(lo);
       settle_unit(hi);
@@ -429,16 +438,38 @@ __device__ __forceinline__ void rows_form(const BlocksParams& p, const Work& w, 
         mask_unit(lo, lim, -INFINITY);
         mask_unit(hi, lim - 64, -INFINITY);
       }
-      float ma, mb;
-      with_partner(__builtin_fmaxf(unit_max(lo), unit_max(hi)), ma, mb);
-      // a row that has seen no key yet keeps m = -inf, l = 0, O = 0
-      const float anchor = max3(m, ma, mb);
-      const float alpha = anchor == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - anchor) * p.c1);
-      const float m_use = anchor == -INFINITY ? 0.0f : anchor;
-      m = anchor;
-      l *= alpha;
-      weigh<MODE, 2>(lo, wlo, m_use, p.c1, p.ck, need_mask, lim, l);
-      weigh<MODE, 2>(hi, whi, m_use, p.c1, p.ck, need_mask, lim - 64, l);
+      float alpha = 1.0f;
+      // the row's maximum, a row that has seen no key yet keeping m = -inf, l = 0, O = 0
+      auto move = [&]() __attribute__((always_inline)) {
+        float ma, mb;
+        with_partner(__builtin_fmaxf(unit_max(lo), unit_max(hi)), ma, mb);
+        const float anchor = max3(m, ma, mb);
+        if (anchor != -INFINITY) alpha = __builtin_amdgcn_exp2f((m - anchor) * p.c1);
+        m = anchor;
+        l *= alpha;
+      };
+      if constexpr (mode_lattice(MODE)) {
+        move();
+        const float m_use = m == -INFINITY ? 0.0f : m;
+        uint32_t wlo[2][8], whi[2][8];
+        weigh<MODE, 2>(lo, wlo, m_use, p.c1, p.ck, need_mask, lim, l);
+        weigh<MODE, 2>(hi, whi, m_use, p.c1, p.ck, need_mask, lim - 64, l);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          pb[k] = p_operand<MODE>(lo[k >> 1], wlo[k >> 1], k & 1);
+          pc[k] = p_operand<MODE>(hi[k >> 1], whi[k >> 1], k & 1);
+        }
+      } else {
+        auto all = [&](float nb) __attribute__((always_inline)) {
+          return packed_weights(lo, pb, nb, p.c1) + packed_weights(hi, pc, nb, p.c1);
+        };
+        float sum = all(-m * p.c1);
+        if (__builtin_amdgcn_ballot_w64(!(sum <= ANCHOR_HOLDS)) != 0) {
+          move();
+          sum = all(m == -INFINITY ? 0.0f : -m * p.c1);
+        }
+        l += sum;
+      }
       if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
@@ -449,12 +480,6 @@ __device__ __forceinline__ void rows_form(const BlocksParams& p, const Work& w, 
     wait_vmcnt<LOADS + NSC>();  // V has landed, the next tile's scales and K may be outstanding
     lds_barrier();
     if (active) {
-      bf16x8 pb[4], pc[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        pb[k] = p_operand<MODE>(lo[k >> 1], wlo[k >> 1], k & 1);
-        pc[k] = p_operand<MODE>(hi[k >> 1], whi[k >> 1], k & 1);
-      }
 #pragma unroll
       for (int db = 0; db < NDB; db += 2) {
         add_pv<D>(oacc[db], oacc[db + 1], vaddr[db], vaddr[db + 1], pb, vlo);
@@ -490,8 +515,8 @@ __device__ __forceinline__ void rows_form(const BlocksParams& p, const Work& w, 
 // a barrier after each such half step keeps it so.  A step has 64 keys, so that the
 // query rows, which no registers are left for, are read from LDS once for all of them.
 //
-// What bounds it (8192 rows of 8 KV heads after 32K keys, d = 128: 883 us + 26 of the
-// merge, 1.17 PFLOP/s; the rows form 1080): the clock that the board's power allows
+// What bounds it (8192 rows of 8 KV heads after 32K keys, d = 128: 905 us + 26 of the
+// merge, 1.14 PFLOP/s; the rows form 1059): the clock that the board's power allows
 // (1.94 GHz, with the matrix core busy 56% of the cycles and the VALU 58%): each of
 // the steps to here took more off the cycles than off the time.  Widening a step's
 // codes once for all waves into BF16 rows saved a third of the VALU's work and lost

@@ -163,24 +163,24 @@ int part_count(int keys, int split) { return split <= 0 || split >= keys ? 1 : (
 // What a form of attn_decode_blocks takes for `tiles` tiles of keys cut into `parts`, as
 // fitted to its times: the workgroups that one of 256 compute units gets, times the tiles
 // of a part and what starting costs, in tiles of a workgroup of 128 rows that has its
-// compute unit alone (2.6 us at d = 128).  Two of these share one at 0.85 of their time
+// compute unit alone (2.4 us at d = 128).  Two of these share one at 0.85 of their time
 // one after the other; of several sequences, whose lengths differ, many fill up as others
 // end.  Of 32 rows two gain little, and more than two wait for each other; of 512 one has
-// a compute unit, and takes a tile in 2.3 times the time.
+// a compute unit, and takes a tile in 2.35 times the time.
 double blocks_cost(int rows, long long heads, long long R, double tiles, long long parts, bool ragged) {
   const double n = (double)ceil_div(heads * ceil_div(R, rows) * parts, 256), part = tiles / (double)parts;
   if (rows == WROWS) return n * (n == 2 ? 1 : 1.1) * (part + 1) + (parts > 1 ? 2 : 0);
-  if (rows == BLOCKS_WIDE) return n * 2.3 * (part + 6);
+  if (rows == BLOCKS_WIDE) return n * 2.35 * (part + 6);
   return n * (n == 1 ? 1 : !ragged ? 0.85 : n < 4 ? 0.82 : 0.72) * (part + 1);
 }
 
 // Query rows of a workgroup, for R rows of a sequence and KV head.  The wide form
-// (exact weights) takes its rows' keys a third faster, once it runs and if it has them:
+// (exact weights) takes its rows' keys a fourth faster, once it runs and if it has them:
 // for long caches, whose causal ends weigh little, by the cost above.  Times of a call in
 // 128 / 512 rows, each with its best cut, 8 KV heads, d = 128, R rows: 8192 after 32K keys
-// 1080 / 890 us, 2048 after 16K 161 / 144 (d = 64: 105 / 97), 1200 of 26K 161 / 161, 4 sequences
-// of 528 rows of up to 26K 249 / 324, of 1000 394 / 339; 8192 of 4K 143 / 144, 2048 after 4K
-// 56 / 66, 4 sequences of 2048 of 2K 76 / 94.
+// 1059 / 931 us, 2048 after 16K 152 / 150, 1200 of 26K 154 / 161, 4 sequences of 528 rows of
+// up to 26K 241 / 324, of 1000 379 / 344; 8192 of 4K 136 / 144, 2048 after 4K 54 / 66, 4
+// sequences of 2048 of 2K 71 / 94.
 int blocks_rows(int B, long long heads, long long R, int Sk, long long parts, bool exact) {
   if (R <= 4 * WROWS) return WROWS;
   const double tiles = (double)ceil_div(Sk, BC);
