@@ -165,17 +165,24 @@ int part_count(int keys, int split) { return split <= 0 || split >= keys ? 1 : (
 // of a part and what starting costs, in tiles of a workgroup of 128 rows that has its
 // compute unit alone (2.4 us at d = 128).  Two of these share one at 0.85 of their time
 // one after the other; of several sequences, whose lengths differ, many fill up as others
-// end.  Of 32 rows two gain little, and more than two wait for each other; of 512 one has
-// a compute unit, and takes a tile in 2.35 times the time.
+// end.  Of 512 rows one has a compute unit, and takes a tile in 2.35 times the time.
 double blocks_cost(int rows, long long heads, long long R, double tiles, long long parts, bool ragged) {
   const double n = (double)ceil_div(heads * ceil_div(R, rows) * parts, 256), part = tiles / (double)parts;
-  if (rows == WROWS) return n * (n == 2 ? 1 : 1.1) * (part + 1) + (parts > 1 ? 2 : 0);
   if (rows == BLOCKS_WIDE) return n * 2.35 * (part + 6);
   return n * (n == 1 ? 1 : !ragged ? 0.85 : n < 4 ? 0.82 : 0.72) * (part + 1);
 }
 
+// The same of 32 rows (tiles of 0.7 us at d = 128, 0.4 at 64), the merge included.  Two on
+// a compute unit gain little at d = 128, where a whole cache each ends with the longest,
+// more at 64; more than two wait for each other, and fill up as others end.
+double blocks_cost_keys(long long groups, double tiles, long long parts, int d) {
+  const long long all = groups * parts;
+  const double turns = all > 512 ? 1.15 / 256 * (double)all : all > 256 ? 2.0 : d == 64 ? 1.25 : parts == 1 ? 1.2 : 1.0;
+  return turns * (tiles / (double)parts + 1) + (parts == 1 ? 0 : d == 64 ? 6 : 4);
+}
+
 // Query rows of a workgroup, for R rows of a sequence and KV head.  The wide form
-// (exact weights) takes its rows' keys a fourth faster, once it runs and if it has them:
+// (exact weights) takes a third less time for its rows' keys, once it runs and if it has them:
 // for long caches, whose causal ends weigh little, by the cost above.  Times of a call in
 // 128 / 512 rows, each with its best cut, 8 KV heads, d = 128, R rows: 8192 after 32K keys
 // 1059 / 931 us, 2048 after 16K 152 / 150, 1200 of 26K 154 / 161, 4 sequences of 528 rows of
@@ -378,7 +385,6 @@ size_t attn_decode_blocks_workspace_bytes(int B, int Hq, int Sq, int Sk, int d, 
 }
 
 int attn_decode_blocks_split_keys(int B, int Hq, int Hkv, int Sq, int Sk, int d) {
-  (void)d;  // (a cut of one head dimension is one of both)
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || Hq % Hkv != 0) return 0;
   const long long R = (long long)(Hq / Hkv) * Sq, heads = (long long)B * Hkv, tiles = ceil_div(Sk, BC);
   long long parts = 1;
@@ -390,13 +396,17 @@ int attn_decode_blocks_split_keys(int B, int Hq, int Hkv, int Sq, int Sk, int d)
     // others follow the ones that run, few do: 100 of 9K 191 / 201 / 203)
     parts = tiles >= 128 ? 5 : tiles >= 48 && groups < 512 ? 3 : 1;
   } else {
-    // the cheapest of all, whose parts have eight tiles or more, and the merge (20
-    // sequences of 8 KV heads, one row, up to 8K keys: 3 parts of 480 workgroups 42 us, 4 of 640 48)
-    const long long most = tiles / 8 < 2048 / groups ? tiles / 8 : 2048 / groups;
+    // the cheapest of all, whose parts have eight tiles or more (four of sixteen and more,
+    // where each workgroup has its compute unit), and the merge (8 KV heads, d = 128, one row: 20 sequences of up to
+    // 8K keys in 3 parts, 480 workgroups, 42 us, in 4, 640, 46; 3 of 4K in 4 / 8 parts 12.0 /
+    // 10.3; 16 of 8K in 2 / 4 33.3 / 34.1, of d = 64 22.0 / 20.0)
+    const long long most = tiles / 4 < 2048 / groups ? tiles / 4 : 2048 / groups;
     double best = INFINITY;
     for (long long n = 1; n <= most || n == 1; ++n) {
-      const int rows = blocks_rows(B, heads, R, Sk, n, true);
-      const double cost = blocks_cost(rows, heads, R, (double)tiles, n, B > 1) + (n > 1 ? 5e-5 * (double)(heads * R * n) : 0);
+      if (n > 1 && n > tiles / 8 && (R > 4 * WROWS || groups * n > 256 || tiles < 16)) break;
+      const double cost = R <= 4 * WROWS ? blocks_cost_keys(groups, (double)tiles, n, d)
+                                         : blocks_cost(blocks_rows(B, heads, R, Sk, n, true), heads, R, (double)tiles, n, B > 1) +
+                                               (n > 1 ? 5e-5 * (double)(heads * R * n) : 0);
       if (cost < best) best = cost, parts = n;
     }
   }

@@ -137,10 +137,11 @@ def test_blocks_cuts(host):
     for B in (1, 2, 3, 5, 8, 12, 16, 20, 26, 31, 32):
         for Sk in (100, 1024, 2000, 4096, 9000, 32768, 131072):
             f = cut(B, 32, 8, 1, Sk)
-            # parts of eight tiles or more, no more workgroups than two on each compute unit but for long caches
-            assert f["parts"] == 1 or f["split"] >= 1024
-            assert f["groups"] <= 512 or Sk > 4096 and f["groups"] <= 2048
-    assert cut(16, 32, 8, 1, 8192)["parts"] == 4 and cut(20, 32, 8, 1, 8192)["parts"] == 3
+            # parts of eight tiles or more (four, where each workgroup has its compute unit), no more workgroups than two on
+            # each compute unit but for long caches
+            assert f["parts"] == 1 or f["split"] >= (1024 if f["groups"] > 256 or Sk < 1920 else 512)
+            assert f["groups"] <= 512 or Sk >= 4096 and f["groups"] <= 2048
+    assert cut(16, 32, 8, 1, 8192)["parts"] == 2 and cut(3, 32, 8, 1, 4096)["parts"] == 8 and cut(20, 32, 8, 1, 8192)["parts"] == 3
     for B, Sk, parts in ((45, 4096, 1), (45, 8192, 3), (64, 8192, 1), (64, 16384, 5), (100, 32768, 5)):
         assert cut(B, 32, 8, 1, Sk)["parts"] == parts
     # many rows: no second turn of compute units for a few workgroups
