@@ -158,7 +158,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_kernel(RopeParams p) {
   const Place<D> at(p, t.turned);
   const int token = blockIdx.x * rope_tokens(D) + threadIdx.x / Place<D>::LPR;
   if (token >= p.B * p.S) return;  // (a row's lanes leave together)
-  const int b = token / p.S, s = token - b * p.S, h0 = r * p.run, h1 = min(h0 + p.run, t.heads);
+  const int b = token / p.S, s = token - b * p.S, h0 = r * t.run, h1 = min(h0 + t.run, t.heads);
   const uint16_t* in = t.in + (int64_t)b * t.sb + (int64_t)s * t.ss + (int64_t)h0 * t.sh;
   u32x4 a0 = stream_in(in + at.c0), a1 = stream_in(in + at.c1);
   Turn turn;
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams 
   int r = blockIdx.y;
   const RopeTensor& t = p.t[tensor_of(p, r)];
   const Place<D> at(p, t.turned);
-  const int h0 = r * p.run, h1 = min(h0 + p.run, t.heads);
+  const int h0 = r * t.run, h1 = min(h0 + t.run, t.heads);
   float w[16], dw[16];
   if (t.weight) load_weights(w, t.weight, p.weight_bf16, at.c0, at.c1);
 #pragma unroll

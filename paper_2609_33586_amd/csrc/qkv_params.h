@@ -27,7 +27,8 @@ struct RopeTensor {
   int64_t gb, gs, gh;  // strides of grad
   float inv;           // 1 / descale
   int heads;           // 0: absent
-  int runs;            // runs of `run` heads, each a workgroup's
+  int runs;            // runs of `run` heads or fewer, each a workgroup's
+  int run;             // heads that a thread takes one after the other
   int turned;          // rotated (q and k)
   int partials;        // first of its rows of partial sums in the workspace
 };
@@ -40,7 +41,6 @@ struct RopeParams {
   int each_position, rot, interleaved, weight_bf16;
   float amplitude, eps;
   int B, S, d;
-  int run;     // heads that a thread takes one after the other
   int tiles;   // tiles of rope_tokens(d) positions
   int groups;  // workgroups of a run of heads: each takes every groups-th tile
 };

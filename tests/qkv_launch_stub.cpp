@@ -24,8 +24,8 @@ int launch_blocks(const BlocksParams& p, int, int, void*) { return g_blocks = p,
 extern "C" {
 int h15_stub_qkv_launches(void) { return g_launches; }
 int h15_stub_rope(int what) {
-  const int v[] = {g_rope.tiles, g_rope.run, g_rope.groups, g_rope.t[0].runs, g_rope.t[1].runs, g_rope.t[2].runs,
-                   g_rope.t[0].partials, g_rope.t[1].partials, g_rope.weight_bf16};
+  const int v[] = {g_rope.tiles, g_rope.t[0].run, g_rope.groups, g_rope.t[0].runs, g_rope.t[1].runs, g_rope.t[2].runs,
+                   g_rope.t[0].partials, g_rope.t[1].partials, g_rope.weight_bf16, g_rope.t[1].run, g_rope.t[2].run};
   return v[what];
 }
 int h15_stub_append(int what) {

@@ -46,7 +46,8 @@ def spec(rot=64, wt=0, q=True, k=True):
 
 def rope_form(L, B, S, Hq, Hkv, d):
     assert L.attn_rope(at(0), at(1), at(2), None, spec(), at(3), at(4), at(5), B, S, Hq, Hkv, d, 0, None) == pkg.ATTN_ELAUNCH
-    return {n: L.h15_stub_rope(i) for i, n in enumerate(("tiles", "run", "groups", "q", "k", "v"))}
+    f = {n: L.h15_stub_rope(i) for i, n in enumerate(("tiles", "run", "groups", "q", "k", "v"))}
+    return {**f, "k_run": L.h15_stub_rope(9), "v_run": L.h15_stub_rope(10)}
 
 
 @pytest.mark.parametrize("B,S,Hq,Hkv,d", [(1, 1, 1, 1, 64), (4, 1, 8, 2, 64), (1, 33, 32, 8, 128), (2, 4096, 32, 8, 128), (64, 16384, 64, 8, 64),
@@ -54,7 +55,8 @@ def rope_form(L, B, S, Hq, Hkv, d):
 def test_rope_runs_cover_every_head(host, B, S, Hq, Hkv, d):
     f = rope_form(host, B, S, Hq, Hkv, d)
     assert f["tiles"] == -(-B * S // (4096 // d)) and f["run"] >= 1
-    assert f["q"] == -(-Hq // f["run"]) and f["k"] == f["v"] == -(-Hkv // f["run"])
+    for heads, runs, run in ((Hq, f["q"], f["run"]), (Hkv, f["k"], f["k_run"]), (Hkv, f["v"], f["v_run"])):
+        assert (runs - 1) * run < heads <= runs * run <= heads + runs - 1 and run <= 8  # (as even as they go)
     assert 1 <= f["groups"] <= f["tiles"]
 
 
