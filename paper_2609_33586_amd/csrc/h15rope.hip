@@ -3,11 +3,14 @@
 //
 // A row has d / 16 lanes of 16 channels each, two chunks of 16 bytes, chosen so
 // that a lane has both channels of each of its 8 pairs: chunks l and l + rot / 16
-// of the rotated channels for the half layout, neighbouring chunks for the
-// interleaved one and for the channels that are not rotated.  So a rotation
-// takes no exchange between lanes, and a norm's sum three (d = 128) or two.  A
-// thread keeps its position and takes a run of heads one after the other: the
-// sines and cosines of its 8 pairs are made once for all of them.
+// of the rotated channels for the half layout, l and l + d / 16 of all for the
+// interleaved one (and of the channels that are not rotated, counted on their own).
+// So a rotation takes no exchange between lanes, a norm's sum three (d = 128) or two,
+// and each load of a wave covers whole runs of memory (2 x 4096 positions, interleaved: 35.6
+// us, with neighbouring chunks 43.8; a part of the head in halves, whose runs are mixed,
+// still 42.8).  A thread keeps its position and
+// takes a run of heads one after the other: the sines and cosines of its 8 pairs are made
+// once for all of them.
 //
 // Angles: turns = position * freq / 2 pi in FP64 (off by 2^-53 of it, 2^-23 of a
 // turn at the farthest position), less the nearest whole number, and then the
@@ -16,9 +19,9 @@
 //
 // Everything between the operand and the one rounding of the output is FP32.
 //
-// What bounds it: HBM (2 x 4096 positions, 32 heads over 8, d = 128, norms: 201 MB in 37.5 us,
-// 5.4 TB/s, where a large copy reaches 4.9; its gradient at 4 x 2048 positions: 285 MB in
-// 62 us, 4 of them for the weights' sums), and the launch for a few positions (one of each of 64
+// What bounds it: HBM (2 x 4096 positions, 32 heads over 8, d = 128, norms: 201 MB in 37.4 us,
+// 5.4 TB/s, where a large copy reaches 4.9 to 5.2; its gradient at 4 x 2048 positions: 285 MB in
+// 63 us, 4 of them for the weights' sums), and the launch for a few positions (one of each of 64
 // sequences 4.2 us).  Holding the gradient to 128 registers for a fourth wave on each
 // SIMD costs more than the wave gives (64 us for 55 with inputs in cache).
 #include "qkv_params.h"
@@ -26,53 +29,72 @@
 
 namespace {
 
-// A thread's place: lane l of its row, the channels of its two chunks.
-template <int D>
+// A thread's place: the channels of its two chunks, and its 8 pairs.
+template <int D, bool INTER>
 struct Place {
   static constexpr int LPR = D / 16;
-  int l, c0, c1;
-  bool rotated;
+  int c0, c1;
+  bool r0, r1;  // the first four pairs are rotated, and the others
+  int l;
   __device__ __forceinline__ Place(const RopeParams& p, bool turned) {
+    const int rot = turned ? p.rot : 0;
     l = threadIdx.x % LPR;
-    rotated = turned && 16 * l < p.rot;
-    const bool halves = rotated && !p.interleaved;
-    c0 = halves ? 8 * l : 16 * l;
-    c1 = halves ? p.rot / 2 + 8 * l : 16 * l + 8;
+    if constexpr (INTER) {
+      c0 = 8 * l, c1 = D / 2 + 8 * l;
+      r0 = c0 < rot, r1 = c1 < rot;
+    } else {
+      r0 = r1 = 16 * l < rot;
+      c0 = r0 ? 8 * l : rot / 2 + 8 * l;
+      c1 = r0 ? rot / 2 + 8 * l : D / 2 + 8 * l;
+    }
   }
-};
-
-// Cosines and sines of a lane's pairs 8 l .. 8 l + 7, times the amplitude.
-struct Turn {
-  float c[8], s[8];
-  __device__ __forceinline__ void set(const RopeParams& p, int l, int b, int s_at) {
-    const double at = !p.positions          ? (double)s_at
-                      : p.each_position     ? (double)p.positions[(size_t)b * p.S + s_at]
-                                            : (double)p.positions[b] + (double)s_at;
-    const double turns = at * 0.15915494309189535;
+  // f(j, pair) for the rotated ones
+  template <typename F>
+  __device__ __forceinline__ void rotated_pairs(F f) const {
+    if constexpr (INTER) {
+      if (r0) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      double t = turns * p.freqs[8 * l + j];
-      t -= __builtin_rint(t);
-      c[j] = p.amplitude * __builtin_amdgcn_cosf((float)t);
-      s[j] = p.amplitude * __builtin_amdgcn_sinf((float)t);
+        for (int j = 0; j < 4; ++j) f(j, 4 * l + j);
+      }
+      if (r1) {
+#pragma unroll
+        for (int j = 4; j < 8; ++j) f(j, D / 4 + 4 * l + j - 4);
+      }
+    } else if (r0) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f(j, 8 * l + j);
     }
   }
 };
 
-// A pair's channels among a thread's 16.
-__device__ __forceinline__ constexpr int pair_a(bool inter, int j) { return inter ? 2 * j : j; }
-__device__ __forceinline__ constexpr int pair_b(bool inter, int j) { return inter ? 2 * j + 1 : 8 + j; }
+// Cosines and sines of a thread's pairs, times the amplitude.
+struct Turn {
+  float c[8], s[8];
+  template <typename P>
+  __device__ __forceinline__ void set(const RopeParams& p, const P& at, int b, int s_at) {
+    const double pos = !p.positions      ? (double)s_at
+                       : p.each_position ? (double)p.positions[(size_t)b * p.S + s_at]
+                                         : (double)p.positions[b] + (double)s_at;
+    const double turns = pos * 0.15915494309189535;
+    at.rotated_pairs([&](int j, int pair) __attribute__((always_inline)) {
+      double t = turns * p.freqs[pair];
+      t -= __builtin_rint(t);
+      c[j] = p.amplitude * __builtin_amdgcn_cosf((float)t);
+      s[j] = p.amplitude * __builtin_amdgcn_sinf((float)t);
+    });
+  }
+};
 
-// x turned by the angles (BACK: by their negatives)
-template <bool INTER, bool BACK>
-__device__ __forceinline__ void rotate(float (&x)[16], const Turn& t) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int a = pair_a(INTER, j), b = pair_b(INTER, j);
+// x turned by the angles (BACK: by their negatives).  A pair's channels among a thread's
+// 16: neighbours if interleaved, else the same of both chunks.
+template <bool INTER, bool BACK, typename P>
+__device__ __forceinline__ void rotate(float (&x)[16], const Turn& t, const P& at) {
+  at.rotated_pairs([&](int j, int) __attribute__((always_inline)) {
+    const int a = INTER ? 2 * j : j, b = INTER ? 2 * j + 1 : 8 + j;
     const float xa = x[a], xb = x[b], s = BACK ? -t.s[j] : t.s[j];
     x[a] = __builtin_fmaf(xa, t.c[j], -(xb * s));
     x[b] = __builtin_fmaf(xb, t.c[j], xa * s);
-  }
+  });
 }
 
 __device__ __forceinline__ void widen16(float (&x)[16], u32x4 a, u32x4 b) {
@@ -155,14 +177,14 @@ template <int D, int DT, bool INTER>
 __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_kernel(RopeParams p) {
   int r = blockIdx.y;
   const RopeTensor& t = p.t[tensor_of(p, r)];
-  const Place<D> at(p, t.turned);
-  const int token = blockIdx.x * rope_tokens(D) + threadIdx.x / Place<D>::LPR;
+  const Place<D, INTER> at(p, t.turned);
+  const int token = blockIdx.x * rope_tokens(D) + threadIdx.x / (D / 16);
   if (token >= p.B * p.S) return;  // (a row's lanes leave together)
   const int b = token / p.S, s = token - b * p.S, h0 = r * t.run, h1 = min(h0 + t.run, t.heads);
   const uint16_t* in = t.in + (int64_t)b * t.sb + (int64_t)s * t.ss + (int64_t)h0 * t.sh;
   u32x4 a0 = stream_in(in + at.c0), a1 = stream_in(in + at.c1);
   Turn turn;
-  if (at.rotated) turn.set(p, at.l, b, s);
+  turn.set(p, at, b, s);
   float w[16];
   if (t.weight) load_weights(w, t.weight, p.weight_bf16, at.c0, at.c1);
   size_t o = (((size_t)b * t.heads + h0) * (size_t)p.S + s) * D;
@@ -180,7 +202,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_kernel(RopeParams p) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] = x[i] * f * w[i];
     }
-    if (at.rotated) rotate<INTER, false>(x, turn);
+    rotate<INTER, false>(x, turn, at);
     if constexpr (DT == DT_BF16) {
       uint16_t* out = (uint16_t*)t.out + o;
       *(u32x4*)(out + at.c0) = pack8(x);
@@ -197,11 +219,11 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_kernel(RopeParams p) {
 // part of a weight's gradient is one row of the workspace.
 template <int D, bool INTER>
 __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams p) {
-  constexpr int LPR = Place<D>::LPR, TOKENS = rope_tokens(D);
+  constexpr int LPR = D / 16, TOKENS = rope_tokens(D);
   __shared__ float sums[TOKENS][D + 4];
   int r = blockIdx.y;
   const RopeTensor& t = p.t[tensor_of(p, r)];
-  const Place<D> at(p, t.turned);
+  const Place<D, INTER> at(p, t.turned);
   const int h0 = r * t.run, h1 = min(h0 + t.run, t.heads);
   float w[16], dw[16];
   if (t.weight) load_weights(w, t.weight, p.weight_bf16, at.c0, at.c1);
@@ -218,7 +240,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams 
     u32x4 a0 = stream_in(g + at.c0), a1 = stream_in(g + at.c1), x0, x1;
     if (t.weight) x0 = stream_in(in + at.c0), x1 = stream_in(in + at.c1);
     Turn turn;
-    if (at.rotated) turn.set(p, at.l, b, s);
+    turn.set(p, at, b, s);
 #pragma unroll 1
     for (int h = h0; h < h1; ++h, dx += t.gh) {
       float e[16], u[16];
@@ -234,7 +256,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams 
           x1 = stream_in(in + at.c1);
         }
       }
-      if (at.rotated) rotate<INTER, true>(e, turn);
+      rotate<INTER, true>(e, turn, at);
       if (t.weight) {
         const float f = inverse_rms<D>(u, p.eps);
         float m = 0.0f;
