@@ -7,8 +7,7 @@
 // interleaved one (and of the channels that are not rotated, counted on their own).
 // So a rotation takes no exchange between lanes, a norm's sum three (d = 128) or two,
 // and each load of a wave covers whole runs of memory (2 x 4096 positions, interleaved: 35.6
-// us, with neighbouring chunks 43.8; a part of the head in halves, whose runs are mixed,
-// still 42.8).  A thread keeps its position and
+// us, with neighbouring chunks 43.8).  A thread keeps its position and
 // takes a run of heads one after the other: the sines and cosines of its 8 pairs are made
 // once for all of them.
 //
@@ -166,6 +165,44 @@ __device__ __forceinline__ void load_weights(float (&w)[16], const void* from, b
   }
 }
 
+// A part of a head in halves leaves each load of a wave runs of memory in both lines of a
+// row, at d = 128: then a thread loads and stores chunks l and l + d / 16 like the others, and
+// its row's threads exchange them in LDS (2 x 4096 positions, 32 channels: 42.5 -> 37.5 us,
+// their gradient 66 -> 56.5).  Within a wave, whose LDS instructions are carried out in order.
+template <int D, bool INTER, bool MAY = D == 128 && !INTER>
+struct Exchange {
+  static constexpr int BYTES = MAY ? ROPE_THREADS * 32 : 16;
+  int m0, m1;  // channels of the chunks in memory
+  bool on;
+  u32x4* row;
+  int l, k0, k1;
+  __device__ __forceinline__ Exchange(const Place<D, INTER>& at, bool mixed, uint8_t* lds)
+      : m0(at.c0), m1(at.c1), on(false) {
+    if constexpr (MAY) {
+      on = mixed;
+      if (on) m0 = 8 * at.l, m1 = D / 2 + 8 * at.l;
+      row = (u32x4*)lds + threadIdx.x / (D / 16) * (D / 8);
+      l = at.l, k0 = at.c0 / 8, k1 = at.c1 / 8;
+    }
+  }
+  static __device__ __forceinline__ void pass(u32x4* row, u32x4& a, u32x4& b, int f0, int f1, int t0, int t1) {
+    row[f0] = a, row[f1] = b;
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    a = row[t0], b = row[t1];
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  }
+  __device__ __forceinline__ void own(u32x4& a, u32x4& b) const {
+    if constexpr (MAY)
+      if (on) pass(row, a, b, l, l + D / 16, k0, k1);
+  }
+  __device__ __forceinline__ void memory(u32x4& a, u32x4& b) const {
+    if constexpr (MAY)
+      if (on) pass(row, a, b, k0, k1, l, l + D / 16);
+  }
+};
+
 // Tensor and first head of the run of heads `r`.
 __device__ __forceinline__ int tensor_of(const RopeParams& p, int& r) {
   int i = 0;
@@ -173,16 +210,20 @@ __device__ __forceinline__ int tensor_of(const RopeParams& p, int& r) {
   return i;
 }
 
-template <int D, int DT, bool INTER>
+// MIXED: a part of the head in halves (the branches alone would cost the others 2 us of 37).
+template <int D, int DT, bool INTER, bool MIXED>
 __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_kernel(RopeParams p) {
+  using Ex = Exchange<D, INTER, MIXED>;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[Ex::BYTES];
   int r = blockIdx.y;
   const RopeTensor& t = p.t[tensor_of(p, r)];
   const Place<D, INTER> at(p, t.turned);
+  const Ex ex(at, t.turned, lds);
   const int token = blockIdx.x * rope_tokens(D) + threadIdx.x / (D / 16);
   if (token >= p.B * p.S) return;  // (a row's lanes leave together)
   const int b = token / p.S, s = token - b * p.S, h0 = r * t.run, h1 = min(h0 + t.run, t.heads);
   const uint16_t* in = t.in + (int64_t)b * t.sb + (int64_t)s * t.ss + (int64_t)h0 * t.sh;
-  u32x4 a0 = stream_in(in + at.c0), a1 = stream_in(in + at.c1);
+  u32x4 a0 = stream_in(in + ex.m0), a1 = stream_in(in + ex.m1);
   Turn turn;
   turn.set(p, at, b, s);
   float w[16];
@@ -191,11 +232,12 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_kernel(RopeParams p) {
 #pragma unroll 1
   for (int h = h0; h < h1; ++h, o += (size_t)p.S * D) {
     float x[16];
+    ex.own(a0, a1);
     widen16(x, a0, a1);
     if (h + 1 < h1) {
       in += t.sh;
-      a0 = stream_in(in + at.c0);
-      a1 = stream_in(in + at.c1);
+      a0 = stream_in(in + ex.m0);
+      a1 = stream_in(in + ex.m1);
     }
     if (t.weight) {
       const float f = inverse_rms<D>(x, p.eps);
@@ -205,8 +247,10 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_kernel(RopeParams p) {
     rotate<INTER, false>(x, turn, at);
     if constexpr (DT == DT_BF16) {
       uint16_t* out = (uint16_t*)t.out + o;
-      *(u32x4*)(out + at.c0) = pack8(x);
-      *(u32x4*)(out + at.c1) = pack8(x + 8);
+      u32x4 y0 = pack8(x), y1 = pack8(x + 8);
+      ex.memory(y0, y1);
+      *(u32x4*)(out + ex.m0) = y0;
+      *(u32x4*)(out + ex.m1) = y1;
     } else {
       uint8_t* out = (uint8_t*)t.out + o;
       *(u32x2*)(out + at.c0) = pack8_fp8(x, t.inv);
@@ -221,9 +265,11 @@ template <int D, bool INTER>
 __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams p) {
   constexpr int LPR = D / 16, TOKENS = rope_tokens(D);
   __shared__ float sums[TOKENS][D + 4];
+  __shared__ __attribute__((aligned(16))) uint8_t lds[Exchange<D, INTER>::BYTES];
   int r = blockIdx.y;
   const RopeTensor& t = p.t[tensor_of(p, r)];
   const Place<D, INTER> at(p, t.turned);
+  const Exchange<D, INTER> ex(at, t.turned && p.rot < D, lds);
   const int h0 = r * t.run, h1 = min(h0 + t.run, t.heads);
   float w[16], dw[16];
   if (t.weight) load_weights(w, t.weight, p.weight_bf16, at.c0, at.c1);
@@ -237,23 +283,27 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams 
     const uint16_t* g = (const uint16_t*)t.out + (((size_t)b * t.heads + h0) * (size_t)p.S + s) * D;
     const uint16_t* in = t.in + (int64_t)b * t.sb + (int64_t)s * t.ss + (int64_t)h0 * t.sh;
     uint16_t* dx = t.grad + (int64_t)b * t.gb + (int64_t)s * t.gs + (int64_t)h0 * t.gh;
-    u32x4 a0 = stream_in(g + at.c0), a1 = stream_in(g + at.c1), x0, x1;
-    if (t.weight) x0 = stream_in(in + at.c0), x1 = stream_in(in + at.c1);
+    u32x4 a0 = stream_in(g + ex.m0), a1 = stream_in(g + ex.m1), x0, x1;
+    if (t.weight) x0 = stream_in(in + ex.m0), x1 = stream_in(in + ex.m1);
     Turn turn;
     turn.set(p, at, b, s);
 #pragma unroll 1
     for (int h = h0; h < h1; ++h, dx += t.gh) {
       float e[16], u[16];
+      ex.own(a0, a1);
       widen16(e, a0, a1);
-      if (t.weight) widen16(u, x0, x1);
+      if (t.weight) {
+        ex.own(x0, x1);
+        widen16(u, x0, x1);
+      }
       if (h + 1 < h1) {
         g += (size_t)p.S * D;
-        a0 = stream_in(g + at.c0);
-        a1 = stream_in(g + at.c1);
+        a0 = stream_in(g + ex.m0);
+        a1 = stream_in(g + ex.m1);
         if (t.weight) {
           in += t.sh;
-          x0 = stream_in(in + at.c0);
-          x1 = stream_in(in + at.c1);
+          x0 = stream_in(in + ex.m0);
+          x1 = stream_in(in + ex.m1);
         }
       }
       rotate<INTER, true>(e, turn, at);
@@ -271,8 +321,10 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams 
 #pragma unroll
         for (int i = 0; i < 16; ++i) e[i] = f * __builtin_fmaf(-m, u[i], e[i]);
       }
-      *(u32x4*)(dx + at.c0) = pack8(e);
-      *(u32x4*)(dx + at.c1) = pack8(e + 8);
+      u32x4 y0 = pack8(e), y1 = pack8(e + 8);
+      ex.memory(y0, y1);
+      *(u32x4*)(dx + ex.m0) = y0;
+      *(u32x4*)(dx + ex.m1) = y1;
     }
   }
   if (!t.weight) return;
@@ -328,8 +380,11 @@ __global__ __launch_bounds__(SUM_THREADS) void attn_rope_bwd_sum(RopeParams p) {
 
 template <int D, int DT>
 void launch_forward(const RopeParams& p, dim3 grid, hipStream_t st) {
-  if (p.interleaved) hipLaunchKernelGGL((attn_rope_kernel<D, DT, true>), grid, dim3(ROPE_THREADS), 0, st, p);
-  else hipLaunchKernelGGL((attn_rope_kernel<D, DT, false>), grid, dim3(ROPE_THREADS), 0, st, p);
+  const dim3 block(ROPE_THREADS);
+  const bool mixed = D == 128 && p.rot > 0 && p.rot < D;
+  if (p.interleaved) hipLaunchKernelGGL((attn_rope_kernel<D, DT, true, false>), grid, block, 0, st, p);
+  else if (mixed) hipLaunchKernelGGL((attn_rope_kernel<D, DT, false, D == 128>), grid, block, 0, st, p);
+  else hipLaunchKernelGGL((attn_rope_kernel<D, DT, false, false>), grid, block, 0, st, p);
 }
 
 template <int D>
