@@ -165,43 +165,91 @@ __device__ __forceinline__ void load_weights(float (&w)[16], const void* from, b
   }
 }
 
-// A part of a head in halves leaves each load of a wave runs of memory in both lines of a
-// row, at d = 128: then a thread loads and stores chunks l and l + d / 16 like the others, and
-// its row's threads exchange them in LDS (2 x 4096 positions, 32 channels: 42.5 -> 37.5 us,
-// their gradient 66 -> 56.5).  Within a wave, whose LDS instructions are carried out in order.
-template <int D, bool INTER, bool MAY = D == 128 && !INTER>
-struct Exchange {
-  static constexpr int BYTES = MAY ? ROPE_THREADS * 32 : 16;
-  int m0, m1;  // channels of the chunks in memory
+// Where a thread's two loads and stores of 16 bytes lie.
+//   OWN    its own chunks;
+//   MIXED  chunks l and l + d / 16 of its row, where a part of the head in halves would
+//          leave each load of a wave runs of memory in both lines of a row of 128 channels
+//          (2 x 4096 positions, 32 channels: 42.5 -> 37.5 us, their gradient 66 -> 56.5);
+//   ROWS   a chunk of a row, and the same of the one 8 positions on, where a load of 64
+//          channels' chunks would take half of each row's line (2 x 4096 positions: 24.8 ->
+//          19.7 us, their gradient with norms 36.4 -> 31.6).
+// In the last two a wave's threads exchange them in LDS, whose instructions a wave carries
+// out in order.
+enum { OWN = 0, MIXED = 1, ROWS = 2 };
+
+template <int D, bool INTER, int KIND>
+struct Memory {
+  static constexpr int BYTES = KIND == OWN ? 16 : ROPE_THREADS * 32;
+  int t0, t1, c0, c1;  // tokens (ROWS) and channels
   bool on;
-  u32x4* row;
-  int l, k0, k1;
-  __device__ __forceinline__ Exchange(const Place<D, INTER>& at, bool mixed, uint8_t* lds)
-      : m0(at.c0), m1(at.c1), on(false) {
-    if constexpr (MAY) {
-      on = mixed;
-      if (on) m0 = 8 * at.l, m1 = D / 2 + 8 * at.l;
-      row = (u32x4*)lds + threadIdx.x / (D / 16) * (D / 8);
-      l = at.l, k0 = at.c0 / 8, k1 = at.c1 / 8;
+  u32x4* slots;  // the wave's 128
+  int f0, f1, k0, k1;
+  __device__ __forceinline__ Memory(const Place<D, INTER>& at, bool mixed, uint8_t* lds)
+      : t0(0), t1(0), c0(at.c0), c1(at.c1), on(KIND == ROWS || (KIND == MIXED && mixed)) {
+    if constexpr (KIND != OWN) {
+      const int lane = threadIdx.x & 63;
+      slots = (u32x4*)lds + (threadIdx.x >> 6) * 128;
+      const int row = lane / (D / 16) * (D / 8);
+      k0 = row + at.c0 / 8, k1 = row + at.c1 / 8;
+      if constexpr (KIND == ROWS) {
+        f0 = lane, f1 = lane + 64;
+        t0 = (threadIdx.x >> 6) * 16 + (lane >> 3), t1 = t0 + 8;
+        c0 = c1 = 8 * (lane & 7);
+      } else {
+        f0 = row + at.l, f1 = f0 + D / 16;
+        if (on) c0 = 8 * at.l, c1 = D / 2 + 8 * at.l;
+      }
     }
   }
-  static __device__ __forceinline__ void pass(u32x4* row, u32x4& a, u32x4& b, int f0, int f1, int t0, int t1) {
-    row[f0] = a, row[f1] = b;
+  __device__ __forceinline__ void pass(u32x4& a, u32x4& b, int from0, int from1, int to0, int to1) const {
+    slots[from0] = a, slots[from1] = b;
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
-    a = row[t0], b = row[t1];
+    a = slots[to0], b = slots[to1];
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
   }
+  // what was loaded, into the thread's own chunks; and back
   __device__ __forceinline__ void own(u32x4& a, u32x4& b) const {
-    if constexpr (MAY)
-      if (on) pass(row, a, b, l, l + D / 16, k0, k1);
+    if constexpr (KIND != OWN)
+      if (on) pass(a, b, f0, f1, k0, k1);
   }
-  __device__ __forceinline__ void memory(u32x4& a, u32x4& b) const {
-    if constexpr (MAY)
-      if (on) pass(row, a, b, k0, k1, l, l + D / 16);
+  __device__ __forceinline__ void back(u32x4& a, u32x4& b) const {
+    if constexpr (KIND != OWN)
+      if (on) pass(a, b, k0, k1, f0, f1);
   }
 };
+
+// A thread's tokens of a tile: its own, and those of its loads and stores (beyond the
+// last one: the last, and nothing is stored).
+template <int D, int KIND>
+struct Tokens {
+  int own, m0, m1;
+  bool live, w0, w1;
+  template <typename M>
+  __device__ __forceinline__ Tokens(const M& mem, int tile, int total) {
+    const int first = tile * rope_tokens(D);
+    own = first + threadIdx.x / (D / 16);
+    live = own < total;
+    own = min(own, total - 1);
+    m0 = m1 = own;
+    w0 = w1 = live;
+    if constexpr (KIND == ROWS) {
+      w0 = first + mem.t0 < total, w1 = first + mem.t1 < total;
+      m0 = min(first + mem.t0, total - 1), m1 = min(first + mem.t1, total - 1);
+    }
+  }
+};
+
+// Offsets of a token's row of head h in [B][S][H][d] of the strides and in [B][H][S][d]
+__device__ __forceinline__ int64_t strided(const RopeParams& p, int64_t sb, int64_t ss, int token) {
+  const int b = token / p.S;
+  return (int64_t)b * sb + (int64_t)(token - b * p.S) * ss;
+}
+__device__ __forceinline__ size_t plain(const RopeParams& p, int heads, int h, int D, int token) {
+  const int b = token / p.S;
+  return (((size_t)b * heads + h) * (size_t)p.S + (token - b * p.S)) * D;
+}
 
 // Tensor and first head of the run of heads `r`.
 __device__ __forceinline__ int tensor_of(const RopeParams& p, int& r) {
@@ -210,34 +258,38 @@ __device__ __forceinline__ int tensor_of(const RopeParams& p, int& r) {
   return i;
 }
 
-// MIXED: a part of the head in halves (the branches alone would cost the others 2 us of 37).
-template <int D, int DT, bool INTER, bool MIXED>
+template <int D, int DT, bool INTER, int KIND>
 __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_kernel(RopeParams p) {
-  using Ex = Exchange<D, INTER, MIXED>;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[Ex::BYTES];
+  using Mem = Memory<D, INTER, KIND>;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[Mem::BYTES];
   int r = blockIdx.y;
   const RopeTensor& t = p.t[tensor_of(p, r)];
   const Place<D, INTER> at(p, t.turned);
-  const Ex ex(at, t.turned, lds);
-  const int token = blockIdx.x * rope_tokens(D) + threadIdx.x / (D / 16);
-  if (token >= p.B * p.S) return;  // (a row's lanes leave together)
-  const int b = token / p.S, s = token - b * p.S, h0 = r * t.run, h1 = min(h0 + t.run, t.heads);
-  const uint16_t* in = t.in + (int64_t)b * t.sb + (int64_t)s * t.ss + (int64_t)h0 * t.sh;
-  u32x4 a0 = stream_in(in + ex.m0), a1 = stream_in(in + ex.m1);
+  const Mem mem(at, t.turned, lds);
+  const Tokens<D, KIND> k(mem, blockIdx.x, p.B * p.S);
+  if (KIND != ROWS && !k.live) return;  // (a row's lanes leave together)
+  const int b = k.own / p.S, s = k.own - b * p.S, h0 = r * t.run, h1 = min(h0 + t.run, t.heads);
+  const uint16_t* i0 = t.in + strided(p, t.sb, t.ss, k.m0) + (int64_t)h0 * t.sh + mem.c0;
+  const uint16_t* i1 = i0 + (mem.c1 - mem.c0);
+  if constexpr (KIND == ROWS) i1 = t.in + strided(p, t.sb, t.ss, k.m1) + (int64_t)h0 * t.sh + mem.c1;
+  u32x4 a0 = stream_in(i0), a1 = stream_in(i1);
   Turn turn;
   turn.set(p, at, b, s);
   float w[16];
   if (t.weight) load_weights(w, t.weight, p.weight_bf16, at.c0, at.c1);
-  size_t o = (((size_t)b * t.heads + h0) * (size_t)p.S + s) * D;
+  size_t o = plain(p, t.heads, h0, D, k.own), o0 = o + mem.c0, o1 = o + mem.c1;
+  if constexpr (KIND == ROWS) o0 = plain(p, t.heads, h0, D, k.m0) + mem.c0, o1 = plain(p, t.heads, h0, D, k.m1) + mem.c1;
+  const size_t next = (size_t)p.S * D;
 #pragma unroll 1
-  for (int h = h0; h < h1; ++h, o += (size_t)p.S * D) {
+  for (int h = h0; h < h1; ++h, o += next, o0 += next, o1 += next) {
     float x[16];
-    ex.own(a0, a1);
+    mem.own(a0, a1);
     widen16(x, a0, a1);
     if (h + 1 < h1) {
-      in += t.sh;
-      a0 = stream_in(in + ex.m0);
-      a1 = stream_in(in + ex.m1);
+      i0 += t.sh;
+      i1 += t.sh;
+      a0 = stream_in(i0);
+      a1 = stream_in(i1);
     }
     if (t.weight) {
       const float f = inverse_rms<D>(x, p.eps);
@@ -246,12 +298,12 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_kernel(RopeParams p) {
     }
     rotate<INTER, false>(x, turn, at);
     if constexpr (DT == DT_BF16) {
-      uint16_t* out = (uint16_t*)t.out + o;
+      uint16_t* out = (uint16_t*)t.out;
       u32x4 y0 = pack8(x), y1 = pack8(x + 8);
-      ex.memory(y0, y1);
-      *(u32x4*)(out + ex.m0) = y0;
-      *(u32x4*)(out + ex.m1) = y1;
-    } else {
+      mem.back(y0, y1);
+      if (KIND != ROWS || k.w0) *(u32x4*)(out + o0) = y0;
+      if (KIND != ROWS || k.w1) *(u32x4*)(out + o1) = y1;
+    } else if (KIND != ROWS || k.live) {
       uint8_t* out = (uint8_t*)t.out + o;
       *(u32x2*)(out + at.c0) = pack8_fp8(x, t.inv);
       *(u32x2*)(out + at.c1) = pack8_fp8(x + 8, t.inv);
@@ -261,15 +313,16 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_kernel(RopeParams p) {
 
 // A workgroup takes every groups-th tile of positions for its run of heads; its
 // part of a weight's gradient is one row of the workspace.
-template <int D, bool INTER>
+template <int D, bool INTER, int KIND>
 __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams p) {
+  using Mem = Memory<D, INTER, KIND>;
   constexpr int LPR = D / 16, TOKENS = rope_tokens(D);
   __shared__ float sums[TOKENS][D + 4];
-  __shared__ __attribute__((aligned(16))) uint8_t lds[Exchange<D, INTER>::BYTES];
+  __shared__ __attribute__((aligned(16))) uint8_t lds[Mem::BYTES];
   int r = blockIdx.y;
   const RopeTensor& t = p.t[tensor_of(p, r)];
   const Place<D, INTER> at(p, t.turned);
-  const Exchange<D, INTER> ex(at, t.turned && p.rot < D, lds);
+  const Mem mem(at, t.turned && p.rot < D, lds);
   const int h0 = r * t.run, h1 = min(h0 + t.run, t.heads);
   float w[16], dw[16];
   if (t.weight) load_weights(w, t.weight, p.weight_bf16, at.c0, at.c1);
@@ -277,33 +330,39 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams 
   for (int i = 0; i < 16; ++i) dw[i] = 0.0f;
 #pragma unroll 1
   for (int tile = blockIdx.x; tile < p.tiles; tile += p.groups) {
-    const int token = tile * TOKENS + threadIdx.x / LPR;
-    if (token >= p.B * p.S) break;
-    const int b = token / p.S, s = token - b * p.S;
-    const uint16_t* g = (const uint16_t*)t.out + (((size_t)b * t.heads + h0) * (size_t)p.S + s) * D;
-    const uint16_t* in = t.in + (int64_t)b * t.sb + (int64_t)s * t.ss + (int64_t)h0 * t.sh;
-    uint16_t* dx = t.grad + (int64_t)b * t.gb + (int64_t)s * t.gs + (int64_t)h0 * t.gh;
-    u32x4 a0 = stream_in(g + ex.m0), a1 = stream_in(g + ex.m1), x0, x1;
-    if (t.weight) x0 = stream_in(in + ex.m0), x1 = stream_in(in + ex.m1);
+    const Tokens<D, KIND> k(mem, tile, p.B * p.S);
+    if (KIND != ROWS && !k.live) break;
+    const int b = k.own / p.S, s = k.own - b * p.S;
+    const int64_t far = mem.c1 - mem.c0;
+    const uint16_t* g0 = (const uint16_t*)t.out + plain(p, t.heads, h0, D, k.m0) + mem.c0;
+    const uint16_t* g1 = KIND == ROWS ? (const uint16_t*)t.out + plain(p, t.heads, h0, D, k.m1) + mem.c1 : g0 + far;
+    const uint16_t* i0 = t.in + strided(p, t.sb, t.ss, k.m0) + (int64_t)h0 * t.sh + mem.c0;
+    const uint16_t* i1 = KIND == ROWS ? t.in + strided(p, t.sb, t.ss, k.m1) + (int64_t)h0 * t.sh + mem.c1 : i0 + far;
+    uint16_t* d0 = t.grad + strided(p, t.gb, t.gs, k.m0) + (int64_t)h0 * t.gh + mem.c0;
+    uint16_t* d1 = KIND == ROWS ? t.grad + strided(p, t.gb, t.gs, k.m1) + (int64_t)h0 * t.gh + mem.c1 : d0 + far;
+    u32x4 a0 = stream_in(g0), a1 = stream_in(g1), x0, x1;
+    if (t.weight) x0 = stream_in(i0), x1 = stream_in(i1);
     Turn turn;
     turn.set(p, at, b, s);
 #pragma unroll 1
-    for (int h = h0; h < h1; ++h, dx += t.gh) {
+    for (int h = h0; h < h1; ++h, d0 += t.gh, d1 += t.gh) {
       float e[16], u[16];
-      ex.own(a0, a1);
+      mem.own(a0, a1);
       widen16(e, a0, a1);
       if (t.weight) {
-        ex.own(x0, x1);
+        mem.own(x0, x1);
         widen16(u, x0, x1);
       }
       if (h + 1 < h1) {
-        g += (size_t)p.S * D;
-        a0 = stream_in(g + ex.m0);
-        a1 = stream_in(g + ex.m1);
+        g0 += (size_t)p.S * D;
+        g1 += (size_t)p.S * D;
+        a0 = stream_in(g0);
+        a1 = stream_in(g1);
         if (t.weight) {
-          in += t.sh;
-          x0 = stream_in(in + ex.m0);
-          x1 = stream_in(in + ex.m1);
+          i0 += t.sh;
+          i1 += t.sh;
+          x0 = stream_in(i0);
+          x1 = stream_in(i1);
         }
       }
       rotate<INTER, true>(e, turn, at);
@@ -313,7 +372,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams 
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           u[i] *= f;
-          dw[i] = __builtin_fmaf(e[i], u[i], dw[i]);
+          if (KIND != ROWS || k.live) dw[i] = __builtin_fmaf(e[i], u[i], dw[i]);
           e[i] *= w[i];
           m = __builtin_fmaf(e[i], u[i], m);
         }
@@ -322,9 +381,9 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams 
         for (int i = 0; i < 16; ++i) e[i] = f * __builtin_fmaf(-m, u[i], e[i]);
       }
       u32x4 y0 = pack8(e), y1 = pack8(e + 8);
-      ex.memory(y0, y1);
-      *(u32x4*)(dx + ex.m0) = y0;
-      *(u32x4*)(dx + ex.m1) = y1;
+      mem.back(y0, y1);
+      if (KIND != ROWS || k.w0) *(u32x4*)d0 = y0;
+      if (KIND != ROWS || k.w1) *(u32x4*)d1 = y1;
     }
   }
   if (!t.weight) return;
@@ -381,16 +440,19 @@ __global__ __launch_bounds__(SUM_THREADS) void attn_rope_bwd_sum(RopeParams p) {
 template <int D, int DT>
 void launch_forward(const RopeParams& p, dim3 grid, hipStream_t st) {
   const dim3 block(ROPE_THREADS);
-  const bool mixed = D == 128 && p.rot > 0 && p.rot < D;
-  if (p.interleaved) hipLaunchKernelGGL((attn_rope_kernel<D, DT, true, false>), grid, block, 0, st, p);
-  else if (mixed) hipLaunchKernelGGL((attn_rope_kernel<D, DT, false, D == 128>), grid, block, 0, st, p);
-  else hipLaunchKernelGGL((attn_rope_kernel<D, DT, false, false>), grid, block, 0, st, p);
+  constexpr int DIRECT = D == 64 ? ROWS : OWN, PART = D == 64 ? ROWS : MIXED;
+  const bool part = p.rot > 0 && p.rot < D;
+  // (the exchange's branches alone would cost a whole head in halves 2 us of 37)
+  if (p.interleaved) hipLaunchKernelGGL((attn_rope_kernel<D, DT, true, DIRECT>), grid, block, 0, st, p);
+  else if (part) hipLaunchKernelGGL((attn_rope_kernel<D, DT, false, PART>), grid, block, 0, st, p);
+  else hipLaunchKernelGGL((attn_rope_kernel<D, DT, false, DIRECT>), grid, block, 0, st, p);
 }
 
 template <int D>
 void launch_backward(const RopeParams& p, dim3 grid, hipStream_t st) {
-  if (p.interleaved) hipLaunchKernelGGL((attn_rope_bwd_kernel<D, true>), grid, dim3(ROPE_THREADS), 0, st, p);
-  else hipLaunchKernelGGL((attn_rope_bwd_kernel<D, false>), grid, dim3(ROPE_THREADS), 0, st, p);
+  const dim3 block(ROPE_THREADS);
+  if (p.interleaved) hipLaunchKernelGGL((attn_rope_bwd_kernel<D, true, D == 64 ? ROWS : OWN>), grid, block, 0, st, p);
+  else hipLaunchKernelGGL((attn_rope_bwd_kernel<D, false, D == 64 ? ROWS : MIXED>), grid, block, 0, st, p);
   if (p.t[0].dweight || p.t[1].dweight)
     hipLaunchKernelGGL((attn_rope_bwd_sum<D>), dim3(D / 32, 2), dim3(SUM_THREADS), 0, st, p);
 }

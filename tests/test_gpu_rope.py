@@ -145,6 +145,25 @@ def test_many_heads_and_positions():
     run_and_check(q, k, v, "many", freqs=freqs_of(64)[0], wq=w, wk=w, inter=True)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [BF16, FP8])
+@pytest.mark.parametrize("tokens", [1, 5, 9, 17, 40, 63, 65, 97])
+def test_nothing_behind_the_last_position_is_written(d, dtype, tokens):
+    # (a wave's threads also load and store rows of other positions than their own)
+    q, k, v = projection(1, tokens, 3, 1, d, 14)
+    whole = torch.full((3 * tokens * d + 128 * d,), 7.0, device="cuda").to(dtype)
+    out = whole[:3 * tokens * d].view(1, 3, tokens, d)
+    f, kw = freqs_of(d)[0], dict(out_dtype=dtype) if dtype is FP8 else {}
+    pkg.attn_rope(q, freqs=f, q_out=out, **kw)
+    assert bool((whole[3 * tokens * d:].float() == 7).all())
+    assert torch.equal(out.float(), pkg.attn_rope(q, freqs=f, **kw)[0].float())
+    if dtype is FP8:
+        return
+    g = normal((1, 3, tokens, d), 15)
+    pkg.attn_rope_bwd(g, freqs=f, dq=whole[:3 * tokens * d].view(1, tokens, 3, d))
+    assert bool((whole[3 * tokens * d:].float() == 7).all())
+
+
 def test_other_stream_and_graph():
     q, k, v = projection(2, 50, 4, 2, 128, 13)
     f, pos = freqs_of(128)[0], torch.tensor([3, 400], dtype=torch.int32, device="cuda")
