@@ -144,13 +144,31 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-// 1 / sqrt(mean x^2 + eps)
+// mean x^2 + eps
 template <int D>
-__device__ __forceinline__ float inverse_rms(const float (&x)[16], float eps) {
+__device__ __forceinline__ float mean_square(const float (&x)[16], float eps) {
   float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int i = 0; i < 16; ++i) a[i & 3] = __builtin_fmaf(x[i], x[i], a[i & 3]);
-  return __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<D>((a[0] + a[1]) + (a[2] + a[3])), 1.0f / D, eps));
+  return __builtin_fmaf(row_sum<D>((a[0] + a[1]) + (a[2] + a[3])), 1.0f / D, eps);
+}
+
+// f and `down` with f * down = 1 / sqrt(mean x^2 + eps) and x times `down`, so that x f is
+// the normalised row.  `down` is 1, and 2^-70 for a row whose mean (or eps) leaves FP32: the
+// squares of BF16's largest values add up to less than 2^124 then, and what other channels
+// lose below FP32 is less than BF16's least step, before the weight.  (All lanes of a row see
+// the same mean.)
+template <int D>
+__device__ __forceinline__ float inverse_rms(float (&x)[16], float eps, float& down) {
+  float mean = mean_square<D>(x, eps);
+  down = 1.0f;
+  if (mean == INFINITY) {
+    down = 0x1p-70f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] *= down;
+    mean = mean_square<D>(x, eps * 0x1p-140f);
+  }
+  return __builtin_amdgcn_rsqf(mean);
 }
 
 // A thread's 16 weights.
@@ -292,7 +310,8 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_kernel(RopeParams p) {
       a1 = stream_in(i1);
     }
     if (t.weight) {
-      const float f = inverse_rms<D>(x, p.eps);
+      float down;
+      const float f = inverse_rms<D>(x, p.eps, down);
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] = x[i] * f * w[i];
     }
@@ -367,8 +386,8 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams 
       }
       rotate<INTER, true>(e, turn, at);
       if (t.weight) {
-        const float f = inverse_rms<D>(u, p.eps);
-        float m = 0.0f;
+        float down, m = 0.0f;
+        const float f = inverse_rms<D>(u, p.eps, down);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           u[i] *= f;
@@ -379,6 +398,10 @@ __global__ __launch_bounds__(ROPE_THREADS) void attn_rope_bwd_kernel(RopeParams 
         m = row_sum<D>(m) * (1.0f / D);
 #pragma unroll
         for (int i = 0; i < 16; ++i) e[i] = f * __builtin_fmaf(-m, u[i], e[i]);
+        if (down != 1.0f) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) e[i] *= down;
+        }
       }
       u32x4 y0 = pack8(e), y1 = pack8(e + 8);
       mem.back(y0, y1);

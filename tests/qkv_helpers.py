@@ -33,6 +33,19 @@ def projection(B, S, Hq, Hkv, d, seed):
     return x.to(BF16).split([Hq, Hkv, Hkv], 2)
 
 
+def large_rows(B, S, H, d, seed):
+    """Rows of sizes from 2^50 to the type's largest, ordinary ones among them, one of a single large channel, one whose
+    channels are all the largest value; zeros and channels far below the others in between."""
+    top = torch.finfo(BF16).max
+    x = normal((B, S, H, d), seed, torch.float32).double()
+    e = torch.tensor([0, 50, 61, 64, 66, 90, 100, 126], dtype=torch.float64, device="cuda")
+    x = x * torch.exp2(e[torch.arange(S, device="cuda") % 8])[:, None, None]
+    x[:, 9], x[:, 9, :, 17] = x[:, 9] * 2.0 ** -61, 1e20
+    x[:, 10] = torch.where(x[:, 10] < 0, -top, top)
+    x[:, 11, :, ::3], x[:, 12, :, 1::2] = 0.0, x[:, 12, :, 1::2] * 2.0 ** -90
+    return x.clamp(-top, top).to(BF16)
+
+
 def angles(freqs, positions, B, S):
     """[B, S, 1, rot / 2] in float64."""
     at = torch.arange(S, device=freqs.device, dtype=torch.float64)

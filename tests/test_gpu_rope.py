@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2609_33586_amd as pkg
-from qkv_helpers import BF16, FP8, bf16_tolerance, check, normal, projection, rope_ref, say
+from qkv_helpers import BF16, FP8, bf16_tolerance, check, large_rows, normal, projection, rope_ref, say
 
 pytestmark = pytest.mark.gpu
 
@@ -184,3 +184,23 @@ def test_other_stream_and_graph():
         torch.cuda.synchronize()
         want = pkg.attn_rope(q, k, v, freqs=f, positions=pos)
         assert all(torch.equal(a, b) for a, b in zip(out, want)), step
+
+
+@pytest.mark.parametrize("d,rot,inter", [(64, 64, False), (64, 32, True), (128, 128, False), (128, 32, False), (128, 64, True), (128, 0, False)])
+def test_large_rows_have_their_norm(d, rot, inter):
+    # the squares of values beyond 2^64 leave FP32, those of the largest rows with every factor that keeps small rows in it
+    q, k, w = large_rows(2, 40, 3, d, 30), large_rows(2, 40, 2, d, 31), 1 + 0.3 * normal((d,), 32, torch.float32)
+    f = freqs_of(rot)[0] if rot else None
+    run_and_check(q, k, None, "large", freqs=f, inter=inter, amplitude=1.25, wq=w, wk=w.to(BF16).float())
+    # (an eps that is itself of the size of the squares, and the largest: mean + eps leaves FP32, too)
+    for eps in (2.0 ** 126, torch.finfo(torch.float32).max):
+        run_and_check(q, None, None, f"eps {eps}", freqs=f, inter=inter, wq=w, eps=eps)
+
+
+def test_large_rows_as_fp8():
+    q, w, descale = large_rows(1, 40, 3, 128, 33), 1 + 0.3 * normal((128,), 34, torch.float32), (1 / 64, 1.0, 1.0)
+    got = pkg.attn_rope(q, freqs=freqs_of(128)[0], q_weight=w, descale=descale, out_dtype=FP8)[0]
+    z, tol = rope_ref(q, w, freqs_of(128)[0], None, False, 1.0, 1e-6)
+    z, tol = z * 64, (tol + 2.0 ** -23 * z.abs()) * 64
+    held = z.clamp(-448, 448)
+    check(got.float(), held, 2.0 ** -4 * held.abs() + 2 * tol + 2.0 ** -10, "large rows as fp8")

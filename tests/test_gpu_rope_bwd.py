@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2609_33586_amd as pkg
-from qkv_helpers import BF16, angles, check, grad_ref, inverse_rms, normal, projection, say, turned
+from qkv_helpers import BF16, angles, check, grad_ref, inverse_rms, large_rows, normal, projection, say, turned
 
 pytestmark = pytest.mark.gpu
 
@@ -140,3 +140,20 @@ def test_captured_beside_eager_calls():
     got = pkg.attn_rope_bwd(*g, **kw, stream=side)
     torch.cuda.current_stream().wait_stream(side)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("d,rot,inter", [(64, 64, False), (64, 32, True), (128, 128, False), (128, 32, False), (128, 64, True), (128, 0, False)])
+def test_large_rows_have_their_gradient(d, rot, inter):
+    # (rows whose squares leave FP32: dx is small, the weights' gradient has every row's part)
+    x, g = (large_rows(2, 40, 3, d, 30), large_rows(2, 40, 2, d, 31), None), gradients(2, 40, 3, 2, d, 32)
+    w = 1 + 0.3 * normal((d,), 35, torch.float32)
+    f = pkg.attn_rope_frequencies(rot, device="cuda")[0] if rot else None
+    run_and_check(x, g, "large", freqs=f, inter=inter, amplitude=1.25, wq=w, wk=w)
+    for eps in (2.0 ** 126, torch.finfo(torch.float32).max):
+        run_and_check(x, g, f"eps {eps}", freqs=f, inter=inter, wq=w, wk=w, eps=eps)
+    # gradients large enough that the largest rows' dx are ordinary numbers again
+    g = [(y.float() * 2.0 ** 100).to(BF16) for y in g]
+    dx = pkg.attn_rope_bwd(*g, q=x[0], k=x[1], freqs=f, interleaved=inter, q_weight=w, k_weight=w)
+    for i in range(2):
+        want, tol, _, _ = grad_ref(g[i], x[i], w, f, None, inter, 1.0, 1e-6)
+        check(dx[i], want, tol, f"large gradients {i}")
