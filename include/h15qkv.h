@@ -76,8 +76,8 @@ typedef struct attn_rope_spec {
  * v are taken as they are.  The output is z, rounded once to BF16, or, for
  * dtype ATTN_FP8_E4M3, z * (1 / descale) rounded to e4m3 after it is held to
  * +-448 (descales from opts: what attn_fwd_ex and attn_decode then take).
- * Everything before is in FP32.  A NaN stays one; an infinity in a row with a
- * norm makes the row NaN.
+ * Everything before is in FP32; the squares of a row's values may leave it.  A
+ * NaN stays one, and a NaN or an infinity in a row with a norm makes the row NaN.
  *
  * Layouts: q: [B][S][Hq][d], k, v: [B][S][Hkv][d] bf16, strides of each in
  * strides[0..2] (NULL: contiguous), so that all three may be views of one
@@ -110,8 +110,9 @@ int attn_rope(const void* q, const void* k, const void* v, const attn_strides* s
  *              dx = r (e - u mean(e u))
  *
  * dx is rounded once to BF16; dweight is FP32, each sum in a fixed order, so
- * that results are deterministic.  (FP8 outputs have this same gradient, their
- * rounding and limits left out.)
+ * that results are deterministic.  A NaN or an infinity in a row of q or k with a
+ * norm makes its dx and the weight's gradient NaN.  (FP8 outputs have this same
+ * gradient, their rounding and limits left out.)
  *
  * q, k: attn_rope's inputs, read only where there is a weight (else NULL may
  * be given), with strides[0..1]; dq, dk, dv: laid out as q, k, v, with

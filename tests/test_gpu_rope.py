@@ -204,3 +204,25 @@ def test_large_rows_as_fp8():
     z, tol = z * 64, (tol + 2.0 ** -23 * z.abs()) * 64
     held = z.clamp(-448, 448)
     check(got.float(), held, 2.0 ** -4 * held.abs() + 2 * tol + 2.0 ** -10, "large rows as fp8")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("inter", [False, True])
+def test_an_infinity_makes_a_row_with_a_norm_nan(d, inter):
+    # all of it, in the channels that are rotated and in those that are not, and no other row
+    q, k, v = (x.clone() for x in projection(2, 20, 3, 2, d, 36))
+    f, w = freqs_of(d // 2)[0], 1 + 0.3 * normal((d,), 37, torch.float32)
+    w[3] = 0.0
+    kw = dict(freqs=f, interleaved=inter, q_weight=w, k_weight=w)
+    for out in ({}, dict(out_dtype=FP8, descale=(1 / 32, 1 / 32, 1 / 32))):
+        clean = pkg.attn_rope(q, k, v, **kw, **out)
+        x, y = q.clone(), k.clone()
+        x[0, 3, 0, 5], x[1, 4, 1, d - 1], x[1, 19, 2, 0], x[1, 19, 2, 1] = math.inf, -math.inf, math.inf, -math.inf
+        x[0, 7, 2, ::2], x[0, 7, 2, 9] = 1e38, math.inf
+        y[0, 0, 1, d // 2] = math.inf
+        got = pkg.attn_rope(x, y, v, **kw, **out)
+        for new, old, rows in ((got[0], clean[0], [(0, 0, 3), (1, 1, 4), (1, 2, 19), (0, 2, 7)]), (got[1], clean[1], [(0, 1, 0)])):
+            hit = torch.zeros(new.shape[:3], dtype=torch.bool, device="cuda")
+            for at in rows:
+                hit[at] = True
+            assert bool(new.float()[hit].isnan().all()) and torch.equal(new.float()[~hit], old.float()[~hit])

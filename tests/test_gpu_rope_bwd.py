@@ -1,5 +1,7 @@
 """The gradient of norms and rotation (attn_rope_bwd) against the formula in
 float64, and against differences of attn_rope's own definition."""
+import math
+
 import pytest
 import torch
 
@@ -157,3 +159,17 @@ def test_large_rows_have_their_gradient(d, rot, inter):
     for i in range(2):
         want, tol, _, _ = grad_ref(g[i], x[i], w, f, None, inter, 1.0, 1e-6)
         check(dx[i], want, tol, f"large gradients {i}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_an_infinity_makes_its_row_and_the_weights_gradient_nan(d):
+    x, g = [y.clone() for y in projection(2, 20, 3, 2, d, 36)], gradients(2, 20, 3, 2, d, 37)
+    f, w = pkg.attn_rope_frequencies(d // 2, device="cuda")[0], 1 + 0.3 * normal((d,), 38, torch.float32)
+    clean = pkg.attn_rope_bwd(*g, q=x[0], k=x[1], freqs=f, q_weight=w, k_weight=w)
+    x[0][0, 3, 0, 5], x[0][1, 4, 1, d - 1] = math.inf, -math.inf
+    got = pkg.attn_rope_bwd(*g, q=x[0], k=x[1], freqs=f, q_weight=w, k_weight=w)
+    hit = torch.zeros(2, 20, 3, dtype=torch.bool, device="cuda")
+    hit[0, 3, 0] = hit[1, 4, 1] = True
+    assert bool(got[0][hit].isnan().all()) and torch.equal(got[0][~hit], clean[0][~hit])
+    assert bool(got[3].isnan().all())
+    assert all(torch.equal(got[i], clean[i]) for i in (1, 2, 4))
