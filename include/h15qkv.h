@@ -85,10 +85,11 @@ typedef struct attn_rope_spec {
  * dtype.  Any of q, k, v may be NULL, with its output, not all of them.
  *
  * Errors: ATTN_EINVAL for a null spec or pointer (freqs if rot > 0), one of an
- * input and its output, a size that is not positive (Hq without q, Hkv without
- * k and v: ignored), rot < 0 or > d, an amplitude or descale that is not
- * positive and finite, an eps below 2^-126 or not finite with a weight, or an
- * output that overlaps an input or another output; ATTN_EUNSUPPORTED for d
+ * input and its output, a size that is not positive (Hq without q and Hkv
+ * without k and v may be; such a count still enters the limits below and the
+ * launch's shape, below 0 as 0), rot < 0 or > d, an amplitude or descale that is
+ * not positive and finite, an eps below 2^-126 or not finite with a weight, or
+ * an output that overlaps an input or another output; ATTN_EUNSUPPORTED for d
  * not in {64, 128}, rot not a multiple of 16, an unknown dtype or
  * weight_dtype, a stride that is negative or no multiple of 8, a pointer that
  * is not 16-byte aligned (positions: 4, freqs: 8), more than 2^31 - 1 rows (of
@@ -121,9 +122,10 @@ int attn_rope(const void* q, const void* k, const void* v, const attn_strides* s
  * dk_weight: fp32 [d], written where there is a weight and its gradient gq, gk
  * (required then).
  *
- * workspace: attn_rope_bwd_workspace_bytes() bytes of the same sizes, 16-byte
- * aligned, where a weight's gradient is written; it needs no initialising; two
- * calls in flight at once must not share it.
+ * workspace: attn_rope_bwd_workspace_bytes() bytes of the same sizes (an absent
+ * tensor's heads included, 0 for those below 0), 16-byte aligned, where a
+ * weight's gradient is written; it needs no initialising; two calls in flight at
+ * once must not share it.
  *
  * Errors: as attn_rope; a missing or short workspace: ATTN_EINVAL.  Rows of a
  * gradient that lie over each other by their strides, or in each other's
@@ -135,7 +137,7 @@ int attn_rope_bwd(const void* gq, const void* gk, const void* gv, const void* q,
                   int d, void* workspace, size_t workspace_bytes, const attn_opts* opts);
 
 /* Bytes of workspace attn_rope_bwd needs for weights' gradients (0 for invalid
- * sizes). */
+ * sizes, heads below 0 among them). */
 size_t attn_rope_bwd_workspace_bytes(int B, int S, int Hq, int Hkv, int d);
 
 /* ---- A cache of 8-bit blocks ----------------------------------------------

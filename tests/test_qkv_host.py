@@ -177,3 +177,27 @@ def test_checks_under_sanitizers(tmp_path):
     out = res.stdout + res.stderr
     assert "AddressSanitizer" not in out and "runtime error" not in out, out[-4000:]
     assert res.returncode == 0 and " passed" in out, out[-4000:]
+
+
+@pytest.mark.parametrize("B,S,Hq,Hkv,d", [(1, 1, 1, 1, 64), (4, 2048, 32, 8, 128), (3, 777, 8, 2, 64), (64, 8192, 8, 1, 128)])
+def test_backward_workspace_of_absent_tensors(host, B, S, Hq, Hkv, d):
+    # the heads of an absent tensor count as they are named (below 0: as 0), in the workspace's size and in the call alike
+    def backward(q, k, v, hq, hkv, need, wq=True, wk=True):
+        return host.attn_rope_bwd(at(0) if q else None, at(1) if k else None, at(2) if v else None, at(3), at(4), None, spec(q=wq, k=wk),
+                                  at(5) if q else None, at(6) if k else None, at(7) if v else None, None, at(8), at(9), B, S, hq, hkv, d,
+                                  at(10), need, None)
+
+    for q, k, v, hq, hkv in ((False, True, True, Hq, Hkv), (False, True, False, 0, Hkv), (False, True, False, -1, Hkv), (True, False, True, Hq, Hkv),
+                             (True, False, False, Hq, 0), (True, False, False, Hq, -5), (False, False, True, -1, Hkv)):
+        need = host.attn_rope_bwd_workspace_bytes(B, S, max(hq, 0), max(hkv, 0), d)
+        for wq, wk in ((True, True), (q, k)):  # (a weight whose tensor is absent takes no room)
+            assert backward(q, k, v, hq, hkv, need, wq, wk) == pkg.ATTN_ELAUNCH, (q, k, v, hq, hkv)
+            groups = host.h15_stub_rope(2)
+            ends = [host.h15_stub_rope(6 + i) + host.h15_stub_rope(3 + i) * groups for i, have in enumerate((q, k)) if have]
+            assert max(ends, default=0) * d * 4 <= need
+            assert (host.h15_stub_rope(3) > 0) == q and (host.h15_stub_rope(4) > 0) == k and (host.h15_stub_rope(5) > 0) == v
+            if ends:
+                assert backward(q, k, v, hq, hkv, max(ends) * d * 4 - 1, wq, wk) == pkg.ATTN_EINVAL
+    # and in the limits
+    assert backward(False, True, True, 1 << 30, Hkv, 1 << 40) == pkg.ATTN_EUNSUPPORTED
+    assert backward(True, False, False, Hq, 1 << 30, 1 << 40) == pkg.ATTN_EUNSUPPORTED
