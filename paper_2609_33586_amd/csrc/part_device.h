@@ -114,7 +114,7 @@ __device__ __forceinline__ void place(int L, int units, int blocks, int& unit, i
 }
 
 // The sequence of rank `at` by the length of its cache, the longest first (B <= 256
-// lengths, 256 threads).
+// lengths, 256 threads or more, an int of lens for each).
 __device__ __forceinline__ int longest(const int32_t* of, int B, int Sk, int at, int* lens) {
   const int tid = threadIdx.x;
   const int n = tid < B ? min(max(of[tid], 0), Sk) : -1;

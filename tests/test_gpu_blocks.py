@@ -244,3 +244,24 @@ def test_streams_and_graph():
         want = call()
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1]), step
     say("replayed")
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_more_groups_of_512_rows_than_slots(causal):
+    # ragged caches, mostly empty, two blocks of rows each: the longest first, equal lengths in their own order
+    lens = [0] * 256
+    for b, n in ((0, 1), (1, 64), (2, 700), (3, 700), (100, 65), (128, 1100), (200, 64), (254, 513), (255, 2)):
+        lens[b] = n
+    run_and_check(256, 2, 1, 512, 8192, 64, 16, lens, "512 rows, longest first", EXACT, 0, causal, 60, sharp=False)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("mode", [EXACT, H15, SQ8])
+@pytest.mark.parametrize("cut", [0, 256])
+def test_more_groups_of_128_rows_than_slots(d, mode, cut):
+    # (150 positions of two heads: three blocks of rows, the second over both heads)
+    lens = [0] * 100
+    for b, n in ((0, 3), (7, 400), (8, 400), (33, 128), (64, 257), (98, 129), (99, 390)):
+        lens[b] = n
+    for causal in (True, False):
+        run_and_check(100, 4, 2, 150, 400, d, 32, lens, f"128 rows, longest first, cut {cut}", mode, cut, causal, 61, sharp=False)

@@ -201,3 +201,23 @@ def test_backward_workspace_of_absent_tensors(host, B, S, Hq, Hkv, d):
     # and in the limits
     assert backward(False, True, True, 1 << 30, Hkv, 1 << 40) == pkg.ATTN_EUNSUPPORTED
     assert backward(True, False, False, Hq, 1 << 30, 1 << 40) == pkg.ATTN_EUNSUPPORTED
+
+
+def test_forms_that_take_long_caches_first(host):
+    # (the calls that tests of these make: more workgroups than slots, of sequences with lengths of their own)
+    for causal in (0, 1):
+        f = blocks_form(host, 256, 2, 1, 512, 8192, d=64, block=16, causal=causal)
+        assert (f["rows"], f["row_blocks"], f["groups"], f["longest"]) == (512, 2, 512, 1)
+        for d in (64, 128):
+            for mode in (0, 1, 3):
+                for cut, parts in ((0, 1), (256, 2)):
+                    f = blocks_form(host, 100, 4, 2, 150, 400, cut, d=d, block=32, causal=causal, mode=mode)
+                    assert (f["rows"], f["row_blocks"], f["groups"], f["longest"]) == (128, 3, 600 * parts, 1)
+        for mode in (0, 1):
+            f = blocks_form(host, 4, 4, 2, 2, 65536, 256, block=16, causal=causal, mode=mode)
+            assert f["rows"] == 32 and f["stream"] == 1
+    assert blocks_form(host, 1, 32, 8, 512, 16384, 2048)["rows"] == 512
+    # 256 workgroups of 512 rows and 512 of 128 run at once
+    assert [blocks_form(host, B, 1, 1, 512, 8192, d=64)["longest"] for B in (255, 256)] == [0, 0]
+    assert blocks_form(host, 129, 2, 1, 512, 8192, d=64)["longest"] == 1
+    assert [blocks_form(host, B, 2, 2, 200, 400)["longest"] for B in (128, 129)] == [0, 1]
