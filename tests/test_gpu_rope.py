@@ -226,3 +226,11 @@ def test_an_infinity_makes_a_row_with_a_norm_nan(d, inter):
             for at in rows:
                 hit[at] = True
             assert bool(new.float()[hit].isnan().all()) and torch.equal(new.float()[~hit], old.float()[~hit])
+
+
+def test_the_weight_of_an_absent_tensor_says_nothing():
+    q, k, v = projection(2, 40, 4, 2, 128, 40)
+    f, w, other = freqs_of(64)[0], 1 + 0.3 * normal((128,), 41, torch.float32), torch.full((128,), math.nan, device="cuda")
+    assert torch.equal(pkg.attn_rope(None, k, v, freqs=f, q_weight=other, k_weight=w)[1], pkg.attn_rope(None, k, v, freqs=f, k_weight=w)[1])
+    assert torch.equal(pkg.attn_rope(q, None, v, freqs=f, q_weight=w, k_weight=other)[0], pkg.attn_rope(q, None, v, freqs=f, q_weight=w)[0])
+    assert torch.equal(pkg.attn_rope(None, None, v, freqs=f, q_weight=other, k_weight=other)[2], v.transpose(1, 2))

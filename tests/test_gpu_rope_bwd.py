@@ -173,3 +173,19 @@ def test_an_infinity_makes_its_row_and_the_weights_gradient_nan(d):
     assert bool(got[0][hit].isnan().all()) and torch.equal(got[0][~hit], clean[0][~hit])
     assert bool(got[3].isnan().all())
     assert all(torch.equal(got[i], clean[i]) for i in (1, 2, 4))
+
+
+def test_a_weight_whose_tensor_has_no_gradient_is_not_asked_for():
+    # (its tensor may be given, too: it is not read)
+    x, g = projection(2, 40, 4, 2, 128, 3), gradients(2, 40, 4, 2, 128, 4)
+    f, w, other = pkg.attn_rope_frequencies(128, device="cuda")[0], 1 + 0.3 * normal((128,), 5, torch.float32), torch.full((128,), 7.0, device="cuda")
+    for q in (None, x[0]):
+        run_and_check((q, x[1]), [None, g[1], g[2]], "q's weight without gq", freqs=f, wq=other, wk=w)
+        got = pkg.attn_rope_bwd(None, g[1], g[2], q=q, k=x[1], freqs=f, q_weight=other, k_weight=w)
+        want = pkg.attn_rope_bwd(None, g[1], g[2], k=x[1], freqs=f, k_weight=w)
+        assert got[0] is None and got[3] is None and all(torch.equal(got[i], want[i]) for i in (1, 2, 4))
+    for k in (None, x[1]):
+        run_and_check((x[0], k), [g[0], None, None], "k's weight without gk", freqs=f, wq=w, wk=other)
+        got = pkg.attn_rope_bwd(g[0], None, g[2], q=x[0], k=k, freqs=f, q_weight=w, k_weight=other)
+        want = pkg.attn_rope_bwd(g[0], None, g[2], q=x[0], freqs=f, q_weight=w)
+        assert got[1] is None and got[4] is None and all(torch.equal(got[i], want[i]) for i in (0, 2, 3))
