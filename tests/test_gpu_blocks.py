@@ -265,3 +265,50 @@ def test_more_groups_of_128_rows_than_slots(d, mode, cut):
         lens[b] = n
     for causal in (True, False):
         run_and_check(100, 4, 2, 150, 400, d, 32, lens, f"128 rows, longest first, cut {cut}", mode, cut, causal, 61, sharp=False)
+
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_rows_with_the_finest_lattice(d, causal):
+    for i, (Hq, Hkv, Sq, lens, cut) in enumerate([(4, 2, 9, [300, 5], 0), (4, 2, 65, [300, 40], 0), (3, 1, 200, [390, 200], 0),
+                                                  (2, 2, 300, [300, 0], 128), (5, 1, 40, [399, 1], 256)]):
+        run_and_check(2, Hq, Hkv, Sq, 400, d, [16, 32, 64, 128][i % 4], lens, f"case {i}", SQ8, cut, causal, 70 + i)
+
+
+@pytest.mark.parametrize("form,mode", [("keys, streaming", EXACT), ("keys, streaming", H15), ("512 rows", EXACT), ("512 rows, parts", EXACT)])
+def test_what_lies_behind_is_not_read_by_the_forms_of_long_caches(form, mode):
+    # NaN in every code from lens on and scales of 255 in every block there; lengths inside a block, at its end, at a step's
+    # and a tile's
+    if form == "keys, streaming":
+        B, Hq, Hkv, Sq, cap, d, cut = 4, 4, 2, 2, 65536, 128, 256
+        lens = [700, 0, 1025, 512]
+    elif form == "512 rows":
+        B, Hq, Hkv, Sq, cap, d, cut = 128, 2, 1, 450, 8192, 64, 0
+        lens = [0] * 128
+        lens[0], lens[3], lens[4], lens[70], lens[127] = 1, 100, 128, 577, 1024
+    else:
+        B, Hq, Hkv, Sq, cap, d, cut = 1, 2, 1, 600, 175104, 64, 2176
+        lens = [2176 + 2045]
+    block = 16
+    q, (k, v, scales) = normal((B, Hq, Sq, d), 80), block_cache(B, Hkv, cap, d, block, 81)
+    want = [decode(q, (k, v, scales), block, lens, mode, cut, causal) for causal in (True, False)]
+    for b, n in enumerate(lens):
+        k.view(torch.uint8)[b, :, n:], v.view(torch.uint8)[b, :, n:] = 0x7F, 0xFF
+        scales.view(torch.uint8)[b, :, -(-n // block):] = 255
+    for causal, (o, lse) in zip((True, False), want):
+        got = decode(q, (k, v, scales), block, lens, mode, cut, causal)
+        assert bool(torch.isfinite(got[0].float()).all()) and torch.equal(got[0], o) and torch.equal(got[1], lse)
+
+
+@pytest.mark.parametrize("mode", [EXACT, H15])
+@pytest.mark.parametrize("B,Hq,Hkv,Sq,cap,cut", [(20, 8, 2, 1, 3000, 0), (3, 8, 2, 1, 3000, 256), (4, 8, 2, 40, 1500, 256), (1, 32, 8, 512, 16384, 2048)])
+def test_repeats_itself(B, Hq, Hkv, Sq, cap, cut, mode):
+    # no order of workgroups, waves or parts shows in what comes out
+    q, cache = normal((B, Hq, Sq, 128), 90), block_cache(B, Hkv, cap, 128, 64, 91, True)
+    lens = [cap - 37 * b for b in range(B)]
+    want = decode(q, cache, 64, lens, mode, cut)
+    for _ in range(5):
+        torch.empty_like(want[0]).fill_(1)  # (other work in between)
+        got = decode(q, cache, 64, lens, mode, cut)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
