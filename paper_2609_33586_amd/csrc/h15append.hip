@@ -1,19 +1,21 @@
 // Writing new rows of K and V into a cache of 8-bit codes with a scale of two for
 // each block of tokens and head (attn_cache_append).
 //
-// One, two or four waves for each block that n rows can lie in, each head, and K or
-// V, so that a thread has two to eight chunks of 16 bytes: they read the new rows
-// once, into registers, find their largest finite value, take the larger of the
+// A workgroup for each block that n rows can lie in, each head, and K or V, of one, two or
+// four waves, so that a thread has two to eight chunks of 16 bytes: it reads the new rows
+// once, into registers, finds their largest finite value, takes the larger of the
 // scale that this needs and the one that the block has (if it held rows before), and
-// write the codes.  Only where the scale grows are the rows that were there read,
+// writes the codes.  Only where the scale grows are the rows that were there read,
 // shrunk by a power of two and written back.  Division by a scale of two is exact,
 // so a code is rounded once.
 //
-// What bounds it: HBM for many rows (4 sequences of 8 heads, 4096 rows each, blocks of
-// 16, d = 128: 101 MB in 19.8 us; with four waves for each block, whatever its size,
-// 23.9; blocks of 64 with one wave 14.0 us for 40 MB, with two 13.3, with four 12.5),
-// the launch and three loads in turn (length, scale, rows) for few: one row of each of
-// 16 sequences of 8 heads 4.5 us.
+// What bounds it: HBM for many rows (4 sequences of 8 heads, 4096 rows each, d = 128: 101 MB in
+// 19.3 to 20 us for every block; blocks of 16 with four waves 24.4), and for few the launch and a
+// chain of loads, each of which needs the one before: the arguments, a count and a length, K's
+// or V's pointers, the scale of a block that held rows, the rows (one row of each of 16
+// sequences of 8 heads 4.3 us).  Up to 4096 ragged rows, 40 MB: blocks of 16, 32 and 64 in 10.9,
+// 11.0 and 11.0 us; with workgroups of four waves for several blocks, whose indexes differ from
+// wave to wave and whose waves stay where a block gets no row, in 14.3, 14.3 and 11.6.
 //
 // The largest value is found on the bits of the BF16 values: without the sign
 // they order as the values do, and the scale's exponent byte follows from them
@@ -23,7 +25,6 @@
 
 namespace {
 
-constexpr int THREADS = 256;
 // Waves that share a block of T rows of D channels.
 constexpr int block_waves(int D, int T) { return T * D <= 2048 ? 1 : T * D <= 4096 ? 2 : 4; }
 
@@ -37,15 +38,13 @@ __device__ __forceinline__ uint32_t finite_max(uint32_t top, uint32_t x) {
 }
 
 template <int D, int T>
-__global__ __launch_bounds__(THREADS) void attn_append_kernel(AppendParams p, bool write_lens) {
+__global__ __launch_bounds__(64 * block_waves(D, T)) void attn_append_kernel(AppendParams p, bool write_lens) {
   constexpr int CH = D / 8;               // chunks of 8 channels in a row
-  constexpr int W = block_waves(D, T), N = 64 * W, EACH = T * CH / N;  // waves and threads of a block, a thread's chunks
+  constexpr int W = block_waves(D, T), N = 64 * W, EACH = T * CH / N;  // waves, threads, a thread's chunks
   static_assert(T * CH % N == 0, "whole chunks");
-  __shared__ uint32_t tops[THREADS / 64];
-  const int wave = threadIdx.x >> 6, tid = threadIdx.x % N;
-  const int work = blockIdx.x * (THREADS / N) + wave / W;
-  // (the last workgroup's waves without a block go with the last one's, and do nothing)
-  const int unit = min(work / p.reach, p.B * p.Hkv * 2 - 1), j = work - unit * p.reach;  // unit: (b, h, K or V)
+  __shared__ uint32_t tops[W];
+  const int tid = threadIdx.x;
+  const int unit = blockIdx.x / p.reach, j = blockIdx.x - unit * p.reach;  // unit: (b, h, K or V)
   const int which = unit & 1, bh = unit >> 1, b = bh / p.Hkv;
   const int held_rows = min(max(p.lens[b], 0), p.cap);
   const int fresh = min(p.counts ? min(max(p.counts[b], 0), p.n) : p.n, p.cap - held_rows);
@@ -54,12 +53,11 @@ __global__ __launch_bounds__(THREADS) void attn_append_kernel(AppendParams p, bo
   const int block = held_rows / T + j;
   const long long first = (long long)block * T;
   const int lo = (int)max(first, (long long)held_rows), hi = (int)min(first + T, (long long)end);
-  const bool live = j < p.reach && lo < hi;
-  if (W == THREADS / 64 && !live) return;  // (the whole workgroup)
+  if (lo >= hi) return;
   const uint16_t* x = p.x[which] + ((size_t)bh * p.n + (lo - held_rows)) * D;
   uint8_t* const cache = p.cache[which] + ((size_t)bh * p.cap + (size_t)first) * D;
   uint8_t* const scale = p.scales + ((size_t)bh * p.blocks + block) * 2 + which;
-  const int chunks = live ? (hi - lo) * CH : 0, old_rows = live ? lo - (int)first : 0;
+  const int chunks = (hi - lo) * CH, old_rows = lo - (int)first;
   int e_old = 1;
   if (old_rows > 0) e_old = min(max((int)*scale, 1), 254);
   u32x4 v[EACH];
@@ -76,12 +74,11 @@ __global__ __launch_bounds__(THREADS) void attn_append_kernel(AppendParams p, bo
 #pragma unroll
   for (int y = 32; y >= 1; y >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, y, 64));
   if constexpr (W > 1) {
-    if ((threadIdx.x & 63) == 0) tops[wave] = top;
+    if ((tid & 63) == 0) tops[tid >> 6] = top;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < W; ++i) top = max(top, tops[wave / W * W + i]);
+    for (int i = 0; i < W; ++i) top = max(top, tops[i]);
   }
-  if (!live) return;
   // the exponent of top / 448, one up where top's fraction lies above 448's
   const int need = (int)((top + (0x7Fu - 0x60u)) >> 7) - 8;
   const int e = max(need, e_old);
@@ -129,13 +126,13 @@ __global__ __launch_bounds__(256) void attn_append_lens(AppendParams p) {
 
 template <int D>
 void launch_one(const AppendParams& p, int block, bool write_lens, hipStream_t st) {
-  const int per = THREADS / (64 * block_waves(D, block));  // blocks of a workgroup
-  const dim3 grid((unsigned)(((long long)p.B * p.Hkv * 2 * p.reach + per - 1) / per));
+  const dim3 threads(64 * block_waves(D, block));
+  const dim3 grid((unsigned)((long long)p.B * p.Hkv * 2 * p.reach));
   switch (block) {
-    case 16: hipLaunchKernelGGL((attn_append_kernel<D, 16>), grid, dim3(THREADS), 0, st, p, write_lens); break;
-    case 32: hipLaunchKernelGGL((attn_append_kernel<D, 32>), grid, dim3(THREADS), 0, st, p, write_lens); break;
-    case 64: hipLaunchKernelGGL((attn_append_kernel<D, 64>), grid, dim3(THREADS), 0, st, p, write_lens); break;
-    default: hipLaunchKernelGGL((attn_append_kernel<D, 128>), grid, dim3(THREADS), 0, st, p, write_lens); break;
+    case 16: hipLaunchKernelGGL((attn_append_kernel<D, 16>), grid, threads, 0, st, p, write_lens); break;
+    case 32: hipLaunchKernelGGL((attn_append_kernel<D, 32>), grid, threads, 0, st, p, write_lens); break;
+    case 64: hipLaunchKernelGGL((attn_append_kernel<D, 64>), grid, threads, 0, st, p, write_lens); break;
+    default: hipLaunchKernelGGL((attn_append_kernel<D, 128>), grid, threads, 0, st, p, write_lens); break;
   }
 }
 }  // namespace
