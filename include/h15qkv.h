@@ -164,7 +164,9 @@ size_t attn_rope_bwd_workspace_bytes(int B, int S, int Hq, int Hkv, int d);
  * else is left as it was.  lens: int32 [B]; lens_out[b] = lens[b] + c, and may
  * be lens itself.  A length below 0 counts as 0, one above cap as cap, a count
  * below 0 as 0, one above n as n; rows that would lie beyond cap are dropped,
- * and lens_out is cap.
+ * and lens_out is cap.  So a padded batch has a sequence's rows first, its padding
+ * last; attn_decode_blocks, whose Sq rows end with a sequence's last key, takes
+ * them the other way round (see there).
  *
  * Layouts: k, v: [B][Hkv][n][d] bf16.  block: 16, 32, 64 or 128.
  *
@@ -185,12 +187,19 @@ int attn_cache_append(const void* k, const void* v, void* k_cache, void* v_cache
  * for each sequence: Sq query rows per head and sequence attend to the first
  * n = lens[b] (NULL: Sk) slots.  Position i (0 <= i < Sq) sees the keys j <=
  * n - Sq + i when causal (none if that is negative), every key otherwise: a
- * sequence with fewer new rows than Sq has them last, after its padding.  A
- * row that sees no key has O = 0 and LSE = -inf.  Sq may be anything from 1
+ * sequence with c new rows, fewer than Sq, has them last, after its padding.  The
+ * queries of a batch that attn_cache_append took with counts have them first:
+ * handed on as they are, each row's mask would be off by Sq - c keys, which no
+ * check can see.  They are moved behind the padding before the call, or each
+ * sequence has a call of its own, with Sq = c.
+ *
+ * A row that sees no key has O = 0 and LSE = -inf.  Sq may be anything from 1
  * up: a decoded token, a few drafted ones, a chunk of a prompt that has been
  * appended before.  A length below 0 counts as 0, one above Sk as Sk; slots
  * from lens[b] on, and scales of blocks without a slot below it, are never
- * read.
+ * read.  The kernel's form, attn_decode_blocks_split_keys' cut and the workspace
+ * go by Sk, as lens is not on the host: the least bound of lens that is known
+ * there serves best.
  *
  * Parts of split_keys keys, their weights by exp_mode (ATTN_EXP_EXACT, H15, SQ4
  * or SQ8; for the lattice weights the cut is part of the result) and their

@@ -194,7 +194,8 @@ def attn_rope(q, k=None, v=None, *, freqs=None, positions=None, interleaved: boo
     q_weight, k_weight: [d] bf16 or fp32 (None: no norm).  Returns (q_out
     [B,Hq,S,d], k_out, v_out [B,Hkv,S,d]): the given tensors, or new ones of
     out_dtype (bfloat16, the default, or float8_e4m3fn with descale = (q, k, v)
-    factors, as attn_fwd_ex takes them)."""
+    factors, as attn_fwd_ex takes them).  torch records nothing of the call, as
+    of the package's others: attn_rope_bwd is its gradient."""
     L = _lib()
     first = q if q is not None else k if k is not None else v
     if first is None:
@@ -370,8 +371,10 @@ def attn_cache_append(k, v, k_cache, v_cache, scales, lens, *, block: int, count
     k, v: [B,Hkv,n,d] bf16; k_cache, v_cache: [B,Hkv,cap,d] float8_e4m3fn and
     scales: [B,Hkv,ceil(cap / block),2] float8_e8m0fnu (K's, V's), updated in
     place; lens: int32 [B], the slots filled before; counts: int32 [B], the new
-    rows of each sequence (default n).  Returns lens_out, int32 [B], the slots
-    filled after: the given tensor, which may be lens, or a new one."""
+    rows of each sequence, its first of the n (default n).  Returns lens_out,
+    int32 [B], the slots filled after: the given tensor, which may be lens, or a
+    new one.  attn_decode_blocks takes a padded batch's queries the other way
+    round, behind their padding."""
     L = _lib()
     B, Hkv, n, d = shape = _bf16_rows("k", k)
     dev = _current_gpu("k", k, stream)
@@ -408,7 +411,11 @@ def attn_decode_blocks(q, k, v, scales, *, block: int, causal: bool, scale: floa
     q: [B,Hq,Sq,d] bf16; k, v: [B,Hkv,Sk_cap,d] float8_e4m3fn and scales:
     [B,Hkv,ceil(Sk_cap / block),2] float8_e8m0fnu, as attn_cache_append writes
     them, whose first lens[b] slots (int32 [B]; default Sk, default all) are
-    filled.  Returns (O [B,Hq,Sq,d] bf16, LSE [B,Hq,Sq] fp32 or None)."""
+    filled.  When causal, a sequence's last query row sees its last key: of a
+    batch appended with counts, a sequence's c = counts[b] queries are moved to
+    its last c rows before (there the padding comes first), or it has a call of
+    its own with Sq = c.  Returns (O [B,Hq,Sq,d] bf16, LSE [B,Hq,Sq] fp32 or
+    None)."""
     L = _lib()
     B, Hq, Sq, d = shape = _bf16_rows("q", q)
     dev = _current_gpu("q", q, stream)

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2609_33586_amd as pkg
-from qkv_helpers import (BF16, E8M0, EXACT, FP8, H15, append_ref, bf16_tolerance, blocks_ref, check, check_prefix, normal,
+from qkv_helpers import (BF16, E8M0, EXACT, FP8, H15, append_ref, bf16_tolerance, block_cache, blocks_ref, check, check_prefix, normal,
                          projection, rope_ref, say, scale_of)
 
 pytestmark = pytest.mark.gpu
@@ -90,3 +90,31 @@ def test_training_step():
         err = ((got.double() - ref).norm() / ref.norm()).item()
         say(f"{what}: {err:.2e}")
         assert err <= 2.0 ** -9 * 10, what
+
+
+@pytest.mark.parametrize("mode", [EXACT, H15])
+@pytest.mark.parametrize("S", [7, 70])
+def test_padded_batch_with_its_rows_moved_behind_the_padding(mode, S):
+    # attn_cache_append takes a sequence's rows before its padding, attn_decode_blocks after it: moved there, a padded batch's
+    # queries go through one call
+    B, Hq, Hkv, d, block, cap = 4, 8, 2, 128, 16, 256
+    counts, n = [S, 1, 0, S // 2], [3, 40, 17, 0]
+    f = pkg.attn_rope_frequencies(d, device="cuda")[0]
+    k0, v0, scales = block_cache(B, Hkv, cap, d, block, 70)
+    lens, ct = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (n, counts))
+    q, k, v = pkg.attn_rope(*projection(B, S, Hq, Hkv, d, 71), freqs=f, positions=lens)
+    after = pkg.attn_cache_append(k, v, k0, v0, scales, lens, block=block, counts=ct)
+    ends = [a + c for a, c in zip(n, counts)]
+    assert after.tolist() == ends
+    # row i of the batch's first counts[b] goes to S - counts[b] + i, padding to the rows before
+    at = (torch.arange(S, device="cuda") + ct[:, None]) % S
+    moved = q.gather(2, at[:, None, :, None].expand_as(q))
+    o, lse = pkg.attn_decode_blocks(moved, k0, v0, scales, block=block, lens=after, causal=True, scale=scale_of(d), exp_mode=mode, split_keys=0)
+    for b in range(B):
+        if not counts[b]:
+            continue
+        rows = slice(S - counts[b], S)
+        one = slice(b, b + 1)
+        assert torch.equal(moved[b, :, rows], q[b, :, :counts[b]])
+        ref = blocks_ref(q[one, :, :counts[b]], k0[one], v0[one], scales[one], block, [ends[b]], True, scale_of(d), mode, 0)
+        check_prefix(o[one, :, rows], lse[one, :, rows], ref, f"b {b}")
