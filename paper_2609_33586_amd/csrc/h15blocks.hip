@@ -8,6 +8,11 @@
 // inner loops.  K's rows meet them one scale a lane, V's transposed operands one
 // for each 16 keys, which never straddle a block.
 //
+// The exact weights go to the matrix core as BF16, its operand type beside V's BF16 (their
+// sum stays FP32): O is off by 1.9e-3 to 2.3e-3 of its norm, where its own rounding
+// alone gives 1.7e-3, which the lattice weights, exact in BF16, have.  Two BF16 terms of a weight
+// would double the products of P V.
+//
 // Three forms of a workgroup (their rules: qkv_api.cpp), the first two, of 4 waves,
 // those of attn_decode_prefix:
 //   keys  32 query rows; each wave takes its own 64 keys of a round, copies them
@@ -522,6 +527,8 @@ __device__ __forceinline__ void rows_form(const BlocksParams& p, const Work& w, 
 // codes once for all waves into BF16 rows saved a third of the VALU's work and lost
 // as much to LDS (steps of 32 keys, whose rows LDS has room for: 1033 us; the same
 // with codes in LDS 1004).  Two workgroups of 256 rows in place of the two groups: 1030.
+// At d = 128 all 256 registers are taken and 4 spilled; one of them is loaded again, in
+// steps with masked keys.
 template <int D>
 struct WCfg {
   static constexpr int NW = BLOCKS_WIDE / 64;
