@@ -167,7 +167,8 @@ __device__ __forceinline__ float inverse_rms(float (&x)[16], float eps, float& d
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] *= down;
     mean = mean_square<D>(x, eps * 0x1p-140f);
-    if (mean == INFINITY) mean = __builtin_nanf("");  // an infinity is among them: a root of 0 would make zeros of the others
+    // (an infinity is among them: a root of 0 would make zeros of the others)
+    if (mean == INFINITY) mean = __builtin_nanf("");
   }
   return __builtin_amdgcn_rsqf(mean);
 }
